@@ -65,7 +65,9 @@ extern "C" {
 
 /* 101: mcsd_desc gained node_residual at its end (a caller built against 100 must be rebuilt)
  * 102: out_status describes the walk only and is written, not accumulated; mcsd_set_option,
- *      mcsd_get_option, mcsd_release_host_staging; desc->reserved is checked; mcsd_shard_* */
+ *      mcsd_get_option, mcsd_release_host_staging; desc->reserved is checked; mcsd_shard_*
+ * (102 also gained the operators around the step, from mcsd_apply_logit_rules on; nothing that was
+ *  there changed, so a caller built against 102 needs no rebuild) */
 #define MCSD_VERSION 102
 
 /* logit element types (both logit tensors share one) */
@@ -87,6 +89,7 @@ extern "C" {
 #define MCSD_MAX_NODES 512     /* nodes per tree, root included            */
 #define MCSD_MAX_CHILDREN 32   /* candidates per node (the paper uses <= 32) */
 #define MCSD_MAX_VOCAB 65536   /* vocabulary size                          */
+#define MCSD_MAX_SEQUENCES 4096 /* sequences of one mcsd_build_page_tables call */
 
 /* return codes */
 #define MCSD_OK 0
@@ -110,6 +113,8 @@ extern "C" {
 #define MCSD_STATUS_BAD_TOKEN 2  /* a candidate token outside [0, vocab): rejected       */
 #define MCSD_STATUS_NO_MASS 4    /* endpoint draw from a distribution of mass 0 / NaN    */
 #define MCSD_STATUS_TIMEOUT 8    /* a bounded on-chip wait expired; results invalid      */
+#define MCSD_STATUS_NO_PAGES 16  /* mcsd_build_page_tables: no pages for this sequence   */
+#define MCSD_STATUS_BAD_MASK 32  /* mcsd_apply_logit_rules: mask_index beyond the masks  */
 
 /* Options of mcsd_set_option: process-wide tuning and test overrides, 0 = library default.
  * Some also take their initial value from the environment variable of the same
@@ -461,6 +466,170 @@ int mcsd_shard_finish(const mcsd_shard_desc *desc, const void *target_slice, con
 /* out_tokens[b][accept_len[b]] = endpoint_all[b] (the reduced endpoint_part). */
 int mcsd_shard_commit(const mcsd_shard_desc *desc, const int32_t *tree_parent, const int32_t *endpoint_all,
                       const int32_t *accept_len, int32_t *out_tokens);
+
+/*
+ * The steps around the verification on the serving side: rules on the logits it reads, the pages of
+ * the key/value cache, the cache in 4 bits, attention of a draft tree over it, and the move of the
+ * accepted rows inside it.  As above: nothing is allocated, all work is enqueued on the given stream,
+ * an error code means that nothing was enqueued, and every call can be captured in a CUDA graph.
+ */
+
+/*
+ * Penalties for repeated tokens, biases and grammar masks on the logits of a draft tree, target or
+ * draft, ahead of mcsd_sample_candidates and mcsd_verify.  For node n of sequence b and token x let
+ *   c    = occurrences of x among the generated tokens of the history and the tokens of the nodes on
+ *          the path from the root to n (cand_tokens; the root itself is the last history token),
+ *   seen = c > 0 or x occurs in the prompt part of the history;
+ * then, in float32 and in this order,
+ *   l := l > 0 ? l / repetition[b] : l * repetition[b]      if seen
+ *   l := l - frequency[b] * c - presence[b]                 if c > 0
+ *   l := l + bias_values[b][i], bias_ids[b][i] == x         (an id that occurs twice: the highest i)
+ *   l := -inf                                               if the mask of (b, n) has bit x == 0
+ * rounded once to the logits' type.  Tokens outside [0, vocab) in any list are ignored.  A mask that
+ * leaves nothing gives a row of -inf, which mcsd_verify reports as MCSD_STATUS_NO_MASS.
+ * Every pointer is device memory; a NULL switches its rule off.
+ */
+typedef struct mcsd_logit_rules {
+    const int32_t *history;     /* [B][ld_history] tokens: the prompt, then what was generated, the
+                                   root of the tree (the last committed token) included              */
+    const int32_t *history_len; /* [B] tokens used of each row, clipped to [0, n_history]            */
+    const int32_t *prompt_len;  /* [B] tokens of each row that are prompt; NULL: none                */
+    int64_t ld_history;         /* entries between rows, >= n_history                                 */
+    const float *repetition;    /* [B] > 0; 1 is neutral                                              */
+    const float *frequency;     /* [B] 0 is neutral                                                   */
+    const float *presence;      /* [B] 0 is neutral                                                   */
+    const int32_t *bias_ids;    /* [B][n_bias]                                                        */
+    const float *bias_values;   /* [B][n_bias]                                                        */
+    const uint32_t *masks;      /* [n_masks][ld_mask] words, bit x % 32 of word x / 32 is token x      */
+    const int32_t *mask_index;  /* [B][n_nodes] row of masks, < 0: no mask; a row that is not there:
+                                   no mask and MCSD_STATUS_BAD_MASK.  NULL: row b * n_nodes + n       */
+    int64_t n_masks, ld_mask;   /* ld_mask >= (vocab + 31) / 32                                        */
+    int32_t n_history, n_bias;  /* columns of history, and of bias_ids and bias_values                */
+} mcsd_logit_rules;
+
+/* logits [B][rows_per_tree][ld_in] -> out [B][rows_per_tree][ld_out], rows node_begin .. node_end - 1
+ * of every tree (rows_per_tree: n_nodes for target logits, n_internal for draft logits); other rows
+ * and the padding behind a row are left alone.  out == logits (with ld_out == ld_in) works in place
+ * and then only touches the tokens some rule concerns; any other overlap is not allowed.  Of the
+ * descriptor batch, n_nodes, vocab, dtype, stream and out_status (bits are added, not cleared) are
+ * read.  cand_tokens [B][n_nodes] may be NULL when no penalty is given. */
+int mcsd_apply_logit_rules(const mcsd_desc *desc, const mcsd_logit_rules *rules, const int32_t *tree_parent,
+                           const int32_t *cand_tokens, const void *logits, int64_t ld_in, void *out, int64_t ld_out,
+                           int32_t rows_per_tree, int32_t node_begin, int32_t node_end);
+
+/*
+ * Page tables and slot maps of a paged key/value cache, from the lengths of the requests.  Sequence b
+ * holds start[b] positions and gets count[b] more (a prompt, a chunk of it, or n_nodes tree nodes), so
+ * it wants ceil((start + count) / page_size) pages.  Missing pages are taken from the head of a ring
+ * of free pages in sequence order; surplus ones (a shorter length than before; start = count = 0 ends
+ * a request) go to its tail and are not handed out in the same call.  A sequence the ring cannot
+ * serve, and every later one that wants more pages, or one that wants more than max_pages, keeps what
+ * it has: MCSD_STATUS_NO_PAGES and slots of -1.  start[b] < 0 marks an unused batch entry: nothing
+ * about it changes and it has no tokens.
+ */
+typedef struct mcsd_page_desc {
+    int32_t batch;          /* <= MCSD_MAX_SEQUENCES                                                  */
+    int32_t page_size;      /* 16, 32, 64 or 128 positions                                            */
+    int32_t max_pages;      /* columns of page_table that exist                                       */
+    int32_t new_tokens;     /* count of every sequence where count is NULL                            */
+    int32_t ring_capacity;  /* entries of ring: at least the number of pages there are                */
+    int32_t reserved;       /* must be 0                                                              */
+    int64_t ld_table;       /* entries between rows of page_table, >= max_pages                       */
+    int64_t n_slots;        /* entries of slots; tokens beyond are not written                        */
+    const int32_t *start;   /* [B]                                                                    */
+    const int32_t *count;   /* [B], or NULL                                                           */
+    int32_t *page_table;    /* [B][ld_table]: entries [held, wanted) are written, the others kept     */
+    int32_t *held;          /* [B] pages each sequence holds                                          */
+    int32_t *held_out;      /* [B] pages held afterwards; NULL: written to held                       */
+    int32_t *ring;          /* [ring_capacity] page numbers                                           */
+    int32_t *ring_state;    /* [4]: head, free pages, 0, 0 (the last two are used inside a call)      */
+    int32_t *ring_state_out;/* [4] state afterwards; NULL: written to ring_state                      */
+    int64_t *slots;         /* [n_slots] or NULL: page * page_size + row of token i of sequence b at
+                               cu_tokens[b] + i; entries behind the last token are left alone          */
+    int32_t *cu_tokens;     /* [B + 1] or NULL: exclusive sums of the counts                          */
+    int32_t *status;        /* [B] or NULL: 0 or MCSD_STATUS_NO_PAGES                                 */
+    void *stream;
+} mcsd_page_desc;
+int mcsd_build_page_tables(const mcsd_page_desc *desc);
+
+/*
+ * One layer's key/value cache in 4 bits.  A row is one token of one key/value head, D numbers x:
+ *   scale = half((max - min) / 15),  mid = half(min + 8 scale)           (float32 first, saturated to +-65504)
+ *   code  = clamp(rint((x - mid) / scale) + 8, 0, 15), 8 where scale is 0  (ties to even)
+ *   value = mid + scale * (code - 8)
+ * (a row with an infinity or a NaN has mid = NaN, scale = 0: it reads as NaN).  The page of one head is
+ *   key codes [page_size][D / 2] | value codes [page_size][D / 2] | key (scale, mid) [page_size][2] half |
+ *   value (scale, mid) [page_size][2] half
+ * = page_size * (D + 8) bytes; element 2 i of a row sits in the low four bits of its byte i.  Heads of a
+ * page follow each other.
+ */
+typedef struct mcsd_kv_cache {
+    void *pages;          /* device, 16-byte aligned: [n_pages] pages of n_heads blocks                */
+    int64_t page_stride;  /* bytes between pages, a multiple of 16, >= n_heads * mcsd_kv_block_bytes    */
+    int32_t n_pages;
+    int32_t n_heads;      /* key/value heads                                                          */
+    int32_t head_dim;     /* D: 64 or 128                                                             */
+    int32_t page_size;    /* 16, 32, 64 or 128                                                        */
+} mcsd_kv_cache;
+
+/* Bytes of the block of one head in one page; 0 for a size that is not supported. */
+size_t mcsd_kv_block_bytes(int32_t head_dim, int32_t page_size);
+
+/* Quantises rows and stores them at slots (mcsd_build_page_tables); a slot outside the cache (-1) skips
+ * its token.  Two tokens must not share a slot.  keys, values: device, element (t, h, d) at t * token_stride +
+ * h * head_stride + d, in elements; dtype MCSD_DTYPE_*. */
+int mcsd_append_kv(const mcsd_kv_cache *cache, const void *keys, int64_t key_token_stride, int64_t key_head_stride,
+                   const void *values, int64_t value_token_stride, int64_t value_head_stride, int32_t dtype,
+                   int64_t n_tokens, const int64_t *slots, void *stream);
+
+/* Values of the rows at slots, in dtype; rows of slots outside the cache are left as they are.  Either
+ * output may be NULL. */
+int mcsd_read_kv(const mcsd_kv_cache *cache, void *keys, int64_t key_token_stride, int64_t key_head_stride,
+                 void *values, int64_t value_token_stride, int64_t value_head_stride, int32_t dtype,
+                 int64_t n_tokens, const int64_t *slots, void *stream);
+
+/*
+ * Attention of a flattened draft tree (Section 3.3) over the cache above.  Sequence b has its committed
+ * prefix at positions 0 .. prefix_len[b] - 1 and node n of the tree at position prefix_len[b] + n (rows
+ * that mcsd_append_kv stored there); position t lies in row t % page_size of page page_table[b][t /
+ * page_size].  Node n sees the whole prefix, its ancestors and itself:
+ *   s_j = scale * <q, k_j>,  out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j)
+ * with q and out per query head; query head h reads key/value head h / (n_heads / cache->n_heads).  A tree
+ * of one node is plain decoding.  Positions beyond the table or in a page entry outside [0, n_pages)
+ * are not there; a row that sees no position is 0 with lse = -inf.  prefix_len[b] < 0 marks an unused
+ * batch entry: its rows of out and lse are left as they were.
+ */
+typedef struct mcsd_attention_desc {
+    int32_t batch;
+    int32_t n_nodes;         /* <= MCSD_MAX_NODES                                                     */
+    int32_t n_heads;         /* query heads, a multiple of cache->n_heads                              */
+    int32_t dtype;           /* of q and out: MCSD_DTYPE_BF16 or MCSD_DTYPE_F16                        */
+    int32_t max_pages;       /* columns of page_table that exist; max_pages * page_size < 2^31         */
+    int32_t reserved;        /* must be 0                                                             */
+    int64_t ld_table;        /* entries between rows of page_table, >= max_pages                       */
+    int64_t q_seq_stride, q_node_stride, q_head_stride;       /* in elements; the D numbers of a row    */
+    int64_t out_seq_stride, out_node_stride, out_head_stride; /* follow each other                      */
+    float scale;             /* finite                                                                */
+    void *stream;
+    void *workspace;         /* device scratch, 256-byte aligned, caller-owned; overwritten            */
+    size_t workspace_bytes;  /* >= mcsd_tree_attention_workspace_bytes                                 */
+} mcsd_attention_desc;
+
+/* Depends on the sizes only, not on the lengths; 0 for a descriptor that is not valid. */
+size_t mcsd_tree_attention_workspace_bytes(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache);
+
+/* q, out device as described; lse device [B][n_nodes][n_heads] float32 or NULL. */
+int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
+                        const int32_t *prefix_len, const int32_t *tree_parent, const void *q, void *out, float *lse);
+
+/* mcsd_gather_accepted_kv for the paged cache: the row of the i-th accepted token's node moves from position
+ * prefix_len[b] + path_nodes[b][i] to prefix_len[b] + 1 + i, in place, for every head and for n_layers caches that
+ * lie layer_stride bytes (a multiple of 16) apart behind cache->pages.  Entries that are skipped there are
+ * skipped here, as are positions that the page table does not have and entries with prefix_len[b] < 0. */
+int mcsd_gather_accepted_pages(const mcsd_kv_cache *cache, int64_t n_layers, int64_t layer_stride,
+                               const int32_t *page_table, int64_t ld_table, int32_t max_pages, int32_t batch,
+                               const int32_t *prefix_len, const int32_t *path_nodes, const int32_t *accept_len,
+                               int32_t gamma, void *stream);
 
 /* Frees the device staging buffers and streams mcsd_verify_host keeps on the current
  * device (allocating again on its next call).  Returns MCSD_OK or MCSD_ERR_CUDA. */

@@ -20,15 +20,17 @@ LIB_PATH = os.path.join(_HERE, "libmcsd.so")
 DEBUG_LIB_PATH = os.path.join(_HERE, "libmcsd_debug.so")      # the checked build (see mcsd_debug_bounds_hits)
 
 MCSD_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
-STATUS_DEGENERATE, STATUS_BAD_TOKEN, STATUS_NO_MASS, STATUS_TIMEOUT = 1, 2, 4, 8
-MAX_NODES, MAX_CHILDREN, MAX_VOCAB = 512, 32, 65536
+STATUS_DEGENERATE, STATUS_BAD_TOKEN, STATUS_NO_MASS, STATUS_TIMEOUT, STATUS_NO_PAGES, STATUS_BAD_MASK = 1, 2, 4, 8, 16, 32
+MAX_NODES, MAX_CHILDREN, MAX_VOCAB, MAX_SEQUENCES = 512, 32, 65536, 4096
 
 EXPORTS = ("mcsd_verify", "mcsd_verify_nodes", "mcsd_verify_walk", "mcsd_verify_host", "mcsd_verify_static", "mcsd_verify_path", "mcsd_sample_candidates", "mcsd_tree_attention_layout",
            "mcsd_gather_accepted_kv",
            "mcsd_workspace_bytes", "mcsd_tree_depth", "mcsd_last_launch_count", "mcsd_status_string",
            "mcsd_version", "mcsd_set_option", "mcsd_get_option", "mcsd_release_host_staging",
            "mcsd_shard_columns", "mcsd_shard_workspace_bytes", "mcsd_shard_rounds", "mcsd_shard_partials",
-           "mcsd_shard_decide", "mcsd_shard_endpoint", "mcsd_shard_finish", "mcsd_shard_commit", "mcsd_debug_bounds_hits", "mcsd_last_kernel_times")
+           "mcsd_shard_decide", "mcsd_shard_endpoint", "mcsd_shard_finish", "mcsd_shard_commit", "mcsd_debug_bounds_hits", "mcsd_last_kernel_times",
+           "mcsd_apply_logit_rules", "mcsd_build_page_tables", "mcsd_kv_block_bytes", "mcsd_append_kv", "mcsd_read_kv",
+           "mcsd_tree_attention", "mcsd_tree_attention_workspace_bytes", "mcsd_gather_accepted_pages")
 OPT_CLUSTER, OPT_EPT, OPT_DIRECT, OPT_SAMPLE_AHEAD, OPT_WAIT_POLLS, OPT_TEST_EXTRA_TX, OPT_PDL, OPT_TEST_SHRINK_RANGES, OPT_SPLIT, OPT_TIME_KERNELS, OPT_TRACE, OPT_WALK_CLUSTER = range(12)
 
 
@@ -50,6 +52,38 @@ class McsdShardDesc(ctypes.Structure):
                 ("ld_target", ctypes.c_int64), ("ld_draft", ctypes.c_int64),
                 ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
                 ("node_ratio", ctypes.c_void_p), ("node_accept", ctypes.c_void_p)]
+
+
+class McsdLogitRules(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("history_len", ctypes.c_void_p), ("prompt_len", ctypes.c_void_p),
+                ("ld_history", ctypes.c_int64), ("repetition", ctypes.c_void_p), ("frequency", ctypes.c_void_p),
+                ("presence", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p), ("bias_values", ctypes.c_void_p),
+                ("masks", ctypes.c_void_p), ("mask_index", ctypes.c_void_p), ("n_masks", ctypes.c_int64),
+                ("ld_mask", ctypes.c_int64), ("n_history", ctypes.c_int32), ("n_bias", ctypes.c_int32)]
+
+
+class McsdPageDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("new_tokens", ctypes.c_int32), ("ring_capacity", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("ld_table", ctypes.c_int64), ("n_slots", ctypes.c_int64), ("start", ctypes.c_void_p),
+                ("count", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("held", ctypes.c_void_p),
+                ("held_out", ctypes.c_void_p), ("ring", ctypes.c_void_p), ("ring_state", ctypes.c_void_p),
+                ("ring_state_out", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("cu_tokens", ctypes.c_void_p),
+                ("status", ctypes.c_void_p), ("stream", ctypes.c_void_p)]
+
+
+class McsdKvCache(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32)]
+
+
+class McsdAttentionDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_nodes", ctypes.c_int32), ("n_heads", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("ld_table", ctypes.c_int64), ("q_seq_stride", ctypes.c_int64), ("q_node_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("out_seq_stride", ctypes.c_int64),
+                ("out_node_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64), ("scale", ctypes.c_float),
+                ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 class McsdError(RuntimeError):
@@ -129,6 +163,24 @@ def load_library(path: Optional[str] = None):
     lib.mcsd_last_kernel_times.restype = ctypes.c_int
     lib.mcsd_debug_bounds_hits.argtypes = [ctypes.c_int]
     lib.mcsd_debug_bounds_hits.restype = ctypes.c_longlong
+    cp = ctypes.POINTER(McsdKvCache)
+    lib.mcsd_apply_logit_rules.argtypes = [dp, ctypes.POINTER(McsdLogitRules), vp, vp, vp, i64, vp, i64, i32, i32, i32]
+    lib.mcsd_apply_logit_rules.restype = ctypes.c_int
+    lib.mcsd_build_page_tables.argtypes = [ctypes.POINTER(McsdPageDesc)]
+    lib.mcsd_build_page_tables.restype = ctypes.c_int
+    lib.mcsd_kv_block_bytes.argtypes = [i32, i32]
+    lib.mcsd_kv_block_bytes.restype = ctypes.c_size_t
+    lib.mcsd_append_kv.argtypes = [cp, vp, i64, i64, vp, i64, i64, i32, i64, vp, vp]
+    lib.mcsd_append_kv.restype = ctypes.c_int
+    lib.mcsd_read_kv.argtypes = [cp, vp, i64, i64, vp, i64, i64, i32, i64, vp, vp]
+    lib.mcsd_read_kv.restype = ctypes.c_int
+    ap = ctypes.POINTER(McsdAttentionDesc)
+    lib.mcsd_tree_attention_workspace_bytes.argtypes = [ap, cp]
+    lib.mcsd_tree_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.mcsd_tree_attention.argtypes = [ap, cp, vp, vp, vp, vp, vp, vp]
+    lib.mcsd_tree_attention.restype = ctypes.c_int
+    lib.mcsd_gather_accepted_pages.argtypes = [cp, i64, i64, vp, i64, i32, i32, vp, vp, vp, i32, vp]
+    lib.mcsd_gather_accepted_pages.restype = ctypes.c_int
     if path is None:
         _lib = lib
     return lib
@@ -424,6 +476,315 @@ def mcsd_verify_host(target, draft, parent, cand, unif, temperature: float, mode
                                 _ptr(unif), float(temperature), int(mode), _ptr(accept_len), _ptr(tokens),
                                 _ptr(residual), _ptr(status)))
     return VerifyOutput(accept_len, tokens, residual, status)
+
+
+# ---------------------------------------------------------------- the steps around the verification
+class _on_device:
+    """Makes the device of a tensor current for a call (the library works on the current device)."""
+
+    def __init__(self, device: torch.device):
+        index = device.index if device.index is not None else torch.cuda.current_device()
+        self.guard = torch.cuda.device(index) if index != torch.cuda.current_device() else None
+        self.stream = None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _device_tensor(t: Optional[torch.Tensor], dtype, shape, device, name: str, contiguous: bool = True):
+    if t is None:
+        return None
+    assert t.device == device, f"{name} must be on {device}"
+    assert t.dtype == dtype, f"{name} must be {dtype}"
+    assert shape is None or tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}"
+    assert not contiguous or t.is_contiguous(), f"{name} must be contiguous"
+    return t
+
+
+class LogitRules:
+    """The rules of mcsd_apply_logit_rules (see mcsd.h); every argument is a device tensor or None.
+    history [B, H] int32 with unit stride along a row; history_len, prompt_len [B] int32; repetition, frequency,
+    presence [B] float32; bias_ids [B, K] int32 with bias_values [B, K] float32; masks [M, words] int32 with unit
+    stride along a row; mask_index [B, n_nodes] int32.  The tensors are kept and may change between calls."""
+
+    def __init__(self, *, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None, presence=None,
+                 bias_ids=None, bias_values=None, masks=None, mask_index=None):
+        given = [t for t in (history, repetition, frequency, presence, bias_ids, masks) if t is not None]
+        self.tensors = (history, history_len, prompt_len, repetition, frequency, presence, bias_ids, bias_values, masks, mask_index)
+        self.device = given[0].device if given else None
+        self.batch = next((t.shape[0] for t in (history, repetition, frequency, presence, bias_ids) if t is not None), None)
+        r = self.desc = McsdLogitRules()
+        B, dev = self.batch, self.device
+        if history is not None:
+            assert history.dim() == 2 and (history.shape[1] <= 1 or history.stride(1) == 1), "history rows must be contiguous"
+            assert history_len is not None, "history needs history_len"
+            _device_tensor(history, torch.int32, None, dev, "history", contiguous=False)
+            r.history = history.data_ptr()
+            r.n_history = int(history.shape[1])
+            r.ld_history = int(history.stride(0)) if history.shape[0] > 1 else r.n_history
+        r.history_len = _ptr(_device_tensor(history_len, torch.int32, (B,), dev, "history_len"))
+        r.prompt_len = _ptr(_device_tensor(prompt_len, torch.int32, (B,), dev, "prompt_len"))
+        r.repetition = _ptr(_device_tensor(repetition, torch.float32, (B,), dev, "repetition"))
+        r.frequency = _ptr(_device_tensor(frequency, torch.float32, (B,), dev, "frequency"))
+        r.presence = _ptr(_device_tensor(presence, torch.float32, (B,), dev, "presence"))
+        if bias_ids is not None:
+            assert bias_values is not None and bias_ids.shape == bias_values.shape
+            r.n_bias = int(bias_ids.shape[1])
+            if r.n_bias:
+                r.bias_ids = _ptr(_device_tensor(bias_ids, torch.int32, (B, r.n_bias), dev, "bias_ids"))
+                r.bias_values = _ptr(_device_tensor(bias_values, torch.float32, (B, r.n_bias), dev, "bias_values"))
+        self.mask_index = mask_index
+        if masks is not None:
+            assert masks.dim() == 2 and (masks.shape[1] <= 1 or masks.stride(1) == 1), "mask rows must be contiguous"
+            _device_tensor(masks, torch.int32, None, dev, "masks", contiguous=False)
+            r.masks, r.n_masks = masks.data_ptr(), int(masks.shape[0])
+            r.ld_mask = int(masks.stride(0)) if masks.shape[0] > 1 else int(masks.shape[1])
+            self.mask_words = int(masks.shape[1])
+            if mask_index is not None:
+                _device_tensor(mask_index, torch.int32, None, dev, "mask_index")
+                r.mask_index = mask_index.data_ptr()
+
+
+def mcsd_apply_logit_rules(logits: torch.Tensor, parent, cand: Optional[torch.Tensor], rules: LogitRules, *,
+                           out: Optional[torch.Tensor] = None, node_begin: int = 0, node_end: Optional[int] = None,
+                           status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Applies the rules to rows [node_begin, node_end) of logits [B, rows, V] (rows: n_nodes for target logits, n_internal
+    for draft logits).  out=None works in place; returns the tensor written."""
+    lib = load_library()
+    parent = np.ascontiguousarray(parent, dtype=np.int32)
+    assert logits.is_cuda and logits.dim() == 3
+    B, rows, V = logits.shape
+    n_nodes = int(parent.shape[0])
+    out = logits if out is None else out
+    assert out.shape == logits.shape and out.dtype == logits.dtype and out.device == logits.device
+    assert rules.device is None or rules.device == logits.device
+    assert rules.batch is None or rules.batch == B, "the rules are for another batch size"
+    if rules.mask_index is not None:
+        assert tuple(rules.mask_index.shape) == (B, n_nodes)
+    elif rules.desc.masks:
+        assert rules.desc.n_masks >= B * n_nodes, "masks without mask_index hold a row per node"
+    assert not rules.desc.masks or rules.mask_words >= (V + 31) // 32, "mask rows are too short for the vocabulary"
+    _device_tensor(cand, torch.int32, (B, n_nodes), logits.device, "cand")
+    _device_tensor(status, torch.int32, (B,), logits.device, "status")
+    d = McsdDesc()
+    d.batch, d.n_nodes, d.vocab, d.dtype, d.out_status = B, n_nodes, V, MCSD_DTYPE[logits.dtype], _ptr(status)
+    with _on_device(logits.device) as stream:
+        d.stream = stream
+        _check(lib.mcsd_apply_logit_rules(ctypes.byref(d), ctypes.byref(rules.desc), parent.ctypes.data, _ptr(cand),
+                                          _ptr(logits), _row_stride(logits) if rows else V, _ptr(out),
+                                          _row_stride(out) if rows else V, rows, int(node_begin),
+                                          int(rows if node_end is None else node_end)))
+    return out
+
+
+class PageTables:
+    """Page tables of a batch and the ring of free pages behind them (see mcsd.h): holds the descriptor, so that a
+    step allocates nothing.  table [B, max_pages] int32, held [B] int32, ring [capacity] int32, ring_state [4] int32
+    (head, free pages, 0, 0).  Without held_out and ring_state_out the state is advanced in place."""
+
+    def __init__(self, table, held, ring, ring_state, page_size: int, *, held_out=None, ring_state_out=None):
+        self.lib = load_library()
+        dev, (B, W) = table.device, table.shape
+        assert table.is_cuda and table.dtype == torch.int32 and (W <= 1 or table.stride(1) == 1)
+        _device_tensor(held, torch.int32, (B,), dev, "held")
+        _device_tensor(ring, torch.int32, None, dev, "ring")
+        _device_tensor(ring_state, torch.int32, (4,), dev, "ring_state")
+        _device_tensor(held_out, torch.int32, (B,), dev, "held_out")
+        _device_tensor(ring_state_out, torch.int32, (4,), dev, "ring_state_out")
+        self.device, self.batch, self.page_size = dev, B, int(page_size)
+        self.table, self.held, self.ring, self.ring_state = table, held, ring, ring_state
+        self.held_out = held if held_out is None else held_out
+        self.ring_state_out = ring_state if ring_state_out is None else ring_state_out
+        self.cu_tokens = torch.empty(B + 1, dtype=torch.int32, device=dev)
+        self.status = torch.empty(B, dtype=torch.int32, device=dev)
+        d = self.desc = McsdPageDesc()
+        d.batch, d.page_size, d.max_pages, d.ring_capacity = B, self.page_size, W, int(ring.shape[0])
+        d.ld_table = int(table.stride(0)) if B > 1 else W
+        d.page_table, d.held, d.ring, d.ring_state = table.data_ptr(), held.data_ptr(), ring.data_ptr(), ring_state.data_ptr()
+        d.held_out, d.ring_state_out = _ptr(held_out), _ptr(ring_state_out)
+        d.cu_tokens, d.status = self.cu_tokens.data_ptr(), self.status.data_ptr()
+
+    @classmethod
+    def empty(cls, batch: int, max_pages: int, n_pages: int, page_size: int, device="cuda"):
+        """Tables of a batch that holds nothing yet, over a pool of n_pages free pages."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32), torch.arange(n_pages, **i32),
+                   torch.tensor([0, n_pages, 0, 0], **i32), page_size)
+
+    def mcsd_build_page_tables(self, start: torch.Tensor, count, *, slots: Optional[torch.Tensor] = None):
+        """start [B] int32; count: tokens per sequence, an int for all or [B] int32; slots: [n] int64, filled in packed
+        order (or None).  Returns slots."""
+        d = self.desc
+        d.start = _ptr(_device_tensor(start, torch.int32, (self.batch,), self.device, "start"))
+        if isinstance(count, torch.Tensor):
+            d.count, d.new_tokens = _ptr(_device_tensor(count, torch.int32, (self.batch,), self.device, "count")), 0
+        else:
+            d.count, d.new_tokens = None, int(count)
+        _device_tensor(slots, torch.int64, None, self.device, "slots")
+        d.slots, d.n_slots = _ptr(slots), 0 if slots is None else int(slots.numel())
+        with _on_device(self.device) as stream:
+            d.stream = stream
+            _check(self.lib.mcsd_build_page_tables(ctypes.byref(d)))
+        return slots
+
+
+def mcsd_kv_block_bytes(head_dim: int, page_size: int) -> int:
+    """Bytes of one head of one page of the 4-bit cache (0: a size that is not supported)."""
+    return int(load_library().mcsd_kv_block_bytes(int(head_dim), int(page_size)))
+
+
+class KvCache:
+    """The paged 4-bit key/value cache of one layer, pages [n_pages, heads, block] uint8, or of several layers,
+    [layers, n_pages, heads, block] (see mcsd.h for a block's layout); block = mcsd_kv_block_bytes(head_dim, page_size).
+    `layer(i)` is the cache of one of several layers."""
+
+    def __init__(self, pages: torch.Tensor, head_dim: int, page_size: int):
+        block = mcsd_kv_block_bytes(head_dim, page_size)
+        if block == 0:
+            _check(-10)
+        assert pages.is_cuda and pages.dtype == torch.uint8 and pages.dim() in (3, 4) and pages.shape[-1] == block
+        assert pages.stride(-1) == 1 and (pages.shape[-2] == 1 or pages.stride(-2) == block), "the heads of a page follow each other"
+        self.pages, self.device, self.head_dim, self.page_size = pages, pages.device, int(head_dim), int(page_size)
+        self.n_pages, self.n_heads = int(pages.shape[-3]), int(pages.shape[-2])
+        self.n_layers = int(pages.shape[0]) if pages.dim() == 4 else 1
+        self.layer_stride = int(pages.stride(0)) if pages.dim() == 4 else 0
+        c = self.desc = McsdKvCache()
+        c.pages, c.n_pages, c.n_heads = pages.data_ptr(), self.n_pages, self.n_heads
+        c.page_stride = int(pages.stride(-3)) if self.n_pages > 1 else self.n_heads * block
+        c.head_dim, c.page_size = self.head_dim, self.page_size
+
+    @classmethod
+    def empty(cls, n_pages: int, n_heads: int, head_dim: int, page_size: int, device="cuda", n_layers: Optional[int] = None):
+        lead = (n_pages,) if n_layers is None else (n_layers, n_pages)
+        block = mcsd_kv_block_bytes(head_dim, page_size)
+        if block == 0:
+            _check(-10)
+        return cls(torch.zeros(lead + (n_heads, block), dtype=torch.uint8, device=device), head_dim, page_size)
+
+    def layer(self, i: int) -> "KvCache":
+        assert self.pages.dim() == 4
+        return KvCache(self.pages[i], self.head_dim, self.page_size)
+
+
+def _rows_args(cache: KvCache, t: Optional[torch.Tensor], n: int, name: str):
+    if t is None:
+        return None, 0, 0
+    assert t.device == cache.device and tuple(t.shape) == (n, cache.n_heads, cache.head_dim) and t.stride(2) == 1, \
+        f"{name} must be [tokens, heads, head_dim] with contiguous rows on the cache's device"
+    return t.data_ptr(), (t.stride(0) if n > 1 else cache.n_heads * cache.head_dim), (t.stride(1) if cache.n_heads > 1 else cache.head_dim)
+
+
+def mcsd_append_kv(cache: KvCache, keys: torch.Tensor, values: torch.Tensor, slots: torch.Tensor) -> None:
+    """Quantises keys and values [tokens, heads, head_dim] and stores them at slots [tokens] int64 (-1: skipped)."""
+    assert cache.pages.dim() == 3, "one layer at a time: cache.layer(i)"
+    n = int(slots.shape[0])
+    _device_tensor(slots, torch.int64, (n,), cache.device, "slots")
+    assert keys.dtype == values.dtype
+    k, v = _rows_args(cache, keys, n, "keys"), _rows_args(cache, values, n, "values")
+    with _on_device(cache.device) as stream:
+        _check(load_library().mcsd_append_kv(ctypes.byref(cache.desc), *k, *v, MCSD_DTYPE[keys.dtype], n, slots.data_ptr(), stream))
+
+
+def mcsd_read_kv(cache: KvCache, slots: torch.Tensor, dtype: Optional[torch.dtype] = None, *, keys: Optional[torch.Tensor] = None,
+                 values: Optional[torch.Tensor] = None):
+    """(keys, values) [tokens, heads, head_dim] of the rows at slots; rows of slots outside the cache keep what the
+    outputs hold (zeros if made here).  With neither output given both are made, in dtype."""
+    assert cache.pages.dim() == 3, "one layer at a time: cache.layer(i)"
+    n = int(slots.shape[0])
+    _device_tensor(slots, torch.int64, (n,), cache.device, "slots")
+    if keys is None and values is None:
+        keys = torch.zeros((n, cache.n_heads, cache.head_dim), dtype=dtype or torch.float32, device=cache.device)
+        values = torch.zeros_like(keys)
+    given = (keys if keys is not None else values).dtype
+    assert all(t is None or t.dtype == given for t in (keys, values))
+    k, v = _rows_args(cache, keys, n, "keys"), _rows_args(cache, values, n, "values")
+    with _on_device(cache.device) as stream:
+        _check(load_library().mcsd_read_kv(ctypes.byref(cache.desc), *k, *v, MCSD_DTYPE[given], n, slots.data_ptr(), stream))
+    return keys, values
+
+
+@dataclass
+class AttentionOutput:
+    out: torch.Tensor                   # [B, n_nodes, n_heads, head_dim]
+    lse: Optional[torch.Tensor]         # [B, n_nodes, n_heads] float32
+
+
+class TreeAttention:
+    """Attention of a draft tree over a paged 4-bit cache: holds the descriptor, the outputs and the workspace of one
+    (batch, tree, heads, dtype, cache geometry) shape, so that repeated calls allocate nothing (see mcsd.h)."""
+
+    def __init__(self, batch: int, parent, n_heads: int, dtype: torch.dtype, cache: KvCache, max_pages: int, *, want_lse: bool = True):
+        self.lib = load_library()
+        self.parent = np.ascontiguousarray(parent, dtype=np.int32)
+        self.device, self.dtype = cache.device, dtype
+        self.batch, self.n_nodes, self.n_heads = int(batch), int(self.parent.shape[0]), int(n_heads)
+        self.head_dim, self.max_pages = cache.head_dim, int(max_pages)
+        self.geometry = (cache.n_heads, cache.head_dim, cache.page_size)
+        rc = self.lib.mcsd_tree_depth(self.parent.ctypes.data, self.n_nodes)
+        _check(rc if rc < 0 else 0)
+        self.out = torch.zeros((self.batch, self.n_nodes, self.n_heads, self.head_dim), dtype=dtype, device=self.device)
+        self.lse = torch.zeros((self.batch, self.n_nodes, self.n_heads), dtype=torch.float32, device=self.device) if want_lse else None
+        d = self.desc = McsdAttentionDesc()
+        d.batch, d.n_nodes, d.n_heads, d.dtype = self.batch, self.n_nodes, self.n_heads, MCSD_DTYPE[dtype]
+        d.max_pages, d.ld_table = self.max_pages, self.max_pages
+        d.q_seq_stride, d.q_node_stride, d.q_head_stride = self.out.stride()[:3]
+        d.out_seq_stride, d.out_node_stride, d.out_head_stride = self.out.stride()[:3]
+        ws = int(self.lib.mcsd_tree_attention_workspace_bytes(ctypes.byref(d), ctypes.byref(cache.desc)))
+        if ws == 0:
+            _check(self.lib.mcsd_tree_attention(ctypes.byref(d), ctypes.byref(cache.desc), None, None, self.parent.ctypes.data,
+                                                None, None, None))
+            _check(-2)
+        self.workspace = torch.empty(ws + 256, dtype=torch.uint8, device=self.device)
+        d.workspace = (self.workspace.data_ptr() + 255) // 256 * 256
+        d.workspace_bytes = ws
+
+    def mcsd_tree_attention(self, q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, prefix_len: torch.Tensor, *,
+                            scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> AttentionOutput:
+        """q [B, n_nodes, n_heads, head_dim] with contiguous rows; page_table [B, max_pages] int32; prefix_len [B] int32;
+        scale: 1 / sqrt(head_dim) if None.  out: a tensor like q to write to instead of this object's."""
+        d, shape = self.desc, (self.batch, self.n_nodes, self.n_heads, self.head_dim)
+        out = self.out if out is None else out
+        assert cache.pages.dim() == 3, "one layer at a time: cache.layer(i)"
+        assert cache.device == self.device and self.geometry == (cache.n_heads, cache.head_dim, cache.page_size)
+        for t in (q, out):
+            assert t.device == self.device and t.dtype == self.dtype and t.shape == shape and t.stride(3) == 1
+        _device_tensor(page_table, torch.int32, (self.batch, self.max_pages), self.device, "page_table", contiguous=False)
+        assert self.max_pages <= 1 or page_table.stride(1) == 1
+        _device_tensor(prefix_len, torch.int32, (self.batch,), self.device, "prefix_len")
+        d.ld_table = int(page_table.stride(0)) if self.batch > 1 else self.max_pages
+        d.q_seq_stride, d.q_node_stride, d.q_head_stride = q.stride()[:3]
+        d.out_seq_stride, d.out_node_stride, d.out_head_stride = out.stride()[:3]
+        d.scale = float(scale) if scale is not None else self.head_dim ** -0.5
+        with _on_device(self.device) as stream:
+            d.stream = stream
+            _check(self.lib.mcsd_tree_attention(ctypes.byref(d), ctypes.byref(cache.desc), page_table.data_ptr(),
+                                                prefix_len.data_ptr(), self.parent.ctypes.data, q.data_ptr(), out.data_ptr(),
+                                                _ptr(self.lse)))
+        return AttentionOutput(out, self.lse)
+
+
+def mcsd_gather_accepted_pages(cache: KvCache, page_table: torch.Tensor, prefix_len: torch.Tensor, path_nodes: torch.Tensor,
+                               accept_len: torch.Tensor) -> torch.Tensor:
+    """mcsd_gather_accepted_kv for the paged cache, all its layers in one launch; in place, returns cache.pages.
+    page_table [B, max_pages], path_nodes [B, gamma + 1], prefix_len and accept_len [B], all int32."""
+    B, W = page_table.shape
+    _device_tensor(page_table, torch.int32, None, cache.device, "page_table", contiguous=False)
+    assert W <= 1 or page_table.stride(1) == 1
+    _device_tensor(prefix_len, torch.int32, (B,), cache.device, "prefix_len")
+    _device_tensor(accept_len, torch.int32, (B,), cache.device, "accept_len")
+    _device_tensor(path_nodes, torch.int32, (B, path_nodes.shape[1]), cache.device, "path_nodes")
+    with _on_device(cache.device) as stream:
+        _check(load_library().mcsd_gather_accepted_pages(
+            ctypes.byref(cache.desc), cache.n_layers, cache.layer_stride, page_table.data_ptr(),
+            int(page_table.stride(0)) if B > 1 else W, W, B, prefix_len.data_ptr(), path_nodes.data_ptr(),
+            accept_len.data_ptr(), int(path_nodes.shape[1]) - 1, stream))
+    return cache.pages
 
 
 # ---------------------------------------------------------------- vocabulary split over several devices

@@ -14,8 +14,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmcsd.so")
 DEBUG_LIB = os.path.join(HERE, "libmcsd_debug.so")
-SOURCES = [os.path.join(CSRC, "mcsd_api.cu")]
-HEADERS = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")) + [os.path.join(ROOT, "include", "mcsd.h")]
+SOURCES = [os.path.join(CSRC, "mcsd_api.cu"), os.path.join(CSRC, "mcsd_ops.cu")]
+HEADERS = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))) + [os.path.join(ROOT, "include", "mcsd.h")]
 
 
 def _nvcc() -> str:
@@ -40,6 +40,7 @@ def build(force: bool = False, verbose: bool = False, debug_bounds: bool = False
         return lib
     tmp = lib + f".{os.getpid()}.tmp"
     cmd = [_nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+           "--threads", "0",   # the sources are compiled side by side
            "--shared", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            "-o", tmp] + SOURCES
     if debug_bounds:

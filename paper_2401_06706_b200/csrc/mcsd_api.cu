@@ -11,6 +11,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "mcsd_device.cuh"
+#include "mcsd_host.h"
 
 namespace mcsd {
 namespace {
@@ -816,6 +817,17 @@ int launch_walk(const Call &c, const void *target, const void *draft, const int3
 }
 
 }  // namespace
+}  // namespace mcsd
+
+namespace mcsd {
+// what the host code of the operators around the step shares with this file (mcsd_host.h)
+int tree_depth(const int32_t *parent, int n_nodes)
+{
+    TreePlan plan;
+    const int rc = plan_tree(parent, n_nodes, -1, &plan);
+    return rc == MCSD_OK ? plan.gamma : rc;
+}
+void set_last_launches(int n) { g_last_launches = n; }
 }  // namespace mcsd
 
 using namespace mcsd;

@@ -190,6 +190,51 @@ template <> struct Elem<MCSD_DTYPE_F16> {
     static __device__ __forceinline__ float max_final(const MaxAcc &a) { return fmaxf(from_word(a, 0), from_word(a, 1)); }
 };
 
+// Rounds kVec floats to one 16-byte vector, or stores one element (round to nearest even).
+template <int DT>
+__device__ __forceinline__ uint4 pack_elems(const float *f) {
+    uint4 r;
+    if constexpr (DT == MCSD_DTYPE_F32) {
+        r = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (DT == MCSD_DTYPE_BF16) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            } else {
+                const __half2 h = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&h);
+            }
+        }
+        r = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return r;
+}
+template <int DT>
+__device__ __forceinline__ void store_elem(void *base, long long i, float f) {
+    if constexpr (DT == MCSD_DTYPE_F32) static_cast<float *>(base)[i] = f;
+    else if constexpr (DT == MCSD_DTYPE_BF16) static_cast<__nv_bfloat16 *>(base)[i] = __float2bfloat16_rn(f);
+    else static_cast<__half *>(base)[i] = __float2half_rn(f);
+}
+// Plain (coherent) element load and predicated 128-bit load, for memory that the kernel may write as well.
+template <int DT>
+__device__ __forceinline__ float load_elem(const void *base, long long i) {
+    if constexpr (DT == MCSD_DTYPE_F32) return static_cast<const float *>(base)[i];
+    else if constexpr (DT == MCSD_DTYPE_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(base)[i]);
+    else return __half2float(static_cast<const __half *>(base)[i]);
+}
+__device__ __forceinline__ uint4 ld_plain_v4_if(const void *p, bool pred) {
+    uint4 r;
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %5, 0;\n\t"
+                 "mov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t"
+                 "@q ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "=&r"(r.x), "=&r"(r.y), "=&r"(r.z), "=&r"(r.w)
+                 : "l"(p), "r"(static_cast<uint32_t>(pred)) : "memory");
+    return r;
+}
+
 // ------------------------------------------------------------------ PTX helpers
 __device__ __forceinline__ uint32_t smem_u32(const void *p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
