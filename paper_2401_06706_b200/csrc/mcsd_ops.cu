@@ -147,6 +147,40 @@ int check_attention(const mcsd_attention_desc *d, const mcsd_kv_cache *cache)
     return MCSD_OK;
 }
 
+// CTAs the work is cut for: what is resident at once (three per SM), or one per unit where a call cannot
+// have more units than that.
+int attention_ctas(const mcsd_attention_desc *d, const mcsd_kv_cache *cache)
+{
+    int sms = sm_count();
+    if (sms <= 0) sms = 148;
+    const long long rows = static_cast<long long>(d->n_nodes) * (d->n_heads / cache->n_heads);
+    const long long blocks = (rows + kNarrowRows - 1) / kNarrowRows;
+    const long long units = (static_cast<long long>(d->max_pages) * cache->page_size + kAttUnit - 1) / kAttUnit;
+    const long long most = static_cast<long long>(d->batch) * cache->n_heads * blocks * (units > 0 ? units : 1);
+    const long long resident = 3LL * sms;
+    return static_cast<int>(most < 1 ? 1 : most < resident ? most : resident);
+}
+
+template <int DT, int D>
+int launch_narrow(const AttendParams &p, cudaStream_t st)
+{
+    constexpr int smem = kNarrowSmem<D>;
+    if (cudaFuncSetAttribute(narrow_kernel<DT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MCSD_ERR_CUDA;
+    narrow_kernel<DT, D><<<p.n_ctas, kNarrowWarps * 32, smem, st>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.batch * p.c.n_heads * p.n_blocks));
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, join_kernel<DT, D>, p) != cudaSuccess) return MCSD_ERR_CUDA;
+    return launched(2);
+}
+
 }  // namespace
 }  // namespace mcsd
 
@@ -279,7 +313,8 @@ int mcsd_read_kv(const mcsd_kv_cache *cache, void *keys, int64_t key_token_strid
 size_t mcsd_tree_attention_workspace_bytes(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache)
 {
     if (check_attention(desc, cache) != MCSD_OK) return 0;
-    return 256;
+    const size_t part = sizeof(float) * (cache->head_dim == 128 ? kPartFloats<128> : kPartFloats<64>);
+    return (2 * part * attention_ctas(desc, cache) + 255) / 256 * 256;
 }
 
 int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
@@ -305,18 +340,17 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     p.batch = desc->batch; p.n_nodes = desc->n_nodes; p.n_heads = desc->n_heads; p.max_pages = desc->max_pages;
     p.scale = desc->scale;
     for (int n = 0; n < desc->n_nodes; ++n) p.parent[n] = static_cast<int16_t>(tree_parent[n]);
-    const long long rows = static_cast<long long>(desc->batch) * desc->n_nodes * desc->n_heads;
-    const unsigned grid = static_cast<unsigned>((rows + 7) / 8);
+    p.group = desc->n_heads / cache->n_heads;
+    p.n_rows = desc->n_nodes * p.group;
+    p.n_blocks = (p.n_rows + kNarrowRows - 1) / kNarrowRows;
+    p.n_ctas = attention_ctas(desc, cache);
+    p.part = static_cast<float *>(desc->workspace);
+    p.q_vec = (reinterpret_cast<uintptr_t>(q) | 2ull * static_cast<unsigned long long>(desc->q_seq_stride | desc->q_node_stride |
+                                                                                       desc->q_head_stride)) % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(desc->stream);
     const bool bf = desc->dtype == MCSD_DTYPE_BF16;
-    if (cache->head_dim == 128) {
-        if (bf) attend_kernel<MCSD_DTYPE_BF16, 128><<<grid, 256, 0, st>>>(p);
-        else attend_kernel<MCSD_DTYPE_F16, 128><<<grid, 256, 0, st>>>(p);
-    } else {
-        if (bf) attend_kernel<MCSD_DTYPE_BF16, 64><<<grid, 256, 0, st>>>(p);
-        else attend_kernel<MCSD_DTYPE_F16, 64><<<grid, 256, 0, st>>>(p);
-    }
-    return launched(1);
+    if (cache->head_dim == 128) return bf ? launch_narrow<MCSD_DTYPE_BF16, 128>(p, st) : launch_narrow<MCSD_DTYPE_F16, 128>(p, st);
+    return bf ? launch_narrow<MCSD_DTYPE_BF16, 64>(p, st) : launch_narrow<MCSD_DTYPE_F16, 64>(p, st);
 }
 
 int mcsd_gather_accepted_pages(const mcsd_kv_cache *cache, int64_t n_layers, int64_t layer_stride, const int32_t *page_table,
