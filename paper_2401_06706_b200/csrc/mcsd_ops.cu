@@ -147,26 +147,33 @@ int check_attention(const mcsd_attention_desc *d, const mcsd_kv_cache *cache)
     return MCSD_OK;
 }
 
-// CTAs the work is cut for: what is resident at once (three per SM), or one per unit where a call cannot
-// have more units than that.
-int attention_ctas(const mcsd_attention_desc *d, const mcsd_kv_cache *cache)
+// How a call is laid out; depends on the sizes only.
+struct AttentionPlan {
+    int rows;       // rows of a block
+    int blocks;     // blocks per key/value head
+    int ctas;       // CTAs the work is cut for: what is resident at once, or one per unit where a call cannot have more
+};
+AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *cache)
 {
+    AttentionPlan plan;
     int sms = sm_count();
     if (sms <= 0) sms = 148;
     const long long rows = static_cast<long long>(d->n_nodes) * (d->n_heads / cache->n_heads);
-    const long long blocks = (rows + kNarrowRows - 1) / kNarrowRows;
+    plan.rows = rows <= 8 ? 8 : 16;
+    plan.blocks = static_cast<int>((rows + plan.rows - 1) / plan.rows);
     const long long units = (static_cast<long long>(d->max_pages) * cache->page_size + kAttUnit - 1) / kAttUnit;
-    const long long most = static_cast<long long>(d->batch) * cache->n_heads * blocks * (units > 0 ? units : 1);
-    const long long resident = 3LL * sms;
-    return static_cast<int>(most < 1 ? 1 : most < resident ? most : resident);
+    const long long most = static_cast<long long>(d->batch) * cache->n_heads * plan.blocks * (units > 0 ? units : 1);
+    const long long resident = static_cast<long long>(plan.rows == 8 ? kNarrowCtas<1> : kNarrowCtas<2>) * sms;
+    plan.ctas = static_cast<int>(most < 1 ? 1 : most < resident ? most : resident);
+    return plan;
 }
 
-template <int DT, int D>
+template <int DT, int D, int NB>
 int launch_narrow(const AttendParams &p, cudaStream_t st)
 {
-    constexpr int smem = kNarrowSmem<D>;
-    if (cudaFuncSetAttribute(narrow_kernel<DT, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MCSD_ERR_CUDA;
-    narrow_kernel<DT, D><<<p.n_ctas, kNarrowWarps * 32, smem, st>>>(p);
+    constexpr int smem = kNarrowSmem<D, NB>;
+    if (cudaFuncSetAttribute(narrow_kernel<DT, D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MCSD_ERR_CUDA;
+    narrow_kernel<DT, D, NB><<<p.n_ctas, kNarrowWarps * 32, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.batch * p.c.n_heads * p.n_blocks));
@@ -177,8 +184,14 @@ int launch_narrow(const AttendParams &p, cudaStream_t st)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, join_kernel<DT, D>, p) != cudaSuccess) return MCSD_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, join_kernel<DT, D, kNarrowRows<NB>>, p) != cudaSuccess) return MCSD_ERR_CUDA;
     return launched(2);
+}
+
+template <int DT, int D>
+int launch_attention(const AttendParams &p, int rows, cudaStream_t st)
+{
+    return rows == 8 ? launch_narrow<DT, D, 1>(p, st) : launch_narrow<DT, D, 2>(p, st);
 }
 
 }  // namespace
@@ -313,8 +326,8 @@ int mcsd_read_kv(const mcsd_kv_cache *cache, void *keys, int64_t key_token_strid
 size_t mcsd_tree_attention_workspace_bytes(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache)
 {
     if (check_attention(desc, cache) != MCSD_OK) return 0;
-    const size_t part = sizeof(float) * (cache->head_dim == 128 ? kPartFloats<128> : kPartFloats<64>);
-    return (2 * part * attention_ctas(desc, cache) + 255) / 256 * 256;
+    const AttentionPlan plan = attention_plan(desc, cache);
+    return (2 * sizeof(float) * part_floats(plan.rows, cache->head_dim) * static_cast<size_t>(plan.ctas) + 255) / 256 * 256;
 }
 
 int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
@@ -342,15 +355,16 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     for (int n = 0; n < desc->n_nodes; ++n) p.parent[n] = static_cast<int16_t>(tree_parent[n]);
     p.group = desc->n_heads / cache->n_heads;
     p.n_rows = desc->n_nodes * p.group;
-    p.n_blocks = (p.n_rows + kNarrowRows - 1) / kNarrowRows;
-    p.n_ctas = attention_ctas(desc, cache);
+    const AttentionPlan plan = attention_plan(desc, cache);
+    p.n_blocks = plan.blocks;
+    p.n_ctas = plan.ctas;
     p.part = static_cast<float *>(desc->workspace);
     p.q_vec = (reinterpret_cast<uintptr_t>(q) | 2ull * static_cast<unsigned long long>(desc->q_seq_stride | desc->q_node_stride |
                                                                                        desc->q_head_stride)) % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(desc->stream);
     const bool bf = desc->dtype == MCSD_DTYPE_BF16;
-    if (cache->head_dim == 128) return bf ? launch_narrow<MCSD_DTYPE_BF16, 128>(p, st) : launch_narrow<MCSD_DTYPE_F16, 128>(p, st);
-    return bf ? launch_narrow<MCSD_DTYPE_BF16, 64>(p, st) : launch_narrow<MCSD_DTYPE_F16, 64>(p, st);
+    if (cache->head_dim == 128) return bf ? launch_attention<MCSD_DTYPE_BF16, 128>(p, plan.rows, st) : launch_attention<MCSD_DTYPE_F16, 128>(p, plan.rows, st);
+    return bf ? launch_attention<MCSD_DTYPE_BF16, 64>(p, plan.rows, st) : launch_attention<MCSD_DTYPE_F16, 64>(p, plan.rows, st);
 }
 
 int mcsd_gather_accepted_pages(const mcsd_kv_cache *cache, int64_t n_layers, int64_t layer_stride, const int32_t *page_table,
