@@ -526,8 +526,8 @@ narrow_kernel(const __grid_constant__ AttendParams P)
     }
 }
 
-// Joins the partial results of items that the cut divided: one CTA per item, which finds the CTAs that
-// worked on it from the same arithmetic.
+// Joins the partial results of items that the cut divided: one CTA per item and eight of its rows, which
+// finds the CTAs that worked on the item from the same arithmetic.
 template <int DT, int D, int ROWS>
 __global__ void __launch_bounds__(128)
 join_kernel(const __grid_constant__ AttendParams P)
@@ -542,10 +542,10 @@ join_kernel(const __grid_constant__ AttendParams P)
     const int first = static_cast<int>(u0 / per), last = static_cast<int>((u0 + units - 1) / per);
     asm volatile("griddepcontrol.wait;" ::: "memory");   // (every thread: this kernel must not end before the one it follows)
     if (units == 0 || first == last) return;
-    const int head = item / P.n_blocks, row0 = (item - head * P.n_blocks) * ROWS;
+    const int head = item / P.n_blocks, row0 = (item - head * P.n_blocks) * ROWS, r0 = blockIdx.y * 8;
     auto part_of = [&](int cta) { return P.part + static_cast<long long>(2 * cta + (cta == first ? 1 : 0)) * part_floats(ROWS, D); };
-    for (int x = tid; x < ROWS * (D / 4); x += 128) {
-        const int r = x / (D / 4), c = (x % (D / 4)) * 4;
+    for (int x = tid; x < 8 * (D / 4); x += 128) {
+        const int r = r0 + x / (D / 4), c = (x % (D / 4)) * 4;
         if (row0 + r >= P.n_rows) break;
         float m = kNoTop;
         for (int k = first; k <= last; ++k) m = fmaxf(m, __ldcg(part_of(k) + ROWS * D + r));

@@ -8,6 +8,7 @@
 #include "mcsd_pages.cuh"
 #include "mcsd_cache.cuh"
 #include "mcsd_attend.cuh"
+#include "mcsd_attend_wide.cuh"
 #include "mcsd_host.h"
 
 namespace mcsd {
@@ -159,24 +160,24 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
     int sms = sm_count();
     if (sms <= 0) sms = 148;
     const long long rows = static_cast<long long>(d->n_nodes) * (d->n_heads / cache->n_heads);
-    plan.rows = rows <= 8 ? 8 : 16;
+    plan.rows = rows <= 8 ? 8 : rows <= 64 ? 16 : kWideRows;
     plan.blocks = static_cast<int>((rows + plan.rows - 1) / plan.rows);
     const long long units = (static_cast<long long>(d->max_pages) * cache->page_size + kAttUnit - 1) / kAttUnit;
     const long long most = static_cast<long long>(d->batch) * cache->n_heads * plan.blocks * (units > 0 ? units : 1);
-    const long long resident = static_cast<long long>(plan.rows == 8 ? kNarrowCtas<1> : kNarrowCtas<2>) * sms;
+    const long long resident = static_cast<long long>(plan.rows == 8 ? kNarrowCtas<1> : plan.rows == 16 ? kNarrowCtas<2> : 1) * sms;
     plan.ctas = static_cast<int>(most < 1 ? 1 : most < resident ? most : resident);
     return plan;
 }
 
-template <int DT, int D, int NB>
-int launch_narrow(const AttendParams &p, cudaStream_t st)
+// Launches the kernel that does the work and, as its programmatic dependent, the one that joins divided items.
+template <int DT, int D, int ROWS>
+int launch_with_join(void (*kernel)(const AttendParams), int threads, int smem, const AttendParams &p, cudaStream_t st)
 {
-    constexpr int smem = kNarrowSmem<D, NB>;
-    if (cudaFuncSetAttribute(narrow_kernel<DT, D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MCSD_ERR_CUDA;
-    narrow_kernel<DT, D, NB><<<p.n_ctas, kNarrowWarps * 32, smem, st>>>(p);
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MCSD_ERR_CUDA;
+    kernel<<<p.n_ctas, threads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.batch * p.c.n_heads * p.n_blocks));
+    cfg.gridDim = dim3(static_cast<unsigned>(p.batch * p.c.n_heads * p.n_blocks), ROWS / 8);
     cfg.blockDim = dim3(128);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -184,14 +185,16 @@ int launch_narrow(const AttendParams &p, cudaStream_t st)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, join_kernel<DT, D, kNarrowRows<NB>>, p) != cudaSuccess) return MCSD_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, join_kernel<DT, D, ROWS>, p) != cudaSuccess) return MCSD_ERR_CUDA;
     return launched(2);
 }
 
 template <int DT, int D>
 int launch_attention(const AttendParams &p, int rows, cudaStream_t st)
 {
-    return rows == 8 ? launch_narrow<DT, D, 1>(p, st) : launch_narrow<DT, D, 2>(p, st);
+    if (rows == 8) return launch_with_join<DT, D, 8>(narrow_kernel<DT, D, 1>, kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
+    if (rows == 16) return launch_with_join<DT, D, 16>(narrow_kernel<DT, D, 2>, kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
+    return launch_with_join<DT, D, kWideRows>(wide_kernel<DT, D>, kWideThreads, kWideSmem<D>, p, st);
 }
 
 }  // namespace
