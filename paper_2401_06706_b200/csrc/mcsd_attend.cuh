@@ -23,7 +23,7 @@ struct AttendParams {
     int32_t n_rows;                                 // n_nodes * group: rows that share a key/value head
     int32_t n_blocks;                               // blocks of rows per key/value head
     int32_t n_ctas;                                 // CTAs the work is cut for
-    int32_t q_vec;                                  // q rows may be read in 16-byte vectors
+    int32_t q_vec, o_vec;                           // rows of q may be read, those of out written in 16-byte vectors
     float scale;
     int16_t parent[MCSD_MAX_NODES];
 };

@@ -160,7 +160,7 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
     int sms = sm_count();
     if (sms <= 0) sms = 148;
     const long long rows = static_cast<long long>(d->n_nodes) * (d->n_heads / cache->n_heads);
-    plan.rows = rows <= 8 ? 8 : rows <= 64 ? 16 : kWideRows;
+    plan.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kWideRows;
     plan.blocks = static_cast<int>((rows + plan.rows - 1) / plan.rows);
     const long long units = (static_cast<long long>(d->max_pages) * cache->page_size + kAttUnit - 1) / kAttUnit;
     const long long most = static_cast<long long>(d->batch) * cache->n_heads * plan.blocks * (units > 0 ? units : 1);
@@ -364,6 +364,8 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     p.part = static_cast<float *>(desc->workspace);
     p.q_vec = (reinterpret_cast<uintptr_t>(q) | 2ull * static_cast<unsigned long long>(desc->q_seq_stride | desc->q_node_stride |
                                                                                        desc->q_head_stride)) % 16 == 0;
+    p.o_vec = (reinterpret_cast<uintptr_t>(out) | 2ull * static_cast<unsigned long long>(desc->out_seq_stride | desc->out_node_stride |
+                                                                                         desc->out_head_stride)) % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(desc->stream);
     const bool bf = desc->dtype == MCSD_DTYPE_BF16;
     if (cache->head_dim == 128) return bf ? launch_attention<MCSD_DTYPE_BF16, 128>(p, plan.rows, st) : launch_attention<MCSD_DTYPE_F16, 128>(p, plan.rows, st);
