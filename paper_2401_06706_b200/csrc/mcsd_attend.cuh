@@ -42,29 +42,36 @@ __device__ __forceinline__ int att_len(const AttendParams &P, int b)
 __device__ __forceinline__ int att_units(int len) { return len < 0 ? 0 : max((len + kAttUnit - 1) / kAttUnit, 1); }
 
 // Units before sequence `stop` (all of them for stop == batch) of one item per sequence; every lane gets the sum.
-__device__ __forceinline__ long long att_units_before(const AttendParams &P, int stop, int lane)
+// (The host refuses calls that could have 2^32 units in all.)
+__device__ __forceinline__ uint32_t att_units_before(const AttendParams &P, int stop, int lane)
 {
-    int sum = 0;                                    // (batch * positions / 128 of a cache that exists: far below 2^31)
-    for (int b = lane; b < stop; b += 32) sum += att_units(att_len(P, b));
-    return static_cast<long long>(__reduce_add_sync(0xffffffffu, sum));
+    uint32_t sum = 0;
+    for (int b = lane; b < stop; b += 32) sum += static_cast<uint32_t>(att_units(att_len(P, b)));
+    return __reduce_add_sync(0xffffffffu, sum);
+}
+// Units of one CTA's run.
+__device__ __forceinline__ uint32_t att_share(const AttendParams &P, uint32_t total)
+{
+    const uint32_t n = static_cast<uint32_t>(P.n_ctas);
+    return max(total / n + (total % n != 0u), 1u);
 }
 
-// Position in the cut: the sequence and the unit within its items.
-struct AttCursor { int b, len, units; long long at; };
+// Position in the cut: a sequence, its length and units, and the unit within its items.
+struct AttCursor { int b, len; uint32_t units, at; };
 
 // The sequence that holds unit `u` (in units of all items); u must be below the total.
-__device__ __forceinline__ AttCursor att_find(const AttendParams &P, long long u, int items, int lane)
+__device__ __forceinline__ AttCursor att_find(const AttendParams &P, uint32_t u, uint32_t items, int lane)
 {
     AttCursor c;
-    long long before = 0;
+    uint32_t before = 0;
     for (int b0 = 0;; b0 += 32) {
         const int b = b0 + lane;
         const int len = b < P.batch ? att_len(P, b) : -1;
-        const int n = att_units(len);
-        int incl = n;
+        const uint32_t n = static_cast<uint32_t>(att_units(len));
+        uint32_t incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, incl, o);
+            const uint32_t t = __shfl_up_sync(0xffffffffu, incl, o);
             if (lane >= o) incl += t;
         }
         const unsigned past = __ballot_sync(0xffffffffu, (before + incl) * items > u);
@@ -162,12 +169,11 @@ narrow_kernel(const __grid_constant__ AttendParams P)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
     const int ps = 1 << P.c.page_shift;
-    const int items = P.c.n_heads * P.n_blocks;
-    const long long total = att_units_before(P, P.batch, lane) * items;
-    const long long per = max((total + P.n_ctas - 1) / P.n_ctas, 1LL);
-    long long u = static_cast<long long>(blockIdx.x) * per;
-    const long long u_end = min(u + per, total);
-    if (u >= u_end) return;
+    const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
+    const uint32_t total = att_units_before(P, P.batch, lane) * items, per = att_share(P, total);
+    if (blockIdx.x > (total - 1) / per || total == 0) return;    // (runs of units before the last one are whole)
+    uint32_t u = blockIdx.x * per;
+    const uint32_t u_end = total - u < per ? total : u + per;
     AttCursor cur = att_find(P, u, items, lane);
     unsigned char *ring = s_ring + warp * STAGES * STAGE;
     auto kappa = [](int c) { return D == 128 ? c ^ ((c >> 1) & 1) : c ^ ((c >> 2) & 1); };
@@ -175,13 +181,13 @@ narrow_kernel(const __grid_constant__ AttendParams P)
     const int kg = kappa(g), ka = kappa(2 * t), kb = kappa(2 * t + 1);
 
     while (u < u_end) {
-        const int item = static_cast<int>(cur.at / cur.units);
-        const int k0 = static_cast<int>(cur.at - static_cast<long long>(item) * cur.units);
-        const int k1 = static_cast<int>(min(static_cast<long long>(cur.units), k0 + (u_end - u)));
+        const int item = static_cast<int>(cur.at / cur.units), units = static_cast<int>(cur.units);
+        const int k0 = static_cast<int>(cur.at - item * cur.units);
+        const int k1 = u_end - u < static_cast<uint32_t>(units - k0) ? k0 + static_cast<int>(u_end - u) : units;
         const int b = cur.b, len = cur.len, head = item / P.n_blocks, block = item - head * P.n_blocks;
         const int row0 = block * ROWS;
         const int prefix = P.prefix_len[b];
-        const bool whole = k0 == 0 && k1 == cur.units;
+        const bool whole = k0 == 0 && k1 == units;
 
         __syncthreads();                            // the shared memory of the item before is free
         // this warp's chunks: keys [128 k + 32 warp, + 32) for k = k0 .. k1 - 1, as far as there are keys
@@ -522,7 +528,7 @@ narrow_kernel(const __grid_constant__ AttendParams P)
         }
         u += k1 - k0;
         cur.at += k1 - k0;
-        if (u < u_end && cur.at >= static_cast<long long>(cur.units) * items) cur = att_find(P, u, items, lane);
+        if (u < u_end && cur.at >= cur.units * items) cur = att_find(P, u, items, lane);
     }
 }
 
@@ -533,12 +539,11 @@ __global__ void __launch_bounds__(128)
 join_kernel(const __grid_constant__ AttendParams P)
 {
     const int tid = threadIdx.x, lane = tid & 31;
-    const int items = P.c.n_heads * P.n_blocks;
-    const int b = blockIdx.x / items, item = blockIdx.x - b * items;
+    const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
+    const int b = static_cast<int>(blockIdx.x / items), item = static_cast<int>(blockIdx.x - b * items);
     const int len = att_len(P, b), units = att_units(len);
-    const long long total = att_units_before(P, P.batch, lane) * items;
-    const long long per = max((total + P.n_ctas - 1) / P.n_ctas, 1LL);
-    const long long u0 = att_units_before(P, b, lane) * items + static_cast<long long>(item) * units;
+    const uint32_t per = att_share(P, att_units_before(P, P.batch, lane) * items);
+    const uint32_t u0 = att_units_before(P, b, lane) * items + static_cast<uint32_t>(item) * units;
     const int first = static_cast<int>(u0 / per), last = static_cast<int>((u0 + units - 1) / per);
     asm volatile("griddepcontrol.wait;" ::: "memory");   // (every thread: this kernel must not end before the one it follows)
     if (units == 0 || first == last) return;

@@ -76,10 +76,13 @@ template <int N> __device__ __forceinline__ void regs_down() { asm volatile("set
 // is left waiting, and the rows are written as NaN.
 __device__ __forceinline__ void wide_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
     for (uint32_t i = 0; i < kWaitPolls; ++i) {
-        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
-        if (__any_sync(0xffffffffu, *dead)) return;
+        if (mbar_try_wait(bar, parity)) break;
+        if (*dead || i == kWaitPolls - 1) {
+            *dead = 1;
+            break;
+        }
     }
-    *dead = 1;
+    __syncwarp();
 }
 // One arrival for the whole warp, behind what all its lanes did.
 __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
@@ -152,24 +155,24 @@ wide_kernel(const __grid_constant__ AttendParams P)
     if (s_tmem != tmem) *dead = 1;                  // (cannot be: all columns are this CTA's)
 
     const int ps = 1 << P.c.page_shift;
-    const int items = P.c.n_heads * P.n_blocks;
-    const long long total = att_units_before(P, P.batch, lane) * items;
-    const long long per = max((total + P.n_ctas - 1) / P.n_ctas, 1LL);
-    const long long u_begin = static_cast<long long>(blockIdx.x) * per, u_end = min(u_begin + per, total);
+    const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
+    const uint32_t total = att_units_before(P, P.batch, lane) * items, per = att_share(P, total);
+    const bool any = total != 0 && blockIdx.x <= (total - 1) / per;               // (runs of units before the last one are whole)
+    const uint32_t u_begin = any ? blockIdx.x * per : 0, u_end = any ? (total - u_begin < per ? total : u_begin + per) : 0;
 
     // Every role goes over the same items; f(sequence, length, head, first row, first unit, last unit + 1, whole item).
     auto for_items = [&](auto f) {
         if (u_begin >= u_end) return;
         AttCursor cur = att_find(P, u_begin, items, lane);
-        for (long long u = u_begin; u < u_end;) {
-            const int item = static_cast<int>(cur.at / cur.units);
-            const int k0 = static_cast<int>(cur.at - static_cast<long long>(item) * cur.units);
-            const int k1 = static_cast<int>(min(static_cast<long long>(cur.units), k0 + (u_end - u)));
+        for (uint32_t u = u_begin; u < u_end;) {
+            const int item = static_cast<int>(cur.at / cur.units), units = static_cast<int>(cur.units);
+            const int k0 = static_cast<int>(cur.at - item * cur.units);
+            const int k1 = u_end - u < static_cast<uint32_t>(units - k0) ? k0 + static_cast<int>(u_end - u) : units;
             const int head = item / P.n_blocks;
-            f(cur.b, cur.len, head, (item - head * P.n_blocks) * kWideRows, k0, k1, k0 == 0 && k1 == cur.units);
+            f(cur.b, cur.len, head, (item - head * P.n_blocks) * kWideRows, k0, k1, k0 == 0 && k1 == units);
             u += k1 - k0;
             cur.at += k1 - k0;
-            if (u < u_end && cur.at >= static_cast<long long>(cur.units) * items) cur = att_find(P, u, items, lane);
+            if (u < u_end && cur.at >= cur.units * items) cur = att_find(P, u, items, lane);
         }
     };
 

@@ -160,7 +160,11 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
     int sms = sm_count();
     if (sms <= 0) sms = 148;
     const long long rows = static_cast<long long>(d->n_nodes) * (d->n_heads / cache->n_heads);
-    plan.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : kWideRows;
+    // Blocks of 16 rows read the keys again for every block, one of 128 takes about as long for few rows as for all.
+    // Measured (128 numbers a head, 8 sequences x 32 key heads x 2000 positions), blocks of 16 against one of 128: 45 rows
+    // 96 against 104 us, 60 rows 121 against 106 us; 4 sequences x 8 key heads x 16000 positions: 89 against 96 us, 109
+    // against 96 us.
+    plan.rows = rows <= 8 ? 8 : rows <= 48 ? 16 : kWideRows;
     plan.blocks = static_cast<int>((rows + plan.rows - 1) / plan.rows);
     const long long units = (static_cast<long long>(d->max_pages) * cache->page_size + kAttUnit - 1) / kAttUnit;
     const long long most = static_cast<long long>(d->batch) * cache->n_heads * plan.blocks * (units > 0 ? units : 1);
@@ -348,6 +352,11 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     if (!desc->workspace || reinterpret_cast<uintptr_t>(desc->workspace) % 256 != 0 ||
         desc->workspace_bytes < mcsd_tree_attention_workspace_bytes(desc, cache))
         return MCSD_ERR_WORKSPACE;
+    const AttentionPlan plan = attention_plan(desc, cache);
+    // (the cut counts units of all items in 32 bits)
+    if (static_cast<double>(desc->batch) * cache->n_heads * plan.blocks *
+            (static_cast<double>(desc->max_pages) * cache->page_size / kAttUnit + 2) > 4.2e9)
+        return MCSD_ERR_UNSUPPORTED;
     AttendParams p = {};
     p.c = cache_params(cache);
     p.q = q; p.out = out; p.lse = lse; p.table = page_table; p.prefix_len = prefix_len; p.ld_table = desc->ld_table;
@@ -358,7 +367,6 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     for (int n = 0; n < desc->n_nodes; ++n) p.parent[n] = static_cast<int16_t>(tree_parent[n]);
     p.group = desc->n_heads / cache->n_heads;
     p.n_rows = desc->n_nodes * p.group;
-    const AttentionPlan plan = attention_plan(desc, cache);
     p.n_blocks = plan.blocks;
     p.n_ctas = plan.ctas;
     p.part = static_cast<float *>(desc->workspace);

@@ -268,3 +268,38 @@ def test_many_sequences_and_an_empty_batch():
     _check(q, cache, table, prefix, parent, r.out, r.lse)
     e = _run(q[:0], cache, table[:0], prefix[:0], parent)
     assert e.out.shape[0] == 0
+
+
+@pytest.mark.parametrize("kconfig,heads,kv", [("", 32, 8), ("2", 32, 8), ("4x2x2x1", 32, 32), ("4x2x2x1", 64, 32), ("2x2x2x2", 64, 8), ("4x4x2x2x1", 16, 8)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_busy_batches(kconfig, heads, kv, D):
+    """Enough items that every SM works through several, of unequal lengths, with idle rows in the last block: against
+    products in 64 bits on the device, several times over."""
+    prefixes = [1400, 1, 700, 300, 129, 1023, 64, 900]
+    parent, q, cache, table, prefix = _problem(20, 8, kconfig, heads, kv, D, 16, prefixes, torch.bfloat16)
+    N, G = len(parent), heads // kv
+    att = binding.TreeAttention(8, parent, heads, q.dtype, cache, table.shape[1])
+    runs = []
+    for _ in range(4):
+        r = att.mcsd_tree_attention(q, cache, table, prefix)
+        runs.append((r.out.clone(), r.lse.clone()))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, runs[0][0]) and torch.equal(b, runs[0][1]) for a, b in runs)
+    seen = torch.tensor([[m in ref.path(parent, n) for m in range(N)] for n in range(N)], device="cuda")
+    for b, length in enumerate(prefixes):
+        pos = torch.arange(length + N, device="cuda")
+        slots = table[b, pos // 16].long() * 16 + pos % 16
+        k, v = (t.double().transpose(0, 1) for t in binding.mcsd_read_kv(cache, slots))            # [kv, keys, D]
+        x = q[b].double().view(N, kv, G, D).permute(1, 0, 2, 3).reshape(kv, N * G, D)
+        s = torch.matmul(x, k.transpose(1, 2)) * D ** -0.5
+        mask = torch.cat([torch.ones((N, length), dtype=torch.bool, device="cuda"), seen], 1).repeat_interleave(G, 0)
+        s = s.masked_fill(~mask, float("-inf"))
+        lse = torch.logsumexp(s, -1)
+        p = torch.exp(s - lse[..., None])
+        want = torch.matmul(p, v)
+        # weights rounded to half (2^-12) and scores that are sums of D products in float32, of numbers up to |q| (|mid| + 15 scale)
+        ds = D * 2.0 ** -24 * (D ** -0.5 * x.abs().sum(-1) * 3 * k.abs().amax()) + 2.0 ** -19
+        tol = 2.0 ** -8 * want.abs() + torch.matmul(p, v.abs() + v.abs().amax(-1, keepdim=True)) * (2.0 ** -12 + 2 * ds)[..., None]
+        back = lambda t: t.view(kv, N, G, -1).permute(1, 0, 2, 3).reshape(N, heads, -1)
+        assert ((runs[0][0][b].double() - back(want)).abs() <= back(tol)).all()
+        assert ((runs[0][1][b].double() - back(lse)[..., 0]).abs() <= back(ds + 2.0 ** -21 * lse.abs())[..., 0]).all()
