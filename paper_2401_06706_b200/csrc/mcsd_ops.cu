@@ -62,8 +62,11 @@ CacheParams cache_params(const mcsd_kv_cache *c)
 template <int DT>
 int launch_rules(const RulesParams &p, dim3 grid, size_t smem, bool vec, cudaStream_t st)
 {
-    if (vec) rules_kernel<DT, true><<<grid, kRulesThreads, smem, st>>>(p);
-    else rules_kernel<DT, false><<<grid, kRulesThreads, smem, st>>>(p);
+    void (*kernel)(const RulesParams) = vec ? rules_kernel<DT, true> : rules_kernel<DT, false>;
+    if (smem > 48 * 1024 &&                         // (trees some hundred levels deep)
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+        return MCSD_ERR_CUDA;
+    kernel<<<grid, kRulesThreads, smem, st>>>(p);
     return launched(1);
 }
 
@@ -71,7 +74,8 @@ int launch_rules(const RulesParams &p, dim3 grid, size_t smem, bool vec, cudaStr
 template <bool APPEND, int DT, int D>
 int launch_rows(const RowsParams &p, bool vec, cudaStream_t st)
 {
-    const long long want = (p.n_rows * (D / 8) + 255) / 256, cap = static_cast<long long>(sm_count()) * 8;
+    // a row per D / 8 threads while that fills the SMs, then up to kRowsAhead rows a thread before the grid's end
+    const long long want = (static_cast<long long>(p.n_rows) * (D / 8) + 255) / 256, cap = static_cast<long long>(sm_count()) * 8;
     if (cap <= 0) return MCSD_ERR_CUDA;
     const unsigned grid = static_cast<unsigned>(want < cap ? want : cap);
     if constexpr (APPEND) {
@@ -100,14 +104,14 @@ int rows_call(const mcsd_kv_cache *cache, const void *keys, int64_t key_token, i
     // rows must not overlap where they are written
     if (!APPEND && ((keys && cache->n_heads > 1 && key_head < row) || (values && cache->n_heads > 1 && value_head < row))) return MCSD_ERR_STRIDE;
     if (!APPEND && n_tokens > 1 && ((keys && key_token < row) || (values && value_token < row))) return MCSD_ERR_STRIDE;
-    if (n_tokens > (1LL << 40) / (2 * cache->n_heads)) return MCSD_ERR_UNSUPPORTED;
+    if (n_tokens > (1LL << 30) / cache->n_heads) return MCSD_ERR_UNSUPPORTED;    // (rows are counted in 32 bits)
     RowsParams p = {};
     p.c = cache_params(cache);
     p.keys = const_cast<void *>(keys);
     p.values = const_cast<void *>(values);
     p.key_token = key_token; p.key_head = key_head; p.value_token = value_token; p.value_head = value_head;
     p.slots = reinterpret_cast<const long long *>(slots);
-    p.n_rows = n_tokens * cache->n_heads * 2;
+    p.n_rows = static_cast<uint32_t>(n_tokens * cache->n_heads * 2);
     const unsigned long long es = static_cast<unsigned long long>(elem_size(dtype));
     const unsigned long long all = reinterpret_cast<uintptr_t>(keys) | reinterpret_cast<uintptr_t>(values) |
         es * static_cast<unsigned long long>(key_token | key_head | value_token | value_head);
@@ -250,16 +254,16 @@ int mcsd_apply_logit_rules(const mcsd_desc *desc, const mcsd_logit_rules *rules,
     const int sms = sm_count();
     if (sms <= 0) return MCSD_ERR_CUDA;
     // The widest slice (fewest scans of the history) that still gives every SM two CTAs, rows split
-    // where a narrow slice alone does not.
+    // where a narrow slice alone does not; a CTA has eight warps, a row each.
+    p.depth = depth;
     p.slice = kRulesMaxSlice;
     while (p.slice > 512 && static_cast<long long>((p.V + p.slice - 1) / p.slice) * desc->batch < 2LL * sms) p.slice >>= 1;
     const long long ctas = static_cast<long long>((p.V + p.slice - 1) / p.slice) * desc->batch;
     long long split = (4LL * sms + ctas - 1) / ctas;
-    if (split > n_rows) split = n_rows;
-    if (split < 1) split = 1;
+    if (split > (n_rows + 7) / 8) split = (n_rows + 7) / 8;
     p.rows_per_cta = static_cast<int32_t>((n_rows + split - 1) / split);
     const dim3 grid((p.V + p.slice - 1) / p.slice, desc->batch, (n_rows + p.rows_per_cta - 1) / p.rows_per_cta);
-    const size_t smem = 4 * (2 * static_cast<size_t>(p.slice) + p.slice / 32 + desc->n_nodes);
+    const size_t smem = 4 * (2 * static_cast<size_t>(p.slice) + p.slice / 2 + p.slice / 32 + desc->n_nodes + kRulesThreads / 32 * 2 * static_cast<size_t>(depth));
     const unsigned long long es = static_cast<unsigned long long>(elem_size(desc->dtype));
     const bool vec = (reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(out) |
                       es * static_cast<unsigned long long>(ld_in | ld_out)) % 16 == 0;

@@ -6,7 +6,7 @@
 namespace mcsd {
 
 constexpr int kRulesThreads = 256;
-constexpr int kRulesMaxSlice = 4096;                // tokens of one CTA
+constexpr int kRulesMaxSlice = 2048;                // tokens of one CTA: four CTAs per SM
 constexpr uint32_t kRulesPrompt = 0x80000000u;      // flag of a counter: the token occurs in the prompt
 
 struct RulesParams {
@@ -24,43 +24,36 @@ struct RulesParams {
     const int32_t *cand;
     int32_t *status;
     int32_t n_history, n_bias, n_nodes, rows_per_tree, V, slice, node_begin, node_end, rows_per_cta, in_place;
+    int32_t depth;                                  // of the tree: the longest path, the root excluded
     int16_t parent[MCSD_MAX_NODES];
 };
 
-// Adds `step` to the counters of the tokens on the way from node a up to (not including) node `stop`,
-// as far as they lie in this CTA's slice.
-__device__ __forceinline__ void rules_walk(const RulesParams &P, const int32_t *cand, uint32_t *count, uint32_t *touched,
-                                           int x0, int n_el, int a, int stop, uint32_t step)
-{
-    while (a > stop && a > 0) {
-        const uint32_t t = static_cast<uint32_t>(cand[a]) - static_cast<uint32_t>(x0);
-        if (t < static_cast<uint32_t>(n_el)) {
-            count[t] += step;
-            touched[t >> 5] |= 1u << (t & 31);
-        }
-        a = P.parent[a];
-    }
-}
-
 // One CTA per (slice of the vocabulary, sequence, run of rows).  It counts the history's tokens that fall
-// into its slice in shared memory, once, and then passes over its rows: a token's penalty needs nothing
-// but its own counter, so slices never talk to each other, and every CTA scanning the whole history (4
-// bytes a token from L2) costs less than a launch that would share the counts.  The tokens on the path
-// of a node are added to the same counters before its row and taken out after it: neighbouring rows
-// share most of their path, so only the difference of the two paths moves.
+// into its slice in shared memory, once: a token's penalty needs nothing but its own counter, so slices
+// never talk to each other, and every CTA scanning the whole history (4 bytes a token from L2) costs less
+// than a launch that would share the counts.  Then every warp takes rows of its own, without a barrier: it
+// streams its slice of the row (eight 16-byte loads in flight per lane) with nothing but the mask applied, then
+// takes the tokens some rule concerns one by one from a list, and last the few on the row's path, from their
+// logits read before.  (With the rules applied while streaming, nearly every warp had a lane with a token
+// that needs them, and all lanes went through them: 215 us against 72 us on 64 x 31 rows of 50272 halves.)
 template <int DT, bool VEC>
-__global__ void __launch_bounds__(kRulesThreads)
+__global__ void __launch_bounds__(kRulesThreads, 4)
 rules_kernel(const __grid_constant__ RulesParams P)
 {
     using T = Elem<DT>;
     constexpr int VE = 16 / T::kBytes;              // elements of a 16-byte vector
-    constexpr int NV = kRulesMaxSlice / (VE * kRulesThreads);
+    constexpr uint32_t kAll = (1u << VE) - 1u;
+    constexpr int kFlight = 8, kWarps = kRulesThreads / 32;
     extern __shared__ uint32_t s_rules[];
     uint32_t *s_count = s_rules;                                            // [slice] occurrences | kRulesPrompt
     float *s_bias = reinterpret_cast<float *>(s_count + P.slice);           // [slice]
     uint32_t *s_touched = reinterpret_cast<uint32_t *>(s_bias + P.slice);   // [slice / 32] tokens a rule concerns
-    int32_t *s_cand = reinterpret_cast<int32_t *>(s_touched + P.slice / 32);// [n_nodes]
-    const int tid = threadIdx.x, b = blockIdx.y;
+    uint16_t *s_list = reinterpret_cast<uint16_t *>(s_touched + P.slice / 32); // [slice] these tokens in ascending order
+    int32_t *s_cand = reinterpret_cast<int32_t *>(s_list + P.slice);        // [n_nodes]
+    __shared__ int s_listed;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, b = blockIdx.y;
+    int32_t *s_token = s_cand + P.n_nodes + warp * 2 * P.depth;             // [depth] tokens on the path of this warp's row
+    float *s_value = reinterpret_cast<float *>(s_token + P.depth);          // [depth] their logits
     const int x0 = blockIdx.x * P.slice;
     const int n_el = min(P.slice, P.V - x0);
     const bool penalise = P.repetition || P.frequency || P.presence;
@@ -74,8 +67,9 @@ rules_kernel(const __grid_constant__ RulesParams P)
         const int32_t *row = P.history + b * P.ld_history;
         const int len = min(max(P.history_len[b], 0), P.n_history);
         const int prompt = P.prompt_len ? P.prompt_len[b] : 0;
+#pragma unroll 4
         for (int i = tid; i < len; i += kRulesThreads) {
-            const uint32_t t = static_cast<uint32_t>(row[i]) - static_cast<uint32_t>(x0);
+            const uint32_t t = static_cast<uint32_t>(__ldg(row + i)) - static_cast<uint32_t>(x0);
             if (t < static_cast<uint32_t>(n_el)) {    // (false for negative tokens as well)
                 if (i < prompt) atomicOr(&s_count[t], kRulesPrompt);
                 else atomicAdd(&s_count[t], 1u);
@@ -92,96 +86,153 @@ rules_kernel(const __grid_constant__ RulesParams P)
         const float v = at ? P.bias_values[static_cast<long long>(b) * P.n_bias + at - 1] : 0.f;
         s_bias[i] = v;
         const uint32_t any = __ballot_sync(0xffffffffu, v != 0.f || s_count[i] != 0u);
-        if ((tid & 31) == 0) s_touched[i >> 5] = any;
+        if (lane == 0) s_touched[i >> 5] = any;
     }
     const float theta = P.repetition ? P.repetition[b] : 1.f;
     const float freq = P.frequency ? P.frequency[b] : 0.f;
     const float pres = P.presence ? P.presence[b] : 0.f;
+    __syncthreads();
+    if (warp == 0) {
+        const int per = P.slice / 1024;              // words of the bitmap per lane (slice: at least 512, half of the lanes then)
+        int n = 0;
+        for (int w = lane * max(per, 1); w < (lane + 1) * max(per, 1) && w < P.slice / 32; ++w) n += __popc(s_touched[w]);
+        int at = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, at, o);
+            if (lane >= o) at += t;
+        }
+        if (lane == 31) s_listed = at;
+        at -= n;
+        for (int w = lane * max(per, 1); w < (lane + 1) * max(per, 1) && w < P.slice / 32; ++w)
+            for (uint32_t bits = s_touched[w]; bits; bits &= bits - 1u) s_list[at++] = static_cast<uint16_t>(32 * w + __ffs(bits) - 1);
+    }
+    __syncthreads();
+    const int listed = s_listed;
 
-    auto apply = [&](float l, int i) {
-        const uint32_t c = s_count[i], n = c & ~kRulesPrompt;
+    // the rules but the mask; c: occurrences | kRulesPrompt
+    auto apply = [&](float l, uint32_t c, float v) {
+        const uint32_t n = c & ~kRulesPrompt;
         if (c) l = l > 0.f ? l / theta : l * theta;
         if (n) l = l - freq * static_cast<float>(n) - pres;
-        const float v = s_bias[i];
         return v != 0.f ? l + v : l;
     };
 
-    int before = 0;                                  // node whose path is in the counters
     const int n0 = P.node_begin + blockIdx.z * P.rows_per_cta;
     const int n1 = min(n0 + P.rows_per_cta, P.node_end);
-    for (int n = n0; n < n1; ++n) {
-        __syncthreads();                             // the row before is done with the counters
-        if (tid == 0 && penalise && P.cand) {
-            int a = before, c = n;                   // their lowest common ancestor
-            while (a != c) {
-                if (a > c) a = P.parent[a]; else c = P.parent[c];
-            }
-            rules_walk(P, s_cand, s_count, s_touched, x0, n_el, before, a, 0xffffffffu);
-            rules_walk(P, s_cand, s_count, s_touched, x0, n_el, n, a, 1u);
-        }
-        before = n;
+    auto mask_row = [&](int n) {                     // -1: none
+        if (!P.masks || n >= n1) return -1LL;
+        const long long item = static_cast<long long>(b) * P.n_nodes + n;
+        return P.mask_index ? static_cast<long long>(__ldg(P.mask_index + item)) : item;
+    };
+    long long m_next = mask_row(n0 + warp);
+    for (int n = n0 + warp; n < n1; n += kWarps) {
         const long long r = static_cast<long long>(b) * P.rows_per_tree + n;
-        const uint32_t *mask = nullptr;
-        if (P.masks) {
-            const long long item = static_cast<long long>(b) * P.n_nodes + n;
-            const long long m = P.mask_index ? P.mask_index[item] : item;
-            if (m >= 0 && m < P.n_masks) mask = P.masks + m * P.ld_mask + (x0 >> 5);
-            else if (m >= 0 && P.status && blockIdx.x == 0 && tid == 0) atomicOr(&P.status[b], MCSD_STATUS_BAD_MASK);
-        }
-        __syncthreads();
         const char *src = static_cast<const char *>(P.logits) + (r * P.ld_in + x0) * T::kBytes;
         char *dst = static_cast<char *>(P.out) + (r * P.ld_out + x0) * T::kBytes;
-        if constexpr (VEC) {
-            uint4 v[NV];
-            uint32_t keep[NV], hit[NV];
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int i = (tid + k * kRulesThreads) * VE;
-                keep[k] = (1u << VE) - 1u;
-                hit[k] = 0u;
-                if (i + VE <= n_el) {
-                    if (mask) keep[k] &= __ldg(mask + (i >> 5)) >> (i & 31);
-                    hit[k] = (s_touched[i >> 5] >> (i & 31)) & ((1u << VE) - 1u);
+        const uint32_t *mask = nullptr;
+        const long long m = m_next;
+        m_next = mask_row(n + kWarps);               // (in flight while this row is worked on)
+        if (m >= 0 && m < P.n_masks) mask = P.masks + m * P.ld_mask + (x0 >> 5);
+        else if (m >= 0 && P.status && blockIdx.x == 0 && lane == 0) atomicOr(&P.status[b], MCSD_STATUS_BAD_MASK);
+        auto allowed = [&](int i) { return !mask || ((__ldg(mask + (i >> 5)) >> (i & 31)) & 1u); };
+        // the path: lane i the i-th ancestor, root excluded
+        int length = 0;
+        if (penalise && P.cand) {
+            for (int i0 = 0; i0 < P.depth; i0 += 32) {
+                int a = n;
+                for (int i = 0; i < i0 + lane && a > 0; ++i) a = P.parent[a];
+                if (a > 0 && i0 + lane < P.depth) {
+                    const uint32_t t = static_cast<uint32_t>(s_cand[a]) - static_cast<uint32_t>(x0);
+                    const bool here = t < static_cast<uint32_t>(n_el);
+                    s_token[i0 + lane] = here ? static_cast<int32_t>(t) : -1;
+                    if (here) s_value[i0 + lane] = load_elem<DT>(src, t);
                 }
-            }
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int i = (tid + k * kRulesThreads) * VE;
-                // in place a vector that no rule concerns is not read, nor one that is masked as a whole
-                const bool rd = i + VE <= n_el && keep[k] != 0u && (!P.in_place || hit[k] || keep[k] != (1u << VE) - 1u);
-                v[k] = ld_plain_v4_if(src + static_cast<long long>(i) * T::kBytes, rd);
-            }
-#pragma unroll
-            for (int k = 0; k < NV; ++k) {
-                const int i = (tid + k * kRulesThreads) * VE;
-                if (i + VE > n_el) continue;
-                if (P.in_place && !hit[k] && keep[k] == (1u << VE) - 1u) continue;
-                if (hit[k] || keep[k] != (1u << VE) - 1u) {
-                    float f[VE];
-                    T::unpack(v[k], f);
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) {
-                        if ((hit[k] >> e) & 1u) f[e] = apply(f[e], i + e);
-                        if (!((keep[k] >> e) & 1u)) f[e] = -INFINITY;
-                    }
-                    v[k] = pack_elems<DT>(f);
-                }
-                *reinterpret_cast<uint4 *>(dst + static_cast<long long>(i) * T::kBytes) = v[k];
-            }
-            const int tail = n_el & ~(VE - 1);       // the last tokens of the vocabulary, one by one
-            if (tid < n_el - tail) {
-                const int i = tail + tid;
-                float l = apply(load_elem<DT>(src, i), i);
-                if (mask && !((mask[i >> 5] >> (i & 31)) & 1u)) l = -INFINITY;
-                store_elem<DT>(dst, i, l);
-            }
-        } else {
-            for (int i = tid; i < n_el; i += kRulesThreads) {
-                float l = apply(load_elem<DT>(src, i), i);
-                if (mask && !((mask[i >> 5] >> (i & 31)) & 1u)) l = -INFINITY;
-                store_elem<DT>(dst, i, l);
+                length += __popc(__ballot_sync(0xffffffffu, a > 0 && i0 + lane < P.depth));
             }
         }
+        // the first of the listed tokens' logits are asked for now, so that they arrive with the row's
+        constexpr int kAhead = 2;
+        float ahead[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) ahead[k] = lane + 32 * k < listed ? load_elem<DT>(src, s_list[lane + 32 * k]) : 0.f;
+        __syncwarp();                                // read before any lane writes the row in place
+        // the mask alone; in place only what it takes out is written
+        if constexpr (VEC) {
+            const int n_vec = n_el / VE;
+            // the slice's words of the mask, word lane + 32 j with this lane
+            constexpr int kWords = kRulesMaxSlice / 1024;
+            uint32_t words[kWords];
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) words[j] = mask && 32 * (lane + 32 * j) < n_el ? __ldg(mask + lane + 32 * j) : 0xffffffffu;
+            if (!P.in_place || mask)
+#pragma unroll
+                for (int pass = 0; pass < kRulesMaxSlice / (32 * kFlight * VE); ++pass) {
+                    const int v0 = lane + pass * 32 * kFlight;
+                    if (pass * 32 * kFlight >= n_vec) break;
+                    uint4 v[kFlight];
+                    uint32_t keep[kFlight];
+#pragma unroll
+                    for (int k = 0; k < kFlight; ++k) {
+                        const int i = (v0 + 32 * k) * VE;
+                        const bool in = v0 + 32 * k < n_vec;
+                        if (!P.in_place) v[k] = ld_plain_v4_if(src + static_cast<long long>(i) * T::kBytes, in);
+                        // (word i / 32: 32 / VE lanes share one, a vector further on lies VE words on)
+                        const int word = pass * kFlight * VE + k * VE + lane / (32 / VE);
+                        const uint32_t bits = __shfl_sync(0xffffffffu, words[(pass * kFlight + k) * VE / 32], word & 31) >> (i & 31);
+                        keep[k] = in ? bits & kAll : kAll;
+                    }
+                    if (P.in_place) {
+#pragma unroll
+                        for (int k = 0; k < kFlight; ++k)
+                            v[k] = ld_plain_v4_if(src + static_cast<long long>(v0 + 32 * k) * 16, keep[k] != 0u && keep[k] != kAll);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kFlight; ++k) {
+                        if (v0 + 32 * k >= n_vec || (P.in_place && keep[k] == kAll)) continue;
+                        uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            uint32_t m;
+                            if constexpr (VE == 4) m = 0u - ((keep[k] >> j) & 1u);
+                            else m = ((keep[k] >> (2 * j)) & 1u) * 0xffffu | ((keep[k] >> (2 * j + 1)) & 1u) * 0xffff0000u;
+                            w[j] = (w[j] & m) | (T::kNegInfWord & ~m);
+                        }
+                        reinterpret_cast<uint4 *>(dst)[v0 + 32 * k] = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            const int i = n_vec * VE + lane;         // the last tokens of the vocabulary, one by one
+            if (i < n_el) store_elem<DT>(dst, i, allowed(i) ? load_elem<DT>(src, i) : -INFINITY);
+        } else {
+            for (int i = lane; i < n_el; i += 32) store_elem<DT>(dst, i, allowed(i) ? load_elem<DT>(src, i) : -INFINITY);
+        }
+        __syncwarp();
+        // the tokens some rule concerns
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (lane + 32 * k < listed) {
+                const int i = s_list[lane + 32 * k];
+                if (allowed(i)) store_elem<DT>(dst, i, apply(ahead[k], s_count[i], s_bias[i]));
+            }
+        for (int k = lane + 32 * kAhead; k < listed; k += 32) {
+            const int i = s_list[k];
+            if (allowed(i)) store_elem<DT>(dst, i, apply(load_elem<DT>(src, i), s_count[i], s_bias[i]));
+        }
+        __syncwarp();
+        // the tokens of the path: the first of equal ones writes, with all of them counted
+        for (int i = lane; i < length; i += 32) {
+            const int t = s_token[i];
+            if (t < 0 || !allowed(t)) continue;
+            uint32_t more = 0;
+            bool head = true;
+            for (int j = 0; j < length; ++j)
+                if (s_token[j] == t) {
+                    ++more;
+                    head = head && j >= i;
+                }
+            if (head) store_elem<DT>(dst, t, apply(s_value[i], s_count[t] + more, s_bias[t]));
+        }
+        __syncwarp();
     }
 }
 
