@@ -21,7 +21,7 @@ struct RowsParams {
     void *keys, *values;                            // (read only in append_kernel); a null one is skipped
     long long key_token, key_head, value_token, value_head;  // strides in elements
     const long long *slots;
-    uint32_t n_rows;                                // tokens * heads * 2
+    long long n_tokens;
 };
 
 // Where row `which` (0 key, 1 value) of (token slot, head) lies; false if the slot is not in the cache.
@@ -38,27 +38,70 @@ __device__ __forceinline__ bool kv_row(const CacheParams &c, long long slot, int
     return true;
 }
 
-// Row r of a call: its token, whether it is a value row, and its head; rows of a token's heads follow each other.
-struct RowIndex { uint32_t token; int which, head; };
-__device__ __forceinline__ RowIndex row_index(const RowsParams &P, uint32_t r)
+// A group of D / 8 threads keeps one row of every token (a key or a value row of one head) and steps over
+// the tokens: with 2 n_heads groups per token, group i of the grid has row i % (2 n_heads) of tokens
+// i / (2 n_heads), that + `step`, ...; groups beyond the last full token of the grid have nothing to do.
+struct RowWalk { long long token, step; int which, head; };
+template <int TPR>
+__device__ __forceinline__ RowWalk row_walk(const RowsParams &P)
 {
-    RowIndex x;
-    const uint32_t rest = r / static_cast<uint32_t>(P.c.n_heads);
-    x.head = static_cast<int>(r - rest * static_cast<uint32_t>(P.c.n_heads));
-    x.which = static_cast<int>(rest & 1u);
-    x.token = rest >> 1;
-    return x;
+    const uint32_t rows = 2u * static_cast<uint32_t>(P.c.n_heads);
+    const uint32_t groups = gridDim.x * (256u / TPR), mine = (blockIdx.x * 256u + threadIdx.x) / TPR;
+    RowWalk w;
+    w.step = groups / rows;
+    w.token = mine / rows;
+    const uint32_t row = mine - static_cast<uint32_t>(w.token) * rows;
+    w.which = row >= static_cast<uint32_t>(P.c.n_heads);
+    w.head = static_cast<int>(row) - (w.which ? P.c.n_heads : 0);
+    if (w.token >= w.step) w.token = P.n_tokens;
+    return w;
 }
 
 // D / 8 threads per row, 8 numbers each: the row's extremes by shuffles, then every thread rounds its own
 // 8 and stores one word of codes.  Rows of a token's heads follow each other in the thread order, so that
 // loads are contiguous (a page's rows of one head are 32 to 64 contiguous bytes each).  Bound by HBM: 2 D
-// numbers read and D + 8 bytes written per key/value row pair; a thread takes kRowsAhead rows at a time, so
+// numbers read and D + 8 bytes written per key/value row pair; a thread takes kRowsAhead tokens at a time, so
 // that their slots, and then their numbers, are in flight together.
 // Scale, mid and codes are those of the definition in exact arithmetic: the two per-row numbers are formed
-// in double (once a row), and a code whose float32 quotient lies within 2^-10 of a border between two codes
-// (float32 is off by a few 2^-20 at most) is decided in double; so no code depends on how the compiler orders things.
+// in double (by one of a row's threads), and where a float32 quotient lies within 2^-18 of a border between two codes
+// (two float32 roundings and a reciprocal good to 2^-23 put a number up to 8.5 off by 2^-18.9 at most) the thread's codes are decided in double; so no code depends on
+// how the compiler orders things.  Rounding to an integer is an addition of 1.5 2^23 (the conversion
+// instructions have a quarter of the rate).
 constexpr int kRowsAhead = 4;
+
+// Extremes of a thread's 8 numbers, NaN if one is NaN.
+__device__ __forceinline__ float min_nan(float a, float b) { float d; asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
+__device__ __forceinline__ float max_nan(float a, float b) { float d; asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
+template <int DT> struct Pair;                      // two 16-bit numbers in a word
+template <> struct Pair<MCSD_DTYPE_F16> {
+    typedef __half2 T;
+    static __device__ __forceinline__ T lo(T a, T b) { return __hmin2_nan(a, b); }
+    static __device__ __forceinline__ T hi(T a, T b) { return __hmax2_nan(a, b); }
+    static __device__ __forceinline__ float2 wide(T a) { return __half22float2(a); }
+    static __device__ __forceinline__ T low_and_minus_high(T l, T h) { return __halves2half2(__hmin_nan(__low2half(l), __high2half(l)), __hneg(__hmax_nan(__low2half(h), __high2half(h)))); }
+};
+template <> struct Pair<MCSD_DTYPE_BF16> {
+    typedef __nv_bfloat162 T;
+    static __device__ __forceinline__ T lo(T a, T b) { return __hmin2_nan(a, b); }
+    static __device__ __forceinline__ T hi(T a, T b) { return __hmax2_nan(a, b); }
+    static __device__ __forceinline__ float2 wide(T a) { return __bfloat1622float2(a); }
+    static __device__ __forceinline__ T low_and_minus_high(T l, T h) { return __halves2bfloat162(__hmin_nan(__low2bfloat16(l), __high2bfloat16(l)), __hneg(__hmax_nan(__low2bfloat16(h), __high2bfloat16(h)))); }
+};
+
+// (scale, mid) of a row from its extremes; (0, NaN) if one of them is not finite.
+__device__ __forceinline__ uint32_t row_param(float lo, float hi)
+{
+    if (!(fabsf(lo) <= 3.4028235e38f && fabsf(hi) <= 3.4028235e38f)) return 0x7fff0000u;
+    // range / 15, correctly rounded: the quotient by the rounded reciprocal, corrected by its exact remainder (Markstein)
+    constexpr double kFifteenth = 1.0 / 15.0;
+    const double range = static_cast<double>(hi) - static_cast<double>(lo);
+    const double near = range * kFifteenth;
+    const double step = fma(fma(-15.0, near, range), kFifteenth, near);
+    const __half scale = __float2half_rn(static_cast<float>(fmin(step, 65504.0)));
+    const double mid = fma(8.0, static_cast<double>(__half2float(scale)), static_cast<double>(lo));
+    const __half2 p = __halves2half2(scale, __float2half_rn(static_cast<float>(fmax(-65504.0, fmin(mid, 65504.0)))));
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
 
 template <int DT, int D, bool VEC>
 __global__ void __launch_bounds__(256)
@@ -66,79 +109,107 @@ append_kernel(const RowsParams P)
 {
     constexpr int TPR = D / 8;                      // threads of a row
     constexpr int kLoads = Elem<DT>::kBytes / 2;
-    const uint32_t stride = gridDim.x * (256 / TPR);
     const int lane = threadIdx.x % TPR;
     const uint32_t group = ((1u << TPR) - 1u) << (threadIdx.x & 31 & ~(TPR - 1));
-    for (uint32_t r0 = (blockIdx.x * 256 + threadIdx.x) / TPR; r0 < P.n_rows;) {
+    const RowWalk walk = row_walk<TPR>(P);
+    const char *src = static_cast<const char *>(walk.which ? P.values : P.keys) +
+                      (walk.head * (walk.which ? P.value_head : P.key_head) + lane * 8) * Elem<DT>::kBytes;
+    const long long pitch = (walk.which ? P.value_token : P.key_token) * Elem<DT>::kBytes;
+    for (long long token = walk.token; token < P.n_tokens; token += kRowsAhead * walk.step) {
         unsigned char *codes[kRowsAhead];
         __half2 *param[kRowsAhead];
-        uint4 raw[kRowsAhead][VEC ? kLoads : 1];
-        long long at[kRowsAhead];
-        const void *src[kRowsAhead];
+        uint4 raw[kRowsAhead][kLoads];              // the numbers, in their type
 #pragma unroll
         for (int u = 0; u < kRowsAhead; ++u) {
-            const uint32_t r = r0 + u * stride;     // (far below 2^32: the host bounds the rows)
+            const long long tok = token + u * walk.step;
             codes[u] = nullptr;
-            if (r >= P.n_rows) continue;
-            const RowIndex x = row_index(P, r);
-            if (!kv_row<D>(P.c, __ldg(P.slots + x.token), x.head, x.which, codes[u], param[u])) codes[u] = nullptr;
-            src[u] = x.which ? P.values : P.keys;
-            at[u] = (x.which ? x.token * P.value_token + x.head * P.value_head : x.token * P.key_token + x.head * P.key_head) + lane * 8;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) raw[u][i] = make_uint4(0u, 0u, 0u, 0u);
+            if (tok >= P.n_tokens) continue;
+            if (!kv_row<D>(P.c, __ldg(P.slots + tok), walk.head, walk.which, codes[u], param[u])) codes[u] = nullptr;
             if constexpr (VEC) {
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i) raw[u][i] = ld_stream_v4(static_cast<const char *>(src[u]) + at[u] * Elem<DT>::kBytes + 16 * i);
+                for (int i = 0; i < kLoads; ++i) raw[u][i] = ld_stream_v4(src + tok * pitch + 16 * i);
+            } else {
+                float x8[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x8[i] = load_elem<DT>(src + tok * pitch, i);
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) raw[u][i] = pack_elems<DT>(x8 + i * (8 / kLoads));   // (exact: they come from that type)
             }
         }
+        // extremes of the rows; then thread u of a row's forms the two numbers of row u
+        float my_lo = 0.f, my_hi = 0.f;
 #pragma unroll
         for (int u = 0; u < kRowsAhead; ++u) {
-            if (!codes[u]) continue;                // (the same for all threads of the row)
-            float x[8];
-            if constexpr (VEC) {
+            float lo, hi;
+            if constexpr (DT == MCSD_DTYPE_F32) {
+                float x[8];
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) Elem<DT>::unpack(raw[u][i], x + i * (8 / kLoads));
+                lo = hi = x[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) { lo = min_nan(lo, x[i]); hi = max_nan(hi, x[i]); }
+#pragma unroll
+                for (int o = TPR / 2; o > 0; o >>= 1) {
+                    lo = min_nan(lo, __shfl_xor_sync(group, lo, o));
+                    hi = max_nan(hi, __shfl_xor_sync(group, hi, o));
+                }
             } else {
+                typedef typename Pair<DT>::T T;
+                const T *w = reinterpret_cast<const T *>(&raw[u][0]);
+                T both = Pair<DT>::low_and_minus_high(Pair<DT>::lo(Pair<DT>::lo(w[0], w[1]), Pair<DT>::lo(w[2], w[3])),
+                                                      Pair<DT>::hi(Pair<DT>::hi(w[0], w[1]), Pair<DT>::hi(w[2], w[3])));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = load_elem<DT>(src[u], at[u] + i);
+                for (int o = TPR / 2; o > 0; o >>= 1) {
+                    const uint32_t other = __shfl_xor_sync(group, *reinterpret_cast<const uint32_t *>(&both), o);
+                    both = Pair<DT>::lo(both, *reinterpret_cast<const T *>(&other));
+                }
+                const float2 f = Pair<DT>::wide(both);
+                lo = f.x;
+                hi = -f.y;
             }
-            float lo = x[0], hi = x[0], odd = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                lo = fminf(lo, x[i]);
-                hi = fmaxf(hi, x[i]);
-                odd += x[i] * 0.f;                  // NaN if any number is infinite or NaN
-            }
-#pragma unroll
-            for (int o = TPR / 2; o > 0; o >>= 1) {
-                lo = fminf(lo, __shfl_xor_sync(group, lo, o));
-                hi = fmaxf(hi, __shfl_xor_sync(group, hi, o));
-            }
-            const bool bad = (__ballot_sync(group, !(odd == 0.f)) & group) != 0u;
-            // range / 15, correctly rounded: the quotient by the rounded reciprocal, corrected by its exact remainder (Markstein)
-            constexpr double kFifteenth = 1.0 / 15.0;
-            const double range = static_cast<double>(hi) - static_cast<double>(lo);
-            const double near = range * kFifteenth;
-            const double step = fma(fma(-15.0, near, range), kFifteenth, near);
-            const __half scale = __float2half_rn(static_cast<float>(fmin(step, 65504.0)));
-            const float s = __half2float(scale);
-            const __half mid = __float2half_rn(static_cast<float>(fmax(-65504.0, fmin(fma(8.0, static_cast<double>(s), static_cast<double>(lo)), 65504.0))));
-            const float m = __half2float(mid);
-            const float inv = s > 0.f ? 1.f / s : 0.f;
-            uint32_t word = 0u;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float q = (x[i] - m) * inv;
-                float n = rintf(q);
-                // near a border (or where the difference itself may have rounded) the quotient is formed in double
-                if (fabsf(fabsf(q - n) - 0.5f) < 0.0009765625f)
-                    n = static_cast<float>(rint((static_cast<double>(x[i]) - static_cast<double>(m)) / static_cast<double>(s)));
-                n = fminf(fmaxf(n, -8.f), 7.f);
-                word |= static_cast<uint32_t>(static_cast<int>(n) + 8) << (4 * i);
-            }
-            reinterpret_cast<uint32_t *>(codes[u])[lane] = !bad && s > 0.f ? word : 0x88888888u;
-            if (lane == 0) *param[u] = bad ? __halves2half2(__ushort_as_half(0), __ushort_as_half(0x7fff)) : __halves2half2(scale, mid);
+            if (lane == u) { my_lo = lo; my_hi = hi; }
         }
-        if (P.n_rows - r0 <= kRowsAhead * stride) break;
-        r0 += kRowsAhead * stride;
+        const uint32_t mine = row_param(my_lo, my_hi);
+#pragma unroll
+        for (int u = 0; u < kRowsAhead; ++u) {
+            const uint32_t both = __shfl_sync(group, mine, u, TPR);
+            if (!codes[u]) continue;                // (the same for all threads of the row)
+            const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&both));
+            const float s = p.x, m = p.y;
+            float inv;
+            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));      // (unused where s is 0)
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) Elem<DT>::unpack(raw[u][i], x + i * (8 / kLoads));
+            constexpr float kRound = 12582912.f + 8.f;              // 1.5 2^23, and code 8 at 0
+            uint32_t word = 0u;
+            float far = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                float2 q = __fmul2_rn(add2(make_float2(x[i], x[i + 1]), make_float2(-m, -m)), make_float2(inv, inv));
+                q.x = fminf(fmaxf(q.x, -8.f), 7.f);
+                q.y = fminf(fmaxf(q.y, -8.f), 7.f);
+                const float2 t = add2(q, make_float2(kRound, kRound));
+                const float2 d = add2(q, make_float2(kRound - t.x, kRound - t.y));     // off the code (the difference is exact)
+                far = max3(far, fabsf(d.x), fabsf(d.y));
+                word |= (__float_as_uint(t.x) & 15u) << (4 * i) | (__float_as_uint(t.y) & 15u) << (4 * i + 4);
+            }
+            if (far > 0.5f - 3.814697265625e-6f) {
+                word = 0u;
+#pragma unroll 1
+                for (int i = 0; i < 8; ++i) {
+                    const double q = (static_cast<double>(x[0]) - static_cast<double>(m)) / static_cast<double>(s);
+                    const double n = fmin(fmax(rint(q), -8.0), 7.0);
+                    word = word >> 4 | static_cast<uint32_t>(static_cast<int>(n) + 8) << 28;
+#pragma unroll
+                    for (int j = 0; j < 7; ++j) x[j] = x[j + 1];
+                }
+            }
+            reinterpret_cast<uint32_t *>(codes[u])[lane] = s > 0.f ? word : 0x88888888u;
+            if (lane == 0) *reinterpret_cast<uint32_t *>(param[u]) = both;
+        }
     }
 }
 
@@ -148,24 +219,25 @@ __global__ void __launch_bounds__(256)
 read_kernel(const RowsParams P)
 {
     constexpr int TPR = D / 8;
-    const uint32_t stride = gridDim.x * (256 / TPR);
     const int lane = threadIdx.x % TPR;
-    for (uint32_t r0 = (blockIdx.x * 256 + threadIdx.x) / TPR; r0 < P.n_rows;) {
-        void *dst[kRowsAhead];
-        long long at[kRowsAhead];
+    const RowWalk walk = row_walk<TPR>(P);
+    char *out = static_cast<char *>(walk.which ? P.values : P.keys);
+    if (!out) return;
+    out += (walk.head * (walk.which ? P.value_head : P.key_head) + lane * 8) * Elem<DT>::kBytes;
+    const long long pitch = (walk.which ? P.value_token : P.key_token) * Elem<DT>::kBytes;
+    for (long long token = walk.token; token < P.n_tokens; token += kRowsAhead * walk.step) {
+        char *dst[kRowsAhead];
         __half2 p[kRowsAhead];
         uint32_t word[kRowsAhead];
 #pragma unroll
         for (int u = 0; u < kRowsAhead; ++u) {
-            const uint32_t r = r0 + u * stride;
+            const long long tok = token + u * walk.step;
             dst[u] = nullptr;
-            if (r >= P.n_rows) continue;
-            const RowIndex x = row_index(P, r);
-            dst[u] = x.which ? P.values : P.keys;
+            if (tok >= P.n_tokens) continue;
             unsigned char *codes;
             __half2 *param;
-            if (!dst[u] || !kv_row<D>(P.c, __ldg(P.slots + x.token), x.head, x.which, codes, param)) { dst[u] = nullptr; continue; }
-            at[u] = (x.which ? x.token * P.value_token + x.head * P.value_head : x.token * P.key_token + x.head * P.key_head) + lane * 8;
+            if (!kv_row<D>(P.c, __ldg(P.slots + tok), walk.head, walk.which, codes, param)) continue;
+            dst[u] = out + tok * pitch;
             p[u] = *param;
             word[u] = reinterpret_cast<const uint32_t *>(codes)[lane];
         }
@@ -175,19 +247,23 @@ read_kernel(const RowsParams P)
             const float2 f = __half22float2(p[u]);
             float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = fmaf(f.x, static_cast<float>((word[u] >> (4 * i)) & 15u) - 8.f, f.y);
+            for (int i = 0; i < 8; i += 2) {        // (a code in the mantissa of 2^23: no conversion)
+                const float2 c = add2(make_float2(__uint_as_float((word[u] >> (4 * i)) & 15u | 0x4b000000u),
+                                                  __uint_as_float((word[u] >> (4 * i + 4)) & 15u | 0x4b000000u)), make_float2(-8388616.f, -8388616.f));
+                const float2 y = fma2(make_float2(f.x, f.x), c, make_float2(f.y, f.y));
+                x[i] = y.x;
+                x[i + 1] = y.y;
+            }
             if constexpr (VEC) {
                 constexpr int kStores = Elem<DT>::kBytes / 2;
-                uint4 *q = reinterpret_cast<uint4 *>(static_cast<char *>(dst[u]) + at[u] * Elem<DT>::kBytes);
+                uint4 *q = reinterpret_cast<uint4 *>(dst[u]);
 #pragma unroll
                 for (int i = 0; i < kStores; ++i) q[i] = pack_elems<DT>(x + i * (8 / kStores));
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) store_elem<DT>(dst[u], at[u] + i, x[i]);
+                for (int i = 0; i < 8; ++i) store_elem<DT>(dst[u], i, x[i]);
             }
         }
-        if (P.n_rows - r0 <= kRowsAhead * stride) break;
-        r0 += kRowsAhead * stride;
     }
 }
 

@@ -74,9 +74,12 @@ int launch_rules(const RulesParams &p, dim3 grid, size_t smem, bool vec, cudaStr
 template <bool APPEND, int DT, int D>
 int launch_rows(const RowsParams &p, bool vec, cudaStream_t st)
 {
-    // a row per D / 8 threads while that fills the SMs, then up to kRowsAhead rows a thread before the grid's end
-    const long long want = (static_cast<long long>(p.n_rows) * (D / 8) + 255) / 256, cap = static_cast<long long>(sm_count()) * 8;
-    if (cap <= 0) return MCSD_ERR_CUDA;
+    // A group of D / 8 threads per row (2 n_heads groups a token) while that fills the SMs, then several tokens a
+    // group; a token at least.
+    const long long groups = 256 / (D / 8), rows = 2LL * p.c.n_heads, resident = static_cast<long long>(sm_count()) * 8;
+    if (resident <= 0) return MCSD_ERR_CUDA;
+    const long long want = (p.n_tokens * rows + groups - 1) / groups, least = (rows + groups - 1) / groups;
+    const long long cap = resident > least ? resident : least;
     const unsigned grid = static_cast<unsigned>(want < cap ? want : cap);
     if constexpr (APPEND) {
         if (vec) append_kernel<DT, D, true><<<grid, 256, 0, st>>>(p);
@@ -104,14 +107,14 @@ int rows_call(const mcsd_kv_cache *cache, const void *keys, int64_t key_token, i
     // rows must not overlap where they are written
     if (!APPEND && ((keys && cache->n_heads > 1 && key_head < row) || (values && cache->n_heads > 1 && value_head < row))) return MCSD_ERR_STRIDE;
     if (!APPEND && n_tokens > 1 && ((keys && key_token < row) || (values && value_token < row))) return MCSD_ERR_STRIDE;
-    if (n_tokens > (1LL << 30) / cache->n_heads) return MCSD_ERR_UNSUPPORTED;    // (rows are counted in 32 bits)
+    if (n_tokens > (1LL << 40) / cache->n_heads) return MCSD_ERR_UNSUPPORTED;
     RowsParams p = {};
     p.c = cache_params(cache);
     p.keys = const_cast<void *>(keys);
     p.values = const_cast<void *>(values);
     p.key_token = key_token; p.key_head = key_head; p.value_token = value_token; p.value_head = value_head;
     p.slots = reinterpret_cast<const long long *>(slots);
-    p.n_rows = static_cast<uint32_t>(n_tokens * cache->n_heads * 2);
+    p.n_tokens = n_tokens;
     const unsigned long long es = static_cast<unsigned long long>(elem_size(dtype));
     const unsigned long long all = reinterpret_cast<uintptr_t>(keys) | reinterpret_cast<uintptr_t>(values) |
         es * static_cast<unsigned long long>(key_token | key_head | value_token | value_head);
