@@ -480,17 +480,20 @@ def mcsd_verify_host(target, draft, parent, cand, unif, temperature: float, mode
 
 # ---------------------------------------------------------------- the steps around the verification
 class _on_device:
-    """Makes the device of a tensor current for a call (the library works on the current device)."""
+    """Makes the device of a tensor current for a call (the library works on the current device); gives the raw
+    handle of the device's current stream."""
+
+    __slots__ = ("index", "guard")
 
     def __init__(self, device: torch.device):
-        index = device.index if device.index is not None else torch.cuda.current_device()
-        self.guard = torch.cuda.device(index) if index != torch.cuda.current_device() else None
-        self.stream = None
+        self.index, self.guard = device.index, None
 
     def __enter__(self):
-        if self.guard is not None:
+        current = torch._C._cuda_getDevice()
+        if self.index is not None and self.index != current:
+            self.guard, current = torch.cuda.device(self.index), self.index
             self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(current)
 
     def __exit__(self, *exc):
         if self.guard is not None:
@@ -498,11 +501,12 @@ class _on_device:
 
 
 def _device_tensor(t: Optional[torch.Tensor], dtype, shape, device, name: str, contiguous: bool = True):
+    """The tensor (or None), once its device, type, shape and layout are what a call needs."""
     if t is None:
         return None
     assert t.device == device, f"{name} must be on {device}"
-    assert t.dtype == dtype, f"{name} must be {dtype}"
-    assert shape is None or tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}"
+    assert t.dtype is dtype, f"{name} must be {dtype}"
+    assert shape is None or t.shape == shape, f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}"
     assert not contiguous or t.is_contiguous(), f"{name} must be contiguous"
     return t
 
@@ -520,6 +524,7 @@ class LogitRules:
         self.device = given[0].device if given else None
         self.batch = next((t.shape[0] for t in (history, repetition, frequency, presence, bias_ids) if t is not None), None)
         r = self.desc = McsdLogitRules()
+        self.call = McsdDesc()
         B, dev = self.batch, self.device
         if history is not None:
             assert history.dim() == 2 and (history.shape[1] <= 1 or history.stride(1) == 1), "history rows must be contiguous"
@@ -559,27 +564,27 @@ def mcsd_apply_logit_rules(logits: torch.Tensor, parent, cand: Optional[torch.Te
     lib = load_library()
     parent = np.ascontiguousarray(parent, dtype=np.int32)
     assert logits.is_cuda and logits.dim() == 3
-    B, rows, V = logits.shape
+    (B, rows, V), device = logits.shape, logits.device
     n_nodes = int(parent.shape[0])
     out = logits if out is None else out
-    assert out.shape == logits.shape and out.dtype == logits.dtype and out.device == logits.device
-    assert rules.device is None or rules.device == logits.device
+    assert out is logits or (out.shape == logits.shape and out.dtype is logits.dtype and out.device == device)
+    assert rules.device is None or rules.device == device
     assert rules.batch is None or rules.batch == B, "the rules are for another batch size"
     if rules.mask_index is not None:
         assert tuple(rules.mask_index.shape) == (B, n_nodes)
     elif rules.desc.masks:
         assert rules.desc.n_masks >= B * n_nodes, "masks without mask_index hold a row per node"
     assert not rules.desc.masks or rules.mask_words >= (V + 31) // 32, "mask rows are too short for the vocabulary"
-    _device_tensor(cand, torch.int32, (B, n_nodes), logits.device, "cand")
-    _device_tensor(status, torch.int32, (B,), logits.device, "status")
-    d = McsdDesc()
+    _device_tensor(cand, torch.int32, (B, n_nodes), device, "cand")
+    _device_tensor(status, torch.int32, (B,), device, "status")
+    d = rules.call
     d.batch, d.n_nodes, d.vocab, d.dtype, d.out_status = B, n_nodes, V, MCSD_DTYPE[logits.dtype], _ptr(status)
     with _on_device(logits.device) as stream:
         d.stream = stream
-        _check(lib.mcsd_apply_logit_rules(ctypes.byref(d), ctypes.byref(rules.desc), parent.ctypes.data, _ptr(cand),
-                                          _ptr(logits), _row_stride(logits) if rows else V, _ptr(out),
-                                          _row_stride(out) if rows else V, rows, int(node_begin),
-                                          int(rows if node_end is None else node_end)))
+        rc = lib.mcsd_apply_logit_rules(d, rules.desc, parent.ctypes.data, _ptr(cand), logits.data_ptr(),
+                                        _row_stride(logits) if rows else V, out.data_ptr(), _row_stride(out) if rows else V,
+                                        rows, node_begin, rows if node_end is None else node_end)
+    _check(rc)
     return out
 
 
@@ -630,7 +635,8 @@ class PageTables:
         d.slots, d.n_slots = _ptr(slots), 0 if slots is None else int(slots.numel())
         with _on_device(self.device) as stream:
             d.stream = stream
-            _check(self.lib.mcsd_build_page_tables(ctypes.byref(d)))
+            rc = self.lib.mcsd_build_page_tables(d)
+        _check(rc)
         return slots
 
 
@@ -645,6 +651,7 @@ class KvCache:
     `layer(i)` is the cache of one of several layers."""
 
     def __init__(self, pages: torch.Tensor, head_dim: int, page_size: int):
+        self.lib = load_library()
         block = mcsd_kv_block_bytes(head_dim, page_size)
         if block == 0:
             _check(-10)
@@ -675,9 +682,10 @@ class KvCache:
 def _rows_args(cache: KvCache, t: Optional[torch.Tensor], n: int, name: str):
     if t is None:
         return None, 0, 0
-    assert t.device == cache.device and tuple(t.shape) == (n, cache.n_heads, cache.head_dim) and t.stride(2) == 1, \
+    token, head, one = t.stride()
+    assert t.device == cache.device and t.shape == (n, cache.n_heads, cache.head_dim) and one == 1, \
         f"{name} must be [tokens, heads, head_dim] with contiguous rows on the cache's device"
-    return t.data_ptr(), (t.stride(0) if n > 1 else cache.n_heads * cache.head_dim), (t.stride(1) if cache.n_heads > 1 else cache.head_dim)
+    return t.data_ptr(), (token if n > 1 else cache.n_heads * cache.head_dim), (head if cache.n_heads > 1 else cache.head_dim)
 
 
 def mcsd_append_kv(cache: KvCache, keys: torch.Tensor, values: torch.Tensor, slots: torch.Tensor) -> None:
@@ -688,7 +696,8 @@ def mcsd_append_kv(cache: KvCache, keys: torch.Tensor, values: torch.Tensor, slo
     assert keys.dtype == values.dtype
     k, v = _rows_args(cache, keys, n, "keys"), _rows_args(cache, values, n, "values")
     with _on_device(cache.device) as stream:
-        _check(load_library().mcsd_append_kv(ctypes.byref(cache.desc), *k, *v, MCSD_DTYPE[keys.dtype], n, slots.data_ptr(), stream))
+        rc = cache.lib.mcsd_append_kv(cache.desc, *k, *v, MCSD_DTYPE[keys.dtype], n, slots.data_ptr(), stream)
+    _check(rc)
 
 
 def mcsd_read_kv(cache: KvCache, slots: torch.Tensor, dtype: Optional[torch.dtype] = None, *, keys: Optional[torch.Tensor] = None,
@@ -705,7 +714,8 @@ def mcsd_read_kv(cache: KvCache, slots: torch.Tensor, dtype: Optional[torch.dtyp
     assert all(t is None or t.dtype == given for t in (keys, values))
     k, v = _rows_args(cache, keys, n, "keys"), _rows_args(cache, values, n, "values")
     with _on_device(cache.device) as stream:
-        _check(load_library().mcsd_read_kv(ctypes.byref(cache.desc), *k, *v, MCSD_DTYPE[given], n, slots.data_ptr(), stream))
+        rc = cache.lib.mcsd_read_kv(cache.desc, *k, *v, MCSD_DTYPE[given], n, slots.data_ptr(), stream)
+    _check(rc)
     return keys, values
 
 
@@ -728,6 +738,7 @@ class TreeAttention:
         self.geometry = (cache.n_heads, cache.head_dim, cache.page_size)
         rc = self.lib.mcsd_tree_depth(self.parent.ctypes.data, self.n_nodes)
         _check(rc if rc < 0 else 0)
+        self.parent_ptr = self.parent.ctypes.data
         self.out = torch.zeros((self.batch, self.n_nodes, self.n_heads, self.head_dim), dtype=dtype, device=self.device)
         self.lse = torch.zeros((self.batch, self.n_nodes, self.n_heads), dtype=torch.float32, device=self.device) if want_lse else None
         d = self.desc = McsdAttentionDesc()
@@ -752,20 +763,21 @@ class TreeAttention:
         out = self.out if out is None else out
         assert cache.pages.dim() == 3, "one layer at a time: cache.layer(i)"
         assert cache.device == self.device and self.geometry == (cache.n_heads, cache.head_dim, cache.page_size)
-        for t in (q, out):
-            assert t.device == self.device and t.dtype == self.dtype and t.shape == shape and t.stride(3) == 1
+        qs, os_ = q.stride(), out.stride()
+        assert q.device == self.device and q.dtype is self.dtype and q.shape == shape and qs[3] == 1
+        assert out is self.out or (out.device == self.device and out.dtype is self.dtype and out.shape == shape and os_[3] == 1)
         _device_tensor(page_table, torch.int32, (self.batch, self.max_pages), self.device, "page_table", contiguous=False)
         assert self.max_pages <= 1 or page_table.stride(1) == 1
         _device_tensor(prefix_len, torch.int32, (self.batch,), self.device, "prefix_len")
         d.ld_table = int(page_table.stride(0)) if self.batch > 1 else self.max_pages
-        d.q_seq_stride, d.q_node_stride, d.q_head_stride = q.stride()[:3]
-        d.out_seq_stride, d.out_node_stride, d.out_head_stride = out.stride()[:3]
+        d.q_seq_stride, d.q_node_stride, d.q_head_stride, _ = qs
+        d.out_seq_stride, d.out_node_stride, d.out_head_stride, _ = os_
         d.scale = float(scale) if scale is not None else self.head_dim ** -0.5
         with _on_device(self.device) as stream:
             d.stream = stream
-            _check(self.lib.mcsd_tree_attention(ctypes.byref(d), ctypes.byref(cache.desc), page_table.data_ptr(),
-                                                prefix_len.data_ptr(), self.parent.ctypes.data, q.data_ptr(), out.data_ptr(),
-                                                _ptr(self.lse)))
+            rc = self.lib.mcsd_tree_attention(d, cache.desc, page_table.data_ptr(), prefix_len.data_ptr(), self.parent_ptr,
+                                              q.data_ptr(), out.data_ptr(), _ptr(self.lse))
+        _check(rc)
         return AttentionOutput(out, self.lse)
 
 
@@ -780,10 +792,10 @@ def mcsd_gather_accepted_pages(cache: KvCache, page_table: torch.Tensor, prefix_
     _device_tensor(accept_len, torch.int32, (B,), cache.device, "accept_len")
     _device_tensor(path_nodes, torch.int32, (B, path_nodes.shape[1]), cache.device, "path_nodes")
     with _on_device(cache.device) as stream:
-        _check(load_library().mcsd_gather_accepted_pages(
-            ctypes.byref(cache.desc), cache.n_layers, cache.layer_stride, page_table.data_ptr(),
-            int(page_table.stride(0)) if B > 1 else W, W, B, prefix_len.data_ptr(), path_nodes.data_ptr(),
-            accept_len.data_ptr(), int(path_nodes.shape[1]) - 1, stream))
+        rc = cache.lib.mcsd_gather_accepted_pages(
+            cache.desc, cache.n_layers, cache.layer_stride, page_table.data_ptr(), page_table.stride(0) if B > 1 else W, W, B,
+            prefix_len.data_ptr(), path_nodes.data_ptr(), accept_len.data_ptr(), path_nodes.shape[1] - 1, stream)
+    _check(rc)
     return cache.pages
 
 

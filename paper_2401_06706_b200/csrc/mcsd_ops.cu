@@ -1,7 +1,11 @@
 // Host side of the operators around the verification step: argument validation, launch configuration
 // and the extern "C" entry points from mcsd_apply_logit_rules on (mcsd.h).
+#include <atomic>
 #include <cmath>
 #include <cstring>
+#include <map>
+#include <mutex>
+#include <utility>
 
 #include "mcsd_common.cuh"
 #include "mcsd_rules.cuh"
@@ -14,12 +18,33 @@
 namespace mcsd {
 namespace {
 
+// Multiprocessors of the current device, 0 if there is none (asked once per device).
 int sm_count()
 {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
     int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
-        return 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev >= 0 && dev < kDevices && (n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev >= 0 && dev < kDevices) known[dev].store(n, std::memory_order_relaxed);
     return n;
+}
+
+// Shared memory beyond the default for a kernel, set once per kernel and device.
+template <typename Kernel>
+bool allow_smem(Kernel kernel, int bytes)
+{
+    static std::mutex lock;
+    static std::map<std::pair<const void *, int>, int> known;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return false;
+    std::lock_guard<std::mutex> hold(lock);
+    int &have = known[{reinterpret_cast<const void *>(kernel), dev}];
+    if (have >= bytes) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    have = bytes;
+    return true;
 }
 
 bool good_dtype(int dtype) { return dtype == MCSD_DTYPE_F32 || dtype == MCSD_DTYPE_BF16 || dtype == MCSD_DTYPE_F16; }
@@ -64,7 +89,7 @@ int launch_rules(const RulesParams &p, dim3 grid, size_t smem, bool vec, cudaStr
 {
     void (*kernel)(const RulesParams) = vec ? rules_kernel<DT, true> : rules_kernel<DT, false>;
     if (smem > 48 * 1024 &&                         // (trees some hundred levels deep)
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
+        !allow_smem(kernel, static_cast<int>(smem)))
         return MCSD_ERR_CUDA;
     kernel<<<grid, kRulesThreads, smem, st>>>(p);
     return launched(1);
@@ -184,7 +209,7 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
 template <int DT, int D, int ROWS>
 int launch_with_join(void (*kernel)(const AttendParams), int threads, int smem, const AttendParams &p, cudaStream_t st)
 {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return MCSD_ERR_CUDA;
+    if (!allow_smem(kernel, smem)) return MCSD_ERR_CUDA;
     kernel<<<p.n_ctas, threads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
@@ -308,9 +333,7 @@ int mcsd_build_page_tables(const mcsd_page_desc *d)
     if (ctas < (d->batch + 31) / 32) ctas = (d->batch + 31) / 32;
     if (ctas > sms) ctas = sms;
     const size_t smem = sizeof(int32_t) * (5 * static_cast<size_t>(d->batch) + 1);
-    if (smem > 40000 &&
-        cudaFuncSetAttribute(pages_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) != cudaSuccess)
-        return MCSD_ERR_CUDA;
+    if (smem > 40000 && !allow_smem(pages_kernel, static_cast<int>(smem))) return MCSD_ERR_CUDA;
     pages_kernel<<<static_cast<unsigned>(ctas), kPagesThreads, smem, static_cast<cudaStream_t>(d->stream)>>>(p);
     return launched(1);
 }
