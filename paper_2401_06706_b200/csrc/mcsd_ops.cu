@@ -429,8 +429,13 @@ int mcsd_gather_accepted_pages(const mcsd_kv_cache *cache, int64_t n_layers, int
     p.n_layers = n_layers; p.layer_stride = layer_stride;
     p.table = page_table; p.prefix_len = prefix_len; p.path_nodes = path_nodes; p.accept_len = accept_len;
     p.ld_table = ld_table; p.max_pages = max_pages; p.batch = batch; p.gamma = gamma;
-    const long long want = (n_layers * batch * cache->n_heads + 15) / 16, cap = static_cast<long long>(sm_count()) * 8;
+    // runs of layers as long as the threads of four CTAs per SM still have one each, up to eight
+    const long long cap = static_cast<long long>(sm_count()) * 8, lines = static_cast<long long>(batch) * cache->n_heads;
     if (cap <= 0) return MCSD_ERR_CUDA;
+    long long run = n_layers * lines / (cap / 2 * 16);
+    run = run < 1 ? 1 : run > 8 ? 8 : run;
+    p.layers_per_item = static_cast<int32_t>(run);
+    const long long want = ((n_layers + run - 1) / run * lines + 15) / 16;
     const unsigned grid = static_cast<unsigned>(want < cap ? want : cap);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (cache->head_dim == 128) move_kernel<128><<<grid, 256, 0, st>>>(p);
