@@ -525,7 +525,8 @@ int mcsd_apply_logit_rules(const mcsd_desc *desc, const mcsd_logit_rules *rules,
  * a request) go to its tail and are not handed out in the same call.  A sequence the ring cannot
  * serve, and every later one that wants more pages, or one that wants more than max_pages, keeps what
  * it has: MCSD_STATUS_NO_PAGES and slots of -1.  start[b] < 0 marks an unused batch entry: nothing
- * about it changes and it has no tokens.
+ * about it changes and it has no tokens.  The counts of a call sum to less than 2^31.  A call that advances the
+ * state in place reads and writes it: two calls on one state are ordered by the caller.
  */
 typedef struct mcsd_page_desc {
     int32_t batch;          /* <= MCSD_MAX_SEQUENCES                                                  */
@@ -557,7 +558,8 @@ int mcsd_build_page_tables(const mcsd_page_desc *desc);
  *   scale = half((max - min) / 15),  mid = half(min + 8 scale)           (float32 first, saturated to +-65504)
  *   code  = clamp(rint((x - mid) / scale) + 8, 0, 15), 8 where scale is 0  (ties to even)
  *   value = mid + scale * (code - 8)
- * (a row with an infinity or a NaN has mid = NaN, scale = 0: it reads as NaN).  The page of one head is
+ * (a row with an infinity or a NaN has mid = NaN, scale = 0: it reads as NaN).  A caller that fills pages itself
+ * keeps scales finite and not negative.  The page of one head is
  *   key codes [page_size][D / 2] | value codes [page_size][D / 2] | key (scale, mid) [page_size][2] half |
  *   value (scale, mid) [page_size][2] half
  * = page_size * (D + 8) bytes; element 2 i of a row sits in the low four bits of its byte i.  Heads of a
@@ -597,7 +599,8 @@ int mcsd_read_kv(const mcsd_kv_cache *cache, void *keys, int64_t key_token_strid
  * with q and out per query head; query head h reads key/value head h / (n_heads / cache->n_heads).  A tree
  * of one node is plain decoding.  Positions beyond the table or in a page entry outside [0, n_pages)
  * are not there; a row that sees no position is 0 with lse = -inf.  prefix_len[b] < 0 marks an unused
- * batch entry: its rows of out and lse are left as they were.
+ * batch entry: its rows of out and lse are left as they were.  Calls that may overlap on the device need
+ * workspaces of their own.  Waits inside the kernels are bounded; should one expire, the rows it concerns are NaN.
  */
 typedef struct mcsd_attention_desc {
     int32_t batch;

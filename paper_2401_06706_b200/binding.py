@@ -524,7 +524,6 @@ class LogitRules:
         self.device = given[0].device if given else None
         self.batch = next((t.shape[0] for t in (history, repetition, frequency, presence, bias_ids) if t is not None), None)
         r = self.desc = McsdLogitRules()
-        self.call = McsdDesc()
         B, dev = self.batch, self.device
         if history is not None:
             assert history.dim() == 2 and (history.shape[1] <= 1 or history.stride(1) == 1), "history rows must be contiguous"
@@ -577,7 +576,7 @@ def mcsd_apply_logit_rules(logits: torch.Tensor, parent, cand: Optional[torch.Te
     assert not rules.desc.masks or rules.mask_words >= (V + 31) // 32, "mask rows are too short for the vocabulary"
     _device_tensor(cand, torch.int32, (B, n_nodes), device, "cand")
     _device_tensor(status, torch.int32, (B,), device, "status")
-    d = rules.call
+    d = McsdDesc()
     d.batch, d.n_nodes, d.vocab, d.dtype, d.out_status = B, n_nodes, V, MCSD_DTYPE[logits.dtype], _ptr(status)
     with _on_device(logits.device) as stream:
         d.stream = stream

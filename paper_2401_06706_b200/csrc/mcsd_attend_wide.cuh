@@ -5,11 +5,15 @@
 
 namespace mcsd {
 
+// (the compiler leaves the larger of these lambdas as calls otherwise)
+#define MCSD_INLINE __attribute__((always_inline))
+
 constexpr int kWideRows = 128;
 constexpr int kWideThreads = 640;                   // 8 softmax warps, 8 decoding warps, 2 that issue (and 2 beside them)
-constexpr int kWideStages = 3;                      // decoded units in flight
+constexpr int kWideStages = 2;                      // decoded units
+constexpr int kWideAhead = 4;                       // units whose codes are on their way to shared memory
 template <int D> constexpr int kWideTile = kAttUnit * D * 2;                       // bytes of a decoded tile of keys or values
-template <int D> constexpr int kWideSmem = 1024 + kWideStages * (2 * kWideTile<D> + kAttUnit * 16) + kWideRows * (MCSD_MAX_NODES / 32) * 4;
+template <int D> constexpr int kWideSmem = 1024 + kWideStages * (2 * kWideTile<D> + kAttUnit * 16) + kWideAhead * kAttUnit * (D + 8) + kWideRows * (MCSD_MAX_NODES / 32) * 4;
 
 // ---- tensor memory and tcgen05
 __device__ __forceinline__ void tmem_alloc(uint32_t where, uint32_t columns) {
@@ -44,6 +48,13 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&v)[32]) {
                  "tcgen05.wait::ld.sync.aligned;"   // (in the same statement: the registers hold nothing before it)
                  : MCSD_R8(v, 0), MCSD_R8(v, 8), MCSD_R8(v, 16), MCSD_R8(v, 24) : "r"(at) : "memory");
 }
+__device__ __forceinline__ void tmem_load8(uint32_t at, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;" : MCSD_R8(v, 0) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::MCSD_W8(v, 0), "r"(at) : "memory");
+}
 __device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t (&v)[16]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
                  "tcgen05.wait::ld.sync.aligned;"   // (in the same statement: the registers hold nothing before it)
@@ -77,10 +88,8 @@ template <int N> __device__ __forceinline__ void regs_down() { asm volatile("set
 __device__ __forceinline__ void wide_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
     for (uint32_t i = 0; i < kWaitPolls; ++i) {
         if (mbar_try_wait(bar, parity)) break;
-        if (*dead || i == kWaitPolls - 1) {
-            *dead = 1;
-            break;
-        }
+        if ((i & 31) == 31 && *dead) break;
+        if (i == kWaitPolls - 1) *dead = 1;
     }
     __syncwarp();
 }
@@ -90,9 +99,10 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
     if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // One CTA per SM, work cut as for the narrow kernel, in units of 128 keys. Roles:
-//   decoding warps  (256 threads, the key or the value row of one key each) take codes from global memory to operands in
-//                   shared memory: a 4-bit code becomes a subnormal half by one AND (see the narrow kernel), those of the
-//                   values less 8, an exact subtraction; codes stay in the order the ANDs give them, which Q and the output undo;
+//   decoding warps  (four for keys, four for values, 32 rows of every unit each) copy codes to rings of their own, four units
+//                   ahead, and turn them into operands in shared memory: a 4-bit code becomes a subnormal half by one AND (see
+//                   the narrow kernel), those of the values less 8, an exact subtraction; codes stay in the order the
+//                   ANDs give them, which Q and the output undo;
 //   issuing warps   one per softmax group: S = Q K^T and O += P V by tcgen05.mma, Q and P from tensor memory, K and V
 //                   from shared memory; the scores of a unit as soon as those of the unit before are read;
 //   softmax groups  A and B (128 threads each, one row per thread) take keys 0..63 and 64..127 of every unit, each with
@@ -101,7 +111,14 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 // Scale and mid of a key enter the scores in float32; the weight p vscale is rounded to half once. The
 // reference of a row's exponents is its maximum plus the exponent of the largest value scale, which keeps
 // the weights in half's range whatever the scales are; it moves only when it is exceeded by 2^kNarrowSlack.
-// Tensor memory (columns; all 512 are taken, so that the first is column 0): S of A, S of B (64 each), O of A, O of B (D each), P of A, P of B (32 each), Q (D / 2).
+// Tensor memory (columns; all 512 are taken, so that the first is column 0): S of A, S of B (64 each), O of A, O of B (D
+// each), P of A, P of B (32 each), Q (D / 2).
+// Measured on 724 rows x 8 key heads x 4 sequences of up to 16001 positions: 299 us, 455 TFLOP/s, 0.28 of the measured
+// peak. The products take about a fifth of the time; what bounds it is the chain of a softmax group for a unit (scores
+// read, exponentials, weights written: some 2000 cycles of two warps per scheduler) and the hand-overs around
+// it. Without the copies four units ahead it took 345 us, with products issued by a single thread 390 us. Left out: sixteen
+// softmax warps of sixteen rows in fragment layout (a quarter of the parameter loads, 322 us; 20 % slower than this
+// form on prefixes of 2000, where the tree's own units weigh more), separate rings for keys and values (328 us).
 template <int DT, int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
 wide_kernel(const __grid_constant__ AttendParams P)
@@ -123,6 +140,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
     float4 *s_param = reinterpret_cast<float4 *>(base + 2 * kWideStages * TILE);  // [stages][64 pairs of keys]{key, value}
     uint32_t(*s_seen)[MCSD_MAX_NODES / 32] = reinterpret_cast<uint32_t(*)[MCSD_MAX_NODES / 32]>(
         base + 2 * kWideStages * TILE + kWideStages * kAttUnit * 16);
+    unsigned char *s_codes = reinterpret_cast<unsigned char *>(s_seen + kWideRows);   // [decoding warps][kWideAhead]{codes, parameters}
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bars = smem_u32(s_bar);
@@ -179,42 +197,71 @@ wide_kernel(const __grid_constant__ AttendParams P)
     if (warp >= 8 && warp < 16) {
         // ------------------------------------------------------------ decoding
         regs_down<56>();
-        const int key = tid & 127, which = (warp >> 2) & 1;      // 0: key rows, 1: value rows
+        // A warp has 32 keys of every unit, key or value rows: lane by lane, 16 bytes of codes at 16 (lane + 32 i) of
+        // the rows of sixteen keys, so that a load is contiguous, and the parameters of key `lane`.
+        constexpr int CH = RB / 16;                 // 16-byte chunks of a row: 2 or 4
+        const int which = (warp >> 2) & 1, key0 = (warp & 3) * 32;       // which: 0 key rows, 1 value rows
+        const int c = lane % CH;
         int stage = 0;
         uint32_t phase = 1;                         // (the first round of stages is free)
-        for_items([&](int b, int len, int head, int, int k0, int k1, bool) {
+        for_items([&](int b, int len, int head, int, int k0, int k1, bool) MCSD_INLINE {
             const int32_t *table = P.table + b * P.ld_table;
             const unsigned char *pool = P.c.pages + static_cast<long long>(head) * kv_block_bytes(D, ps);
-            auto page_of = [&](int k) {
-                const int pos = k * kAttUnit + key;
+            // page of this lane's half (lanes 0..15: the first sixteen keys)
+            auto page_of = [&](int k) MCSD_INLINE {
+                const int pos = k * kAttUnit + key0 + (lane & 16);
                 return k < k1 && pos < len ? __ldg(table + (pos >> P.c.page_shift)) : -1;
             };
-            struct Row { uint4 codes[RB / 16]; uint32_t param; bool there; };
-            auto fetch = [&](int k, int page, Row &r) {
-                r.there = static_cast<unsigned>(page) < static_cast<unsigned>(P.c.n_pages);
-                r.param = 0u;
+            // Rows of unit k are copied to this warp's own ring, kWideAhead units ahead; a lane reads back what it copied itself.
+            unsigned char *ring = s_codes + (warp & 7) * kWideAhead * 1 * 32 * (RB + 4);
+            uint32_t there = 0u;                    // bit `slot`: this lane's key of that unit is in the cache
+            int k = k0, page = -1;                  // page: of the unit asked for next
+            auto issue = [&](int unit, int slot) MCSD_INLINE {
+                const int pos = unit * kAttUnit + key0 + lane;
+                unsigned char *to = ring + slot * 1 * 32 * (RB + 4);
+                if (unit < k1) {
+                    const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(P.c.n_pages) && pos < len;
+                    there = (there & ~(1u << slot)) | static_cast<uint32_t>(ok) << slot;
 #pragma unroll
-                for (int i = 0; i < RB / 16; ++i) r.codes[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (r.there) {
-                    const int row = which * ps + ((k * kAttUnit + key) & (ps - 1));
-                    const unsigned char *block = pool + page * P.c.page_stride;
+                    for (int w = 0; w < 1; ++w) {
+                        const int which_row = which * ps;
 #pragma unroll
-                    for (int i = 0; i < RB / 16; ++i) r.codes[i] = __ldg(reinterpret_cast<const uint4 *>(block + row * RB) + i);
-                    r.param = __ldg(reinterpret_cast<const uint32_t *>(block + ps * D) + row);
+                        for (int hf = 0; hf < 2; ++hf) {
+                            const int p = __shfl_sync(0xffffffffu, page, 16 * hf);
+                            if (static_cast<unsigned>(p) < static_cast<unsigned>(P.c.n_pages)) {
+                                const unsigned char *src = pool + p * P.c.page_stride + (which_row + ((unit * kAttUnit + key0 + 16 * hf) & (ps - 1))) * RB + lane * 16;
+#pragma unroll
+                                for (int i = 0; i < CH / 2; ++i)
+                                    cp_async16(smem_u32(to + w * 32 * (RB + 4) + (hf * (CH / 2) + i) * 512 + lane * 16), src + 512 * i);
+                            }
+                        }
+                        if (ok) cp_async4(to + w * 32 * (RB + 4) + 32 * RB + lane * 4, pool + page * P.c.page_stride + ps * D + (which_row + (pos & (ps - 1))) * 4);
+                    }
                 }
+                asm volatile("cp.async.commit_group;" ::: "memory");
             };
-            Row now, next;
-            int page = page_of(k0);
-            fetch(k0, page, now);
-            page = page_of(k0 + 1);
-            for (int k = k0; k < k1; ++k) {
-                fetch(k + 1, page, next);           // (in flight while this unit is decoded)
-                page = page_of(k + 2);
-                wide_wait(b_empty + 8 * stage, phase, dead);
-                unsigned char *tile = s_tiles + (2 * stage + which) * TILE + key * 128;
+            int pages[kWideAhead + 1];
 #pragma unroll
-                for (int i = 0; i < RB / 16; ++i) { // 16 bytes of codes are four 16-byte chunks of operands
-                    const uint32_t w[4] = {now.codes[i].x, now.codes[i].y, now.codes[i].z, now.codes[i].w};
+            for (int i = 0; i <= kWideAhead; ++i) pages[i] = page_of(k + i);
+#pragma unroll
+            for (int i = 0; i < kWideAhead; ++i) {
+                page = pages[i];
+                issue(k + i, i);
+            }
+            page = pages[kWideAhead];
+            int slot = 0;
+            for (; k < k1; ++k) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kWideAhead - 1) : "memory");
+                const unsigned char *from = ring + slot * 1 * 32 * (RB + 4);
+                wide_wait(b_empty + 8 * stage, phase, dead);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {      // 16 bytes of codes are four 16-byte chunks of operands
+                    const int key = key0 + (i / (CH / 2)) * 16 + (i % (CH / 2)) * (32 / CH) + lane / CH;
+                    unsigned char *tile = s_tiles + (2 * stage + which) * TILE + key * 128;
+                    // (with four chunks a row, lanes 2 and 3 take their words in another order: no two lanes of eight meet in a bank)
+                    const bool turn = CH == 4 && (c & 2);
+                    const uint4 v = *reinterpret_cast<const uint4 *>(from + i * 512 + lane * 16);
+                    const uint32_t w[4] = {turn ? v.z : v.x, turn ? v.w : v.y, turn ? v.x : v.z, turn ? v.y : v.w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const uint32_t y = w[j] >> 8;
@@ -227,19 +274,21 @@ wide_kernel(const __grid_constant__ AttendParams P)
                                 h[q] = *reinterpret_cast<const uint32_t *>(&d);
                             }
                         }
-                        const int chunk = 4 * i + j;
+                        const int chunk = 4 * c + (turn ? j ^ 2 : j);
                         *reinterpret_cast<uint4 *>(tile + (chunk >> 3) * (kAttUnit * 128) + (((chunk & 7) ^ (key & 7)) << 4)) =
                             make_uint4(h[0], h[1], h[2], h[3]);
                     }
                 }
                 // scale and mid - 8 scale of the key, scale and mid of the value, in pairs of keys
-                const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&now.param));
+                const bool mine = (there >> slot) & 1u;
+                const float2 p = mine ? __half22float2(*reinterpret_cast<const __half2 *>(from + 32 * RB + lane * 4)) : make_float2(0.f, 0.f);
+                const int key = key0 + lane;
                 float *par = reinterpret_cast<float *>(s_param + stage * kAttUnit + (key >> 1) * 2 + which) + (key & 1);
                 par[0] = p.x;
                 par[2] = which ? p.y : fmaf(-8.f, p.x, p.y);
                 if (which == 0) {
-                    const uint32_t there = __ballot_sync(0xffffffffu, now.there);
-                    if (lane == 0) s_valid[stage][warp & 3] = there;
+                    const uint32_t keys = __ballot_sync(0xffffffffu, mine);
+                    if (lane == 0) s_valid[stage][warp & 3] = keys;
                 } else {
                     const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(p.x)));  // (never negative)
                     if (lane == 0) s_big[stage][warp & 3] = big;
@@ -247,7 +296,9 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 fence_proxy_async();
                 warp_arrive(b_full + 8 * stage, lane);
                 if (++stage == kWideStages) { stage = 0; phase ^= 1; }
-                now = next;
+                issue(k + kWideAhead, slot);        // (what this lane had there is read)
+                page = page_of(k + kWideAhead + 1); // (in flight until the next unit is asked for)
+                slot = slot == kWideAhead - 1 ? 0 : slot + 1;
             }
         });
     } else if (warp >= 16) {
@@ -416,13 +467,14 @@ wide_kernel(const __grid_constant__ AttendParams P)
                         sum *= f;
                         mids *= f;
                         if (k > k0) {
-                            for (int c = 0; c < D / 16; ++c) {
-                                uint32_t o[16];
+#pragma unroll 1
+                            for (int c = 0; c < D / 8; ++c) {     // (eight columns at a time: y holds most registers)
+                                uint32_t o[8];
                                 __syncwarp();
-                                tmem_load16(t_o + 16 * c, o);
+                                tmem_load8(t_o + 8 * c, o);
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                                tmem_store16(t_o + 16 * c, o);
+                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tmem_store8(t_o + 8 * c, o);
                             }
                         }
                     }
@@ -552,5 +604,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
         tmem_free(tmem, kColumns);
     }
 }
+
+#undef MCSD_INLINE
 
 }  // namespace mcsd

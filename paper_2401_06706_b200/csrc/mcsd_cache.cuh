@@ -61,7 +61,9 @@ __device__ __forceinline__ RowWalk row_walk(const RowsParams &P)
 // 8 and stores one word of codes.  Rows of a token's heads follow each other in the thread order, so that
 // loads are contiguous (a page's rows of one head are 32 to 64 contiguous bytes each).  Bound by HBM: 2 D
 // numbers read and D + 8 bytes written per key/value row pair; a thread takes kRowsAhead tokens at a time, so
-// that their slots, and then their numbers, are in flight together.
+// that their slots, and then their numbers, are in flight together.  Measured on 40001 tokens x 8 heads x 128 halves: 104 us
+// (0.30 of the measured copy bandwidth: some 200 instructions for the two rows of a warp are what bounds it), the way
+// back 59 us (0.54).
 // Scale, mid and codes are those of the definition in exact arithmetic: the two per-row numbers are formed
 // in double (by one of a row's threads), and where a float32 quotient lies within 2^-18 of a border between two codes
 // (two float32 roundings and a reciprocal good to 2^-23 put a number up to 8.5 off by 2^-18.9 at most) the thread's codes are decided in double; so no code depends on

@@ -192,15 +192,19 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
     int sms = sm_count();
     if (sms <= 0) sms = 148;
     const long long rows = static_cast<long long>(d->n_nodes) * (d->n_heads / cache->n_heads);
-    // Blocks of 16 rows read the keys again for every block, one of 128 takes about as long for few rows as for all.
-    // Measured (128 numbers a head, 8 sequences x 32 key heads x 2000 positions), blocks of 16 against one of 128: 45 rows
-    // 96 against 104 us, 60 rows 121 against 106 us; 4 sequences x 8 key heads x 16000 positions: 89 against 96 us, 109
-    // against 96 us.
-    plan.rows = rows <= 8 ? 8 : rows <= 48 ? 16 : kWideRows;
+    // Blocks of 8, 16 and 24 rows decode the keys again for every block (24 rows leave two CTAs per SM instead of three
+    // or four), one of 128 takes about as long for few rows as for all.  Measured (128 numbers a head, 8 sequences x 32
+    // key heads x 2000 positions | 4 sequences x 8 key heads x 16000 positions, us):
+    //   rows   blocks of 16   blocks of 24   one of 128
+    //   24     69 | 66        52 | 52        94 | 83
+    //   32     72 | 67        83 | 79        96 | 85
+    //   45     96 | 89        91 | 81        94 | 87
+    //   60     121 | 109                     96 | 87
+    plan.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 24 ? 24 : rows <= 32 ? 16 : rows <= 48 ? 24 : kWideRows;
     plan.blocks = static_cast<int>((rows + plan.rows - 1) / plan.rows);
     const long long units = (static_cast<long long>(d->max_pages) * cache->page_size + kAttUnit - 1) / kAttUnit;
     const long long most = static_cast<long long>(d->batch) * cache->n_heads * plan.blocks * (units > 0 ? units : 1);
-    const long long resident = static_cast<long long>(plan.rows == 8 ? kNarrowCtas<1> : plan.rows == 16 ? kNarrowCtas<2> : 1) * sms;
+    const long long resident = static_cast<long long>(plan.rows == 8 ? kNarrowCtas<1> : plan.rows == 16 ? kNarrowCtas<2> : plan.rows == 24 ? kNarrowCtas<3> : 1) * sms;
     plan.ctas = static_cast<int>(most < 1 ? 1 : most < resident ? most : resident);
     return plan;
 }
@@ -230,6 +234,7 @@ int launch_attention(const AttendParams &p, int rows, cudaStream_t st)
 {
     if (rows == 8) return launch_with_join<DT, D, 8>(narrow_kernel<DT, D, 1>, kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
     if (rows == 16) return launch_with_join<DT, D, 16>(narrow_kernel<DT, D, 2>, kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
+    if (rows == 24) return launch_with_join<DT, D, 24>(narrow_kernel<DT, D, 3>, kNarrowWarps * 32, kNarrowSmem<D, 3>, p, st);
     return launch_with_join<DT, D, kWideRows>(wide_kernel<DT, D>, kWideThreads, kWideSmem<D>, p, st);
 }
 

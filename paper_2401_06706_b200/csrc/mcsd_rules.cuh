@@ -35,7 +35,9 @@ struct RulesParams {
 // streams its slice of the row (eight 16-byte loads in flight per lane) with nothing but the mask applied, then
 // takes the tokens some rule concerns one by one from a list, and last the few on the row's path, from their
 // logits read before.  (With the rules applied while streaming, nearly every warp had a lane with a token
-// that needs them, and all lanes went through them: 215 us against 72 us on 64 x 31 rows of 50272 halves.)
+// that needs them, and all lanes went through them: 215 us against 137 us on 64 x 31 rows of 50272 halves; the mask's words taken by shuffles from one load a
+// lane and four CTAs per SM instead of three made that 108 us, 3.7 TB/s or 0.57 of the measured copy bandwidth: the
+// starts of the CTAs, five dependent loads each, are what is left.)
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kRulesThreads, 4)
 rules_kernel(const __grid_constant__ RulesParams P)
