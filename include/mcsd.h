@@ -621,7 +621,8 @@ typedef struct mcsd_attention_desc {
 /* Depends on the sizes only, not on the lengths; 0 for a descriptor that is not valid. */
 size_t mcsd_tree_attention_workspace_bytes(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache);
 
-/* q, out device as described; lse device [B][n_nodes][n_heads] float32 or NULL. */
+/* q, out device as described (out may be q, with the same strides; they must not overlap otherwise); lse device
+ * [B][n_nodes][n_heads] float32 or NULL. */
 int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
                         const int32_t *prefix_len, const int32_t *tree_parent, const void *q, void *out, float *lse);
 

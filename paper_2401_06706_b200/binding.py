@@ -726,7 +726,8 @@ class AttentionOutput:
 
 class TreeAttention:
     """Attention of a draft tree over a paged 4-bit cache: holds the descriptor, the outputs and the workspace of one
-    (batch, tree, heads, dtype, cache geometry) shape, so that repeated calls allocate nothing (see mcsd.h)."""
+    (batch, tree, heads, dtype, cache geometry) shape, so that repeated calls allocate nothing (see mcsd.h). One call at a
+    time: calls that may overlap, from other threads or on other streams or in captured graphs, take an object each."""
 
     def __init__(self, batch: int, parent, n_heads: int, dtype: torch.dtype, cache: KvCache, max_pages: int, *, want_lse: bool = True):
         self.lib = load_library()

@@ -264,7 +264,7 @@ narrow_kernel(const __grid_constant__ AttendParams P)
                 if (P.q_vec) {
                     const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + at * 2);
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) Elem<DT>::unpack(__ldg(src + i), x + 8 * i);
+                    for (int i = 0; i < D / 32; ++i) Elem<DT>::unpack(src[i], x + 8 * i);   // (not the read-only path: out may be q)
                 } else {
 #pragma unroll
                     for (int i = 0; i < D / 4; ++i) x[i] = load_elem<DT>(P.q, at + i);

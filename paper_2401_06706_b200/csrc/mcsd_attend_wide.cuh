@@ -213,30 +213,25 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 return k < k1 && pos < len ? __ldg(table + (pos >> P.c.page_shift)) : -1;
             };
             // Rows of unit k are copied to this warp's own ring, kWideAhead units ahead; a lane reads back what it copied itself.
-            unsigned char *ring = s_codes + (warp & 7) * kWideAhead * 1 * 32 * (RB + 4);
+            unsigned char *ring = s_codes + (warp & 7) * kWideAhead * 32 * (RB + 4);
             uint32_t there = 0u;                    // bit `slot`: this lane's key of that unit is in the cache
             int k = k0, page = -1;                  // page: of the unit asked for next
             auto issue = [&](int unit, int slot) MCSD_INLINE {
                 const int pos = unit * kAttUnit + key0 + lane;
-                unsigned char *to = ring + slot * 1 * 32 * (RB + 4);
+                unsigned char *to = ring + slot * 32 * (RB + 4);
                 if (unit < k1) {
                     const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(P.c.n_pages) && pos < len;
                     there = (there & ~(1u << slot)) | static_cast<uint32_t>(ok) << slot;
 #pragma unroll
-                    for (int w = 0; w < 1; ++w) {
-                        const int which_row = which * ps;
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const int p = __shfl_sync(0xffffffffu, page, 16 * hf);
+                        if (static_cast<unsigned>(p) < static_cast<unsigned>(P.c.n_pages)) {
+                            const unsigned char *src = pool + p * P.c.page_stride + (which * ps + ((unit * kAttUnit + key0 + 16 * hf) & (ps - 1))) * RB + lane * 16;
 #pragma unroll
-                        for (int hf = 0; hf < 2; ++hf) {
-                            const int p = __shfl_sync(0xffffffffu, page, 16 * hf);
-                            if (static_cast<unsigned>(p) < static_cast<unsigned>(P.c.n_pages)) {
-                                const unsigned char *src = pool + p * P.c.page_stride + (which_row + ((unit * kAttUnit + key0 + 16 * hf) & (ps - 1))) * RB + lane * 16;
-#pragma unroll
-                                for (int i = 0; i < CH / 2; ++i)
-                                    cp_async16(smem_u32(to + w * 32 * (RB + 4) + (hf * (CH / 2) + i) * 512 + lane * 16), src + 512 * i);
-                            }
+                            for (int i = 0; i < CH / 2; ++i) cp_async16(smem_u32(to + (hf * (CH / 2) + i) * 512 + lane * 16), src + 512 * i);
                         }
-                        if (ok) cp_async4(to + w * 32 * (RB + 4) + 32 * RB + lane * 4, pool + page * P.c.page_stride + ps * D + (which_row + (pos & (ps - 1))) * 4);
                     }
+                    if (ok) cp_async4(to + 32 * RB + lane * 4, pool + page * P.c.page_stride + ps * D + (which * ps + (pos & (ps - 1))) * 4);
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
@@ -252,7 +247,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
             int slot = 0;
             for (; k < k1; ++k) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(kWideAhead - 1) : "memory");
-                const unsigned char *from = ring + slot * 1 * 32 * (RB + 4);
+                const unsigned char *from = ring + slot * 32 * (RB + 4);
                 wide_wait(b_empty + 8 * stage, phase, dead);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {      // 16 bytes of codes are four 16-byte chunks of operands
@@ -368,7 +363,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
                     const long long at = b * P.q_seq + node * P.q_node + h * P.q_head;
                     if (P.q_vec) {
 #pragma unroll
-                        for (int c = 0; c < D / 8; ++c) raw[c] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + 2 * at) + c);
+                        for (int c = 0; c < D / 8; ++c) raw[c] = (reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + 2 * at))[c];   // (not the read-only path: out may be q)
                     } else {
                         const unsigned short *src = static_cast<const unsigned short *>(P.q) + at;
 #pragma unroll

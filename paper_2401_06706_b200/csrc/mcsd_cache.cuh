@@ -281,14 +281,17 @@ struct MoveParams {
 // Sixteen threads per (run of layers, sequence, head): D / 32 of them own 16 bytes of the key codes each, as many
 // 16 bytes of the value codes, one the key parameters, one the value parameters.  As in gather_kernel,
 // nodes ascend along a path and lie at or behind their destination, so a thread that handles its columns
-// in ascending order never reads what it has overwritten; up to kBatch moves are read before one is written.
+// in ascending order never reads what it has overwritten; up to kBatch moves in each of kLayers layers are read before
+// one is written.
 // Where a row lies is the same in every layer, so a thread finds out once (three loads, each from the one before) and
-// uses it for its run of layers: 35 -> 23 us with runs of six layers instead of one (256 sequences, 32 layers, 8 heads).
+// uses it for its run of layers.  256 sequences, 32 layers, 8 heads: 21 us, with one layer at a time 24 us, with runs of one
+// layer instead of six 35 us. Some 90000 row pairs are four pieces of 4 to 64 bytes each there, read and written at
+// unrelated places: 32-byte sectors make that twice the bytes it moves, and the places bound it, not the rate.
 template <int D>
 __global__ void __launch_bounds__(256)
 move_kernel(const MoveParams P)
 {
-    constexpr int kBatch = 8, NC = D / 32;
+    constexpr int kBatch = 4, kLayers = 2, NC = D / 32;
     const int ps = 1 << P.c.page_shift, lane = threadIdx.x & 15;
     const long long n_items = (P.n_layers + P.layers_per_item - 1) / P.layers_per_item * P.batch * P.c.n_heads;
     const bool wide = lane < 2 * NC;                // a column of codes; then two threads with parameters
@@ -325,21 +328,28 @@ move_kernel(const MoveParams P)
                 from[u] = nd > i + 1 ? place(static_cast<long long>(prefix) + nd) : -1;
                 to[u] = nd > i + 1 ? place(static_cast<long long>(prefix) + 1 + i) : -1;
             }
-            for (long long layer = layer0; layer < layer1; ++layer) {
-                unsigned char *here = base + layer * P.layer_stride;
-                uint4 v[kBatch];
+            for (long long layer = layer0; layer < layer1; layer += kLayers) {
+                uint4 v[kLayers][kBatch];
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u)
-                    if (from[u] >= 0 && to[u] >= 0) {
-                        if (wide) v[u] = *reinterpret_cast<const uint4 *>(here + from[u]);
-                        else v[u].x = *reinterpret_cast<const uint32_t *>(here + from[u]);
-                    }
+                for (int y = 0; y < kLayers; ++y) {
+                    const unsigned char *here = base + (layer + y) * P.layer_stride;
 #pragma unroll
-                for (int u = 0; u < kBatch; ++u)
-                    if (from[u] >= 0 && to[u] >= 0) {
-                        if (wide) *reinterpret_cast<uint4 *>(here + to[u]) = v[u];
-                        else *reinterpret_cast<uint32_t *>(here + to[u]) = v[u].x;
-                    }
+                    for (int u = 0; u < kBatch; ++u)
+                        if (from[u] >= 0 && to[u] >= 0 && layer + y < layer1) {
+                            if (wide) v[y][u] = *reinterpret_cast<const uint4 *>(here + from[u]);
+                            else v[y][u].x = *reinterpret_cast<const uint32_t *>(here + from[u]);
+                        }
+                }
+#pragma unroll
+                for (int y = 0; y < kLayers; ++y) {
+                    unsigned char *here = base + (layer + y) * P.layer_stride;
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+                        if (from[u] >= 0 && to[u] >= 0 && layer + y < layer1) {
+                            if (wide) *reinterpret_cast<uint4 *>(here + to[u]) = v[y][u];
+                            else *reinterpret_cast<uint32_t *>(here + to[u]) = v[y][u].x;
+                        }
+                }
             }
         }
     }

@@ -211,6 +211,17 @@ def test_strided_queries_outputs_and_tables():
         assert (big[..., D:] == 2).all()
 
 
+@pytest.mark.parametrize("kconfig,heads", [("", 2), ("4x2x2x1", 8)])
+def test_output_in_place_of_the_queries(kconfig, heads):
+    """out may be q: a row of queries is read before its result is written, in whole and in divided items."""
+    parent, q, cache, table, prefix = _problem(19, 5, kconfig, heads, 2, 128, 16, [1000, 31, 2500, 130, 7], torch.bfloat16)
+    want = _run(q, cache, table, prefix, parent)
+    att = binding.TreeAttention(5, parent, heads, q.dtype, cache, table.shape[1])
+    got = att.mcsd_tree_attention(q, cache, table, prefix, out=q)
+    torch.cuda.synchronize()
+    assert got.out is q and torch.equal(q, want.out) and torch.equal(got.lse, want.lse)
+
+
 def test_capture_replay_streams_and_a_shared_workspace():
     """A captured call replayed with new lengths, tables and queries; the same object used eagerly in between (its
     workspace is rewritten by every call); a second object on another stream at the same time."""

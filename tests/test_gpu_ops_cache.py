@@ -161,6 +161,31 @@ def test_accepted_rows_move(D, ps, layers, heads, kconfig):
     assert np.array_equal(cache.pages.cpu().numpy().reshape(want.shape), want)
 
 
+@pytest.mark.parametrize("layers", [27, 40])
+def test_accepted_rows_move_in_many_layers(layers):
+    """Enough (layer, sequence, head) triples that a thread has a run of layers (4 of 27, so the last run is shorter; 6
+    of 40), with paths longer than the moves it takes at once."""
+    D, ps, heads, B, gamma = 64, 16, 8, 200, 6
+    parent = synth.tree_from_kconfig([2, 2, 1, 1, 1, 1])
+    rng = np.random.default_rng(layers)
+    prefix = rng.integers(0, ps, B).astype(np.int32)
+    W = (ps + len(parent)) // ps + 1
+    table = rng.permutation(B * W).reshape(B, W).astype(np.int32)
+    nodes = np.full((B, gamma + 1), -1, dtype=np.int32)
+    accept = rng.integers(0, gamma + 1, B).astype(np.int32)
+    for b in range(B):
+        n = 0
+        for i in range(accept[b]):
+            n = int(rng.choice([c for c in range(len(parent)) if parent[c] == n]))
+            nodes[b, i] = n
+    pages = rng.integers(0, 256, (layers, B * W, heads, binding.mcsd_kv_block_bytes(D, ps)), dtype=np.uint8)
+    cache = binding.KvCache(torch.from_numpy(pages).cuda(), D, ps)
+    c = lambda a: torch.from_numpy(a).cuda()
+    binding.mcsd_gather_accepted_pages(cache, c(table), c(prefix), c(nodes), c(accept))
+    want = ref.move(pages, table, prefix, nodes, accept, D, ps)
+    assert np.array_equal(cache.pages.cpu().numpy().reshape(want.shape), want)
+
+
 def test_one_layer_of_several_and_empty_calls():
     cache = binding.KvCache.empty(4, 2, 64, 16, n_layers=3)
     x = torch.randn((5, 2, 64), device="cuda")
