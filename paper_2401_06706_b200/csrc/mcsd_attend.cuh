@@ -23,6 +23,7 @@ struct AttendParams {
     int32_t n_rows;                                 // n_nodes * group: rows that share a key/value head
     int32_t n_blocks;                               // blocks of rows per key/value head
     int32_t n_ctas;                                 // CTAs the work is cut for
+    uint32_t lead;                                  // places of the cut an item costs beside its units
     int32_t q_vec, o_vec;                           // rows of q may be read, those of out written in 16-byte vectors
     float scale;
     int16_t parent[MCSD_MAX_NODES];
@@ -41,33 +42,53 @@ __device__ __forceinline__ int att_len(const AttendParams &P, int b)
 }
 __device__ __forceinline__ int att_units(int len) { return len < 0 ? 0 : max((len + kAttUnit - 1) / kAttUnit, 1); }
 
-// Units before sequence `stop` (all of them for stop == batch) of one item per sequence; every lane gets the sum.
-// (The host refuses calls that could have 2^32 units in all.)
-__device__ __forceinline__ uint32_t att_units_before(const AttendParams &P, int stop, int lane)
+// The cut: `span` places in all, `per` of them to a CTA. An item begins with `lead` places that stand for what it costs
+// beside its units (its queries, the units that hold the tree, its results). Without them a CTA with many short
+// items is the last to end: 32 sequences of up to 1000 positions, 31 rows x 32 heads: 249 -> 126 us; 4 of up to 16001, 724 rows
+// x 8 heads: 294 -> 171 us; 64 decoding ones of up to 8191 x 8 heads: 103 -> 87 us (random lengths; equal ones are as before).
+struct AttCut { uint32_t lead, span, per; };
+
+// Places before sequence `stop` (all of them for stop == batch) of one item per sequence; every lane gets the sum.
+// (The host refuses calls that could have 2^32 places in all.)
+__device__ __forceinline__ uint32_t att_before(const AttendParams &P, uint32_t lead, int stop, int lane)
 {
     uint32_t sum = 0;
-    for (int b = lane; b < stop; b += 32) sum += static_cast<uint32_t>(att_units(att_len(P, b)));
+    for (int b = lane; b < stop; b += 32) {
+        const int len = att_len(P, b);
+        if (len >= 0) sum += static_cast<uint32_t>(att_units(len)) + lead;
+    }
     return __reduce_add_sync(0xffffffffu, sum);
 }
-// Units of one CTA's run.
-__device__ __forceinline__ uint32_t att_share(const AttendParams &P, uint32_t total)
+__device__ __forceinline__ AttCut att_cut(const AttendParams &P, uint32_t items, int lane)
 {
+    AttCut cut;
+    uint32_t sum = 0, used = 0;
+    for (int b = lane; b < P.batch; b += 32) {
+        const int len = att_len(P, b);
+        sum += static_cast<uint32_t>(att_units(len));
+        used += len >= 0;
+    }
+    sum = __reduce_add_sync(0xffffffffu, sum) * items;
+    used = __reduce_add_sync(0xffffffffu, used) * items;
     const uint32_t n = static_cast<uint32_t>(P.n_ctas);
-    return max(total / n + (total % n != 0u), 1u);
+    cut.lead = sum > n ? P.lead : 0u;                // (otherwise every unit has a CTA of its own)
+    cut.span = sum + cut.lead * used;
+    cut.per = max(cut.span / n + (cut.span % n != 0u), 1u);
+    return cut;
 }
 
-// Position in the cut: a sequence, its length and units, and the unit within its items.
-struct AttCursor { int b, len; uint32_t units, at; };
+// Position in the cut: a sequence, its length and places per item, and the place within its items.
+struct AttCursor { int b, len; uint32_t places, at; };
 
-// The sequence that holds unit `u` (in units of all items); u must be below the total.
-__device__ __forceinline__ AttCursor att_find(const AttendParams &P, uint32_t u, uint32_t items, int lane)
+// The sequence that holds place `u` (of all items); u must be below the span.
+__device__ __forceinline__ AttCursor att_find(const AttendParams &P, const AttCut &cut, uint32_t u, uint32_t items, int lane)
 {
     AttCursor c;
     uint32_t before = 0;
     for (int b0 = 0;; b0 += 32) {
         const int b = b0 + lane;
         const int len = b < P.batch ? att_len(P, b) : -1;
-        const uint32_t n = static_cast<uint32_t>(att_units(len));
+        const uint32_t n = len < 0 ? 0u : static_cast<uint32_t>(att_units(len)) + cut.lead;
         uint32_t incl = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -78,13 +99,28 @@ __device__ __forceinline__ AttCursor att_find(const AttendParams &P, uint32_t u,
         if (past || b0 + 32 >= P.batch) {
             const int who = past ? __ffs(past) - 1 : 31;
             c.b = b0 + who;
-            c.units = __shfl_sync(0xffffffffu, n, who);
+            c.places = __shfl_sync(0xffffffffu, n, who);
             c.len = __shfl_sync(0xffffffffu, len, who);
             c.at = u - (before + __shfl_sync(0xffffffffu, incl - n, who)) * items;
             return c;
         }
         before += __shfl_sync(0xffffffffu, incl, 31);
     }
+}
+
+// What a CTA has of the item its cursor stands in: units [k0, k1) of `units`, `places` of the cut in all; k1 <= 0: its
+// run ends before the item's first unit (which can only be the last item of a run).
+struct AttPiece { int item, units, k0, k1; uint32_t places; };
+__device__ __forceinline__ AttPiece att_piece(const AttCut &cut, const AttCursor &cur, uint32_t left)
+{
+    AttPiece x;
+    x.item = static_cast<int>(cur.at / cur.places);
+    const uint32_t from = cur.at - static_cast<uint32_t>(x.item) * cur.places;
+    x.places = left < cur.places - from ? left : cur.places - from;
+    x.units = static_cast<int>(cur.places - cut.lead);
+    x.k0 = max(static_cast<int>(from - cut.lead), 0);
+    x.k1 = static_cast<int>(from + x.places - cut.lead);
+    return x;
 }
 
 // ---- few rows: warp-level matrix instructions on codes that go from shared memory to registers
@@ -149,8 +185,8 @@ __device__ __forceinline__ float att_factor(float m, float l, float top) { retur
 // comes.  A weight may exceed 1 by 2^kNarrowSlack before the maximum is moved, so the sums are rescaled seldom and
 // the usual chunk needs one vote instead of reductions.
 //
-// Measured: 64 sequences of up to 8191 positions, 8 key heads, 4 query heads each: 92 us, 3.9 TB/s of the algorithm's bytes,
-// 0.60 of the measured copy bandwidth; 8 sequences of up to 2050 positions x 32 heads, 45 rows: 86 us. The 32-bit logic
+// Measured: 64 sequences of up to 8191 positions, 8 key heads, 4 query heads each: 91 us, 4.0 TB/s of the algorithm's bytes,
+// 0.61 of the measured copy bandwidth; 8 sequences of up to 2050 positions x 32 heads, 45 rows: 77 us. The 32-bit logic
 // pipe bounds it (52 % busy: an AND for every two codes and row block, a byte permutation and a shift for every
 // eight of the values), then the warps' own latencies; with queries as the long side (sixteen rows a block, a
 // maximum by shuffles in every chunk) the first took 165 us.
@@ -176,24 +212,24 @@ narrow_kernel(const __grid_constant__ AttendParams P)
     const int g = lane >> 2, t = lane & 3;
     const int ps = 1 << P.c.page_shift;
     const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
-    const uint32_t total = att_units_before(P, P.batch, lane) * items, per = att_share(P, total);
-    if (blockIdx.x > (total - 1) / per || total == 0) return;    // (runs of units before the last one are whole)
-    uint32_t u = blockIdx.x * per;
-    const uint32_t u_end = total - u < per ? total : u + per;
-    AttCursor cur = att_find(P, u, items, lane);
+    const AttCut cut = att_cut(P, items, lane);
+    if (cut.span == 0 || blockIdx.x > (cut.span - 1) / cut.per) return;    // (runs before the last one are whole)
+    uint32_t u = blockIdx.x * cut.per;
+    const uint32_t u_end = cut.span - u < cut.per ? cut.span : u + cut.per;
+    AttCursor cur = att_find(P, cut, u, items, lane);
     unsigned char *ring = s_ring + warp * STAGES * STAGE;
     auto kappa = [](int c) { return D == 128 ? c ^ ((c >> 1) & 1) : c ^ ((c >> 2) & 1); };
     auto swizzle = [](int row, int chunk) { return D == 128 ? chunk ^ ((row >> 1) & 2) : chunk; };
     const int kg = kappa(g), ka = kappa(2 * t), kb = kappa(2 * t + 1);
 
     while (u < u_end) {
-        const int item = static_cast<int>(cur.at / cur.units), units = static_cast<int>(cur.units);
-        const int k0 = static_cast<int>(cur.at - item * cur.units);
-        const int k1 = u_end - u < static_cast<uint32_t>(units - k0) ? k0 + static_cast<int>(u_end - u) : units;
-        const int b = cur.b, len = cur.len, head = item / P.n_blocks, block = item - head * P.n_blocks;
+        const AttPiece piece = att_piece(cut, cur, u_end - u);
+        if (piece.k1 <= 0) break;
+        const int k0 = piece.k0, k1 = piece.k1;
+        const int b = cur.b, len = cur.len, head = piece.item / P.n_blocks, block = piece.item - head * P.n_blocks;
         const int row0 = block * ROWS;
         const int prefix = P.prefix_len[b];
-        const bool whole = k0 == 0 && k1 == units;
+        const bool whole = k0 == 0 && k1 == piece.units;
 
         __syncthreads();                            // the shared memory of the item before is free
         // this warp's chunks: keys [128 k + 32 warp, + 32) for k = k0 .. k1 - 1, as far as there are keys
@@ -532,9 +568,9 @@ narrow_kernel(const __grid_constant__ AttendParams P)
                 if (c == 0) { part[ROWS * D + r] = m; part[ROWS * (D + 1) + r] = l; }
             }
         }
-        u += k1 - k0;
-        cur.at += k1 - k0;
-        if (u < u_end && cur.at >= cur.units * items) cur = att_find(P, u, items, lane);
+        u += piece.places;
+        cur.at += piece.places;
+        if (u < u_end && cur.at >= cur.places * items) cur = att_find(P, cut, u, items, lane);
     }
 }
 
@@ -548,9 +584,9 @@ join_kernel(const __grid_constant__ AttendParams P)
     const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
     const int b = static_cast<int>(blockIdx.x / items), item = static_cast<int>(blockIdx.x - b * items);
     const int len = att_len(P, b), units = att_units(len);
-    const uint32_t per = att_share(P, att_units_before(P, P.batch, lane) * items);
-    const uint32_t u0 = att_units_before(P, b, lane) * items + static_cast<uint32_t>(item) * units;
-    const int first = static_cast<int>(u0 / per), last = static_cast<int>((u0 + units - 1) / per);
+    const AttCut cut = att_cut(P, items, lane);
+    const uint32_t u0 = att_before(P, cut.lead, b, lane) * items + static_cast<uint32_t>(item) * (units + cut.lead) + cut.lead;   // its first unit
+    const int first = static_cast<int>(u0 / cut.per), last = static_cast<int>((u0 + units - 1) / cut.per);
     asm volatile("griddepcontrol.wait;" ::: "memory");   // (every thread: this kernel must not end before the one it follows)
     if (units == 0 || first == last) return;
     const int head = item / P.n_blocks, row0 = (item - head * P.n_blocks) * ROWS, r0 = blockIdx.y * 8;

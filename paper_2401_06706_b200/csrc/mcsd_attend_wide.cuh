@@ -113,10 +113,11 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 // the weights in half's range whatever the scales are; it moves only when it is exceeded by 2^kNarrowSlack.
 // Tensor memory (columns; all 512 are taken, so that the first is column 0): S of A, S of B (64 each), O of A, O of B (D
 // each), P of A, P of B (32 each), Q (D / 2).
-// Measured on 724 rows x 8 key heads x 4 sequences of up to 16001 positions: 299 us, 455 TFLOP/s, 0.28 of the measured
+// Measured on 724 rows x 8 key heads x 4 sequences of up to 16001 positions: 285 us, 477 TFLOP/s, 0.29 of the measured
 // peak. The products take about a fifth of the time; what bounds it is the chain of a softmax group for a unit (scores
 // read, exponentials, weights written: some 2000 cycles of two warps per scheduler) and the hand-overs around
-// it. Without the copies four units ahead it took 345 us, with products issued by a single thread 390 us. Left out: sixteen
+// it. With the work cut by units alone it took 297 us, without the copies four units ahead 345 us, with products issued by a
+// single thread 390 us. Left out: sixteen
 // softmax warps of sixteen rows in fragment layout (a quarter of the parameter loads, 322 us; 20 % slower than this
 // form on prefixes of 2000, where the tree's own units weigh more), separate rings for keys and values (328 us).
 template <int DT, int D>
@@ -174,23 +175,22 @@ wide_kernel(const __grid_constant__ AttendParams P)
 
     const int ps = 1 << P.c.page_shift;
     const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
-    const uint32_t total = att_units_before(P, P.batch, lane) * items, per = att_share(P, total);
-    const bool any = total != 0 && blockIdx.x <= (total - 1) / per;               // (runs of units before the last one are whole)
-    const uint32_t u_begin = any ? blockIdx.x * per : 0, u_end = any ? (total - u_begin < per ? total : u_begin + per) : 0;
+    const AttCut cut = att_cut(P, items, lane);
+    const bool any = cut.span != 0 && blockIdx.x <= (cut.span - 1) / cut.per;     // (runs before the last one are whole)
+    const uint32_t u_begin = any ? blockIdx.x * cut.per : 0, u_end = any ? (cut.span - u_begin < cut.per ? cut.span : u_begin + cut.per) : 0;
 
     // Every role goes over the same items; f(sequence, length, head, first row, first unit, last unit + 1, whole item).
     auto for_items = [&](auto f) {
         if (u_begin >= u_end) return;
-        AttCursor cur = att_find(P, u_begin, items, lane);
+        AttCursor cur = att_find(P, cut, u_begin, items, lane);
         for (uint32_t u = u_begin; u < u_end;) {
-            const int item = static_cast<int>(cur.at / cur.units), units = static_cast<int>(cur.units);
-            const int k0 = static_cast<int>(cur.at - item * cur.units);
-            const int k1 = u_end - u < static_cast<uint32_t>(units - k0) ? k0 + static_cast<int>(u_end - u) : units;
-            const int head = item / P.n_blocks;
-            f(cur.b, cur.len, head, (item - head * P.n_blocks) * kWideRows, k0, k1, k0 == 0 && k1 == units);
-            u += k1 - k0;
-            cur.at += k1 - k0;
-            if (u < u_end && cur.at >= cur.units * items) cur = att_find(P, u, items, lane);
+            const AttPiece piece = att_piece(cut, cur, u_end - u);
+            if (piece.k1 <= 0) break;
+            const int head = piece.item / P.n_blocks;
+            f(cur.b, cur.len, head, (piece.item - head * P.n_blocks) * kWideRows, piece.k0, piece.k1, piece.k0 == 0 && piece.k1 == piece.units);
+            u += piece.places;
+            cur.at += piece.places;
+            if (u < u_end && cur.at >= cur.places * items) cur = att_find(P, cut, u, items, lane);
         }
     };
 

@@ -184,6 +184,7 @@ int check_attention(const mcsd_attention_desc *d, const mcsd_kv_cache *cache)
 struct AttentionPlan {
     int rows;       // rows of a block
     int blocks;     // blocks per key/value head
+    int lead;       // places of the cut an item costs beside its units
     int ctas;       // CTAs the work is cut for: what is resident at once, or one per unit where a call cannot have more
 };
 AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *cache)
@@ -202,6 +203,9 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
     //   60     121 | 109                     96 | 87
     plan.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 24 ? 24 : rows <= 32 ? 16 : rows <= 48 ? 24 : kWideRows;
     plan.blocks = static_cast<int>((rows + plan.rows - 1) / plan.rows);
+    // Measured for 0, 1, 2, 3, 4, 6, 8 and 12 places an item: decoding is fastest with 2 or 3, blocks of 16 and 24 rows with 3 to 8,
+    // those of 128 rows with 4 to 6 for a tree of 45 nodes and 6 to 8 for one of 181 (its units see masks); 2 places off costs 2 %.
+    plan.lead = plan.rows == 8 ? 2 : plan.rows < kWideRows ? 4 : 4 + 2 * ((d->n_nodes + kAttUnit - 1) / kAttUnit);
     const long long units = (static_cast<long long>(d->max_pages) * cache->page_size + kAttUnit - 1) / kAttUnit;
     const long long most = static_cast<long long>(d->batch) * cache->n_heads * plan.blocks * (units > 0 ? units : 1);
     const long long resident = static_cast<long long>(plan.rows == 8 ? kNarrowCtas<1> : plan.rows == 16 ? kNarrowCtas<2> : plan.rows == 24 ? kNarrowCtas<3> : 1) * sms;
@@ -388,9 +392,9 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
         desc->workspace_bytes < mcsd_tree_attention_workspace_bytes(desc, cache))
         return MCSD_ERR_WORKSPACE;
     const AttentionPlan plan = attention_plan(desc, cache);
-    // (the cut counts units of all items in 32 bits)
+    // (the cut counts units of all items, and what stands for the items themselves, in 32 bits)
     if (static_cast<double>(desc->batch) * cache->n_heads * plan.blocks *
-            (static_cast<double>(desc->max_pages) * cache->page_size / kAttUnit + 2) > 4.2e9)
+            (static_cast<double>(desc->max_pages) * cache->page_size / kAttUnit + 2 + plan.lead) > 4.2e9)
         return MCSD_ERR_UNSUPPORTED;
     AttendParams p = {};
     p.c = cache_params(cache);
@@ -404,6 +408,7 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     p.n_rows = desc->n_nodes * p.group;
     p.n_blocks = plan.blocks;
     p.n_ctas = plan.ctas;
+    p.lead = static_cast<uint32_t>(plan.lead);
     p.part = static_cast<float *>(desc->workspace);
     p.q_vec = (reinterpret_cast<uintptr_t>(q) | 2ull * static_cast<unsigned long long>(desc->q_seq_stride | desc->q_node_stride |
                                                                                        desc->q_head_stride)) % 16 == 0;
