@@ -61,15 +61,18 @@ __device__ __forceinline__ RowWalk row_walk(const RowsParams &P)
 // 8 and stores one word of codes.  Rows of a token's heads follow each other in the thread order, so that
 // loads are contiguous (a page's rows of one head are 32 to 64 contiguous bytes each).  Bound by HBM: 2 D
 // numbers read and D + 8 bytes written per key/value row pair; a thread takes kRowsAhead tokens at a time, so
-// that their slots, and then their numbers, are in flight together.  Measured on 40001 tokens x 8 heads x 128 halves: 104 us
-// (0.30 of the measured copy bandwidth: some 200 instructions for the two rows of a warp are what bounds it), the way
-// back 59 us (0.54).
+// that their slots, and then their numbers, are in flight together.  Measured on 40001 tokens x 8 heads x 128 halves: 92 us
+// (0.34 of the measured copy bandwidth; the loads of a thread wait for one another, and some 150 instructions for the two rows
+// of a warp are the other half of it), the way back 53 us (0.60). Other numbers of tokens at a time: 4 take 94 us, 2 take 98, and
+// for the way back 2 take 55 us, 4 take 67; with a grid of eight CTAs per SM (not all resident) 106 and 68 us.
 // Scale, mid and codes are those of the definition in exact arithmetic: the two per-row numbers are formed
-// in double (by one of a row's threads), and where a float32 quotient lies within 2^-18 of a border between two codes
-// (two float32 roundings and a reciprocal good to 2^-23 put a number up to 8.5 off by 2^-18.9 at most) the thread's codes are decided in double; so no code depends on
+// in double (by one of a row's threads), and where x / scale - mid / scale in float32 lies within 2^-18 + |mid / scale| 2^-23
+// of a border between two codes (a reciprocal good to 2^-23 and the last rounding put a number up to 8.5 off by 2^-18.9 at most,
+// the rounding of mid / scale by |mid / scale| 2^-24) the thread's codes are decided in double; so no code depends on
 // how the compiler orders things.  Rounding to an integer is an addition of 1.5 2^23 (the conversion
 // instructions have a quarter of the rate).
-constexpr int kRowsAhead = 4;
+constexpr int kRowsAhead = 3;
+constexpr int kAppendCtas = 3, kReadCtas = 6;         // per SM: those that are resident, so that all end at about the same time
 
 // Extremes of a thread's 8 numbers, NaN if one is NaN.
 __device__ __forceinline__ float min_nan(float a, float b) { float d; asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
@@ -90,6 +93,8 @@ template <> struct Pair<MCSD_DTYPE_BF16> {
     static __device__ __forceinline__ T low_and_minus_high(T l, T h) { return __halves2bfloat162(__hmin_nan(__low2bfloat16(l), __high2bfloat16(l)), __hneg(__hmax_nan(__low2bfloat16(h), __high2bfloat16(h)))); }
 };
 
+__device__ __forceinline__ float rcp_approx(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
 // (scale, mid) of a row from its extremes; (0, NaN) if one of them is not finite.
 __device__ __forceinline__ uint32_t row_param(float lo, float hi)
 {
@@ -106,7 +111,7 @@ __device__ __forceinline__ uint32_t row_param(float lo, float hi)
 }
 
 template <int DT, int D, bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, kAppendCtas)
 append_kernel(const RowsParams P)
 {
     constexpr int TPR = D / 8;                      // threads of a row
@@ -173,32 +178,46 @@ append_kernel(const RowsParams P)
             }
             if (lane == u) { my_lo = lo; my_hi = hi; }
         }
-        const uint32_t mine = row_param(my_lo, my_hi);
+        // (the sign of the scale carries whether a number of the row may round beyond codes 0 to 15)
+        uint32_t mine = row_param(my_lo, my_hi);
+        {
+            const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&mine));
+            const float inv = rcp_approx(p.x);
+            if (!((my_hi - p.y) * inv < 7.4f && (my_lo - p.y) * inv > -8.4f)) mine |= 0x8000u;
+        }
 #pragma unroll
         for (int u = 0; u < kRowsAhead; ++u) {
-            const uint32_t both = __shfl_sync(group, mine, u, TPR);
+            const uint32_t flagged = __shfl_sync(group, mine, u, TPR), both = flagged & ~0x8000u;
             if (!codes[u]) continue;                // (the same for all threads of the row)
             const float2 p = __half22float2(*reinterpret_cast<const __half2 *>(&both));
             const float s = p.x, m = p.y;
-            float inv;
-            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));      // (unused where s is 0)
+            const float inv = rcp_approx(s), off = m * inv;         // (unused where s is 0)
             float x[8];
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) Elem<DT>::unpack(raw[u][i], x + i * (8 / kLoads));
-            constexpr float kRound = 12582912.f + 8.f;              // 1.5 2^23, and code 8 at 0
+            float2 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = fma2(make_float2(x[2 * i], x[2 * i + 1]), make_float2(inv, inv), make_float2(-off, -off));
+            if (flagged & 0x8000u) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    q[i].x = fminf(fmaxf(q[i].x, -8.f), 7.f);
+                    q[i].y = fminf(fmaxf(q[i].y, -8.f), 7.f);
+                }
+            }
+            constexpr float kRound = 12582912.f + 8.f;              // 1.5 2^23, and code 8 at 0: a sum's bits are 0x4b400000 + code
             uint32_t word = 0u;
             float far = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                float2 q = __fmul2_rn(add2(make_float2(x[i], x[i + 1]), make_float2(-m, -m)), make_float2(inv, inv));
-                q.x = fminf(fmaxf(q.x, -8.f), 7.f);
-                q.y = fminf(fmaxf(q.y, -8.f), 7.f);
-                const float2 t = add2(q, make_float2(kRound, kRound));
-                const float2 d = add2(q, make_float2(kRound - t.x, kRound - t.y));     // off the code (the difference is exact)
+            for (int i = 3; i >= 0; --i) {
+                const float2 t = add2(q[i], make_float2(kRound, kRound));
+                const float2 d = add2(q[i], make_float2(kRound - t.x, kRound - t.y));  // off the code (the difference is exact)
                 far = max3(far, fabsf(d.x), fabsf(d.y));
-                word |= (__float_as_uint(t.x) & 15u) << (4 * i) | (__float_as_uint(t.y) & 15u) << (4 * i + 4);
+                word = word * 16u + __float_as_uint(t.y);
+                word = word * 16u + __float_as_uint(t.x);
             }
-            if (far > 0.5f - 3.814697265625e-6f) {
+            word -= 0x4b400000u * 0x11111111u;
+            if (far > fmaf(fabsf(off), -1.1920929e-7f, 0.5f - 3.814697265625e-6f)) {
                 word = 0u;
 #pragma unroll 1
                 for (int i = 0; i < 8; ++i) {
@@ -217,7 +236,7 @@ append_kernel(const RowsParams P)
 
 // The way back, one thread per 8 numbers.
 template <int DT, int D, bool VEC>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, kReadCtas)
 read_kernel(const RowsParams P)
 {
     constexpr int TPR = D / 8;

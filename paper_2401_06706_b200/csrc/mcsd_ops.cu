@@ -101,7 +101,7 @@ int launch_rows(const RowsParams &p, bool vec, cudaStream_t st)
 {
     // A group of D / 8 threads per row (2 n_heads groups a token) while that fills the SMs, then several tokens a
     // group; a token at least.
-    const long long groups = 256 / (D / 8), rows = 2LL * p.c.n_heads, resident = static_cast<long long>(sm_count()) * 8;
+    const long long groups = 256 / (D / 8), rows = 2LL * p.c.n_heads, resident = static_cast<long long>(sm_count()) * (APPEND ? kAppendCtas : kReadCtas);
     if (resident <= 0) return MCSD_ERR_CUDA;
     const long long want = (p.n_tokens * rows + groups - 1) / groups, least = (rows + groups - 1) / groups;
     const long long cap = resident > least ? resident : least;
