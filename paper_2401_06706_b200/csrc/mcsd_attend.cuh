@@ -187,7 +187,7 @@ __device__ __forceinline__ float att_factor(float m, float l, float top) { retur
 //
 // Measured: 64 sequences of up to 8191 positions, 8 key heads, 4 query heads each: 91 us, 4.0 TB/s of the algorithm's bytes,
 // 0.61 of the measured copy bandwidth; 8 sequences of up to 2050 positions x 32 heads, 45 rows: 77 us. The 32-bit logic
-// pipe bounds it (52 % busy: an AND for every two codes and row block, a byte permutation and a shift for every
+// pipe bounds it (54 % busy: an AND for every two codes and row block, a byte permutation and a shift for every
 // eight of the values), then the warps' own latencies; with queries as the long side (sixteen rows a block, a
 // maximum by shuffles in every chunk) the first took 165 us.
 //

@@ -211,6 +211,15 @@ def test_strided_queries_outputs_and_tables():
         assert (big[..., D:] == 2).all()
 
 
+@pytest.mark.parametrize("parents", ["7x8x8", list(range(-1, 511))], ids=["wide", "chain"])
+def test_the_largest_trees(parents):
+    """512 nodes: three levels, and a chain (every mask word is used, tree positions fill several units)."""
+    parent, q, cache, table, prefix = _problem(23, 3, parents, 1, 1, 64, 16, [0, 100, 259], torch.float16)
+    assert len(parent) == 512
+    r = _run(q, cache, table, prefix, parent)
+    _check(q, cache, table, prefix, parent, r.out, r.lse)
+
+
 @pytest.mark.parametrize("kconfig,heads", [("", 2), ("4x2x2x1", 8)])
 def test_output_in_place_of_the_queries(kconfig, heads):
     """out may be q: a row of queries is read before its result is written, in whole and in divided items."""
