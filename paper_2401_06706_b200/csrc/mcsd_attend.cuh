@@ -126,6 +126,7 @@ __device__ __forceinline__ AttPiece att_piece(const AttCut &cut, const AttCursor
 // ---- few rows: warp-level matrix instructions on codes that go from shared memory to registers
 constexpr int kNarrowWarps = 4, kNarrowKeys = 32;
 constexpr float kNarrowSlack = 4.f, kNoTop = -3e38f;
+constexpr float kLeastLevel = -24.f;                // log2 of the smallest value scale
 template <int NB> constexpr int kNarrowRows = 8 * NB;                   // rows of a block
 template <int NB> constexpr int kNarrowStages = NB == 1 ? 3 : 4;
 template <int NB> constexpr int kNarrowCtas = NB == 1 ? 4 : NB == 2 ? 3 : 2;          // CTAs per SM
@@ -166,6 +167,10 @@ __device__ __forceinline__ void att_store(const AttendParams &P, int b, int head
         P.lse[(static_cast<long long>(b) * P.n_nodes + node) * P.n_heads + h] =
             l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
+__device__ __forceinline__ float lg2f(float x) { float r; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+// log2 of a value scale (a row without a range counts as the smallest scale, so that its probability stays in range; what is
+// not a scale at all, on a key that nobody sees, as well).
+__device__ __forceinline__ float att_level(float scale) { return fmaxf(lg2f(scale), kLeastLevel); }
 // Factor that brings a partial result with maximum m and sum l to the maximum `top`; a NaN sum stays one.
 __device__ __forceinline__ float att_factor(float m, float l, float top) { return l == l ? ex2f(m - top) : 1.f; }
 
@@ -181,12 +186,14 @@ __device__ __forceinline__ float att_factor(float m, float l, float top) { retur
 //   sum_j p_j v_j = sum_j (p_j vscale_j) c_j - 8 sum_j (p_j vscale_j) + sum_j p_j vmid_j
 // where p vscale is rounded to half once and both of its sums (the second by a matrix instruction with ones)
 // use the rounded weight; scores, maxima, sums and the rest are float32.  Q is scaled by a power of two per row so
-// that no type's range matters; value scales are taken relative to a power of two, raised when a larger one
-// comes.  A weight may exceed 1 by 2^kNarrowSlack before the maximum is moved, so the sums are rescaled seldom and
-// the usual chunk needs one vote instead of reductions.
+// that no type's range matters.  The reference of a row's exponents is the maximum of s_j + log2 vscale_j over the keys
+// that the row sees: its largest weight p vscale lies near 1, and half's range costs the others 2^-25 of that one at
+// most, whatever scales stand on keys that it does not see or hardly weighs (relative to the largest score and the largest scale
+// met, a loud value anywhere takes bits from all rows).  A weight may exceed 1 by 2^kNarrowSlack before the reference is moved,
+// so the sums are rescaled seldom and the usual chunk needs one vote instead of reductions.
 //
-// Measured: 64 sequences of up to 8191 positions, 8 key heads, 4 query heads each: 91 us, 4.0 TB/s of the algorithm's bytes,
-// 0.61 of the measured copy bandwidth; 8 sequences of up to 2050 positions x 32 heads, 45 rows: 77 us. The 32-bit logic
+// Measured: 64 sequences of up to 8191 positions, 8 key heads, 4 query heads each: 92 us, 3.9 TB/s of the algorithm's bytes,
+// 0.60 of the measured copy bandwidth; 8 sequences of up to 2050 positions x 32 heads, 45 rows: 77 us. The 32-bit logic
 // pipe bounds it (54 % busy: an AND for every two codes and row block, a byte permutation and a shift for every
 // eight of the values), then the warps' own latencies; with queries as the long side (sixteen rows a block, a
 // maximum by shuffles in every chunk) the first took 165 us.
@@ -344,8 +351,6 @@ narrow_kernel(const __grid_constant__ AttendParams P)
             top[nb][0] = top[nb][1] = kNoTop;
             sum[nb][0] = sum[nb][1] = mids[nb][0] = mids[nb][1] = 0.f;
         }
-        int expo = -100;                            // value scales are taken in units of 2^expo, unit = 2^-expo
-        float unit = exp2i(100.f);
 
         // One chunk; `plain`: every row sees every key of it.
         auto chunk = [&](auto plain_tag, const unsigned char *stage, int pos0, int valid) {
@@ -383,11 +388,11 @@ narrow_kernel(const __grid_constant__ AttendParams P)
             }
             const __half2 *kp = reinterpret_cast<const __half2 *>(stage + kNarrowKeys * D);
             const __half2 *vp = kp + kNarrowKeys;
-            float vs[2][2], vm[2][2], big = 0.f;
-            bool move = false;
+            float vs[2][2], vm[2][2];
+            float most[NB][2];                      // largest weight of each row among this lane's keys (-inf: it sees none of them), log2
             // scores in log2 units: element c of tile m is (key 16 m + 8 (c / 2) + kappa(g), row 2 t + c % 2)
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
+            for (int m = 0; m < 2; ++m) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const int key = 16 * m + 8 * x + kg;
@@ -406,34 +411,34 @@ narrow_kernel(const __grid_constant__ AttendParams P)
                         }
                     vs[m][x] = v.x;
                     vm[m][x] = v.y;
-                    big = fmaxf(big, v.x);
                 }
+                const float l0 = att_level(vs[m][0]), l1 = att_level(vs[m][1]);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const float2 w0 = add2(make_float2(s[nb][m][0], s[nb][m][1]), make_float2(l0, l0));
+                    const float2 w1 = add2(make_float2(s[nb][m][2], s[nb][m][3]), make_float2(l1, l1));
+                    most[nb][0] = m ? max3(most[nb][0], w0.x, w1.x) : fmaxf(w0.x, w1.x);
+                    most[nb][1] = m ? max3(most[nb][1], w0.y, w1.y) : fmaxf(w0.y, w1.y);
+                }
+            }
+            bool move = false;
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-                    move |= fmaxf(max3(s[nb][0][c], s[nb][0][2 + c], s[nb][1][c]), s[nb][1][2 + c]) > top[nb][c] + kNarrowSlack;
-            move |= big * unit > 1.f;
+                for (int c = 0; c < 2; ++c) move |= most[nb][c] > top[nb][c] + kNarrowSlack;
             if (__any_sync(0xffffffffu, move)) {
-                // (a scale is a half that is not negative: its float's bits are ordered like it)
-                const float most_scale = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(big)));
-                const int was = expo;
-                if (most_scale > 0.f) expo = max(expo, static_cast<int>(__float_as_uint(most_scale) >> 23) - 126);
-                unit = exp2i(static_cast<float>(-expo));
-                const float down = exp2i(static_cast<float>(was - expo));
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     float f[2];
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float now = fmaxf(max3(s[nb][0][c], s[nb][0][2 + c], s[nb][1][c]), fmaxf(s[nb][1][2 + c], top[nb][c]));
+                        float now = fmaxf(most[nb][c], top[nb][c]);
 #pragma unroll
                         for (int q = 4; q < 32; q <<= 1) now = fmaxf(now, __shfl_xor_sync(0xffffffffu, now, q));
                         f[c] = ex2f(top[nb][c] - now);
                         top[nb][c] = now;
                         sum[nb][c] *= f[c];
                         mids[nb][c] *= f[c];
-                        f[c] *= down;
                         ones[nb][c] *= f[c];
                     }
 #pragma unroll
@@ -445,7 +450,6 @@ narrow_kernel(const __grid_constant__ AttendParams P)
             for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const float scale = vs[m][x] * unit;
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
                         float w[2];
@@ -456,7 +460,7 @@ narrow_kernel(const __grid_constant__ AttendParams P)
                             sum[nb][c] += p;
                             // (the parameters of a key that is not seen may be anything)
                             if (plain || z != -INFINITY) mids[nb][c] = fmaf(p, vm[m][x], mids[nb][c]);
-                            w[c] = plain || z != -INFINITY ? p * scale : 0.f;
+                            w[c] = plain || z != -INFINITY ? p * vs[m][x] : 0.f;
                         }
                         pb[nb][m][x] = transpose8(half2_bits(w[0], w[1]));
                     }
@@ -516,7 +520,6 @@ narrow_kernel(const __grid_constant__ AttendParams P)
         __syncwarp();
         // this warp's result as numbers, into its own ring
         float *s_out = reinterpret_cast<float *>(ring);
-        const float back = exp2i(static_cast<float>(expo));
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -528,17 +531,17 @@ narrow_kernel(const __grid_constant__ AttendParams P)
                     z += __shfl_xor_sync(0xffffffffu, z, q);
                 }
                 const int row = nb * 8 + 2 * t + c;
-                const float fixed = fmaf(-8.f * back, ones[nb][c], z);
+                const float fixed = fmaf(-8.f, ones[nb][c], z);
                 float *dst = s_out + row * D + g * (D / 8);
 #pragma unroll
                 for (int x = 0; x < 2; ++x)         // the tile's rows g, then its rows g + 8
 #pragma unroll
                     for (int n = 0; n < MT; n += 4) {
                         float4 v;
-                        v.x = fmaf(o[nb][n][2 * x + c], back * 16777216.f, fixed);
-                        v.y = fmaf(o[nb][n + 1][2 * x + c], back * 1048576.f, fixed);
-                        v.z = fmaf(o[nb][n + 2][2 * x + c], back * 16777216.f, fixed);
-                        v.w = fmaf(o[nb][n + 3][2 * x + c], back * 1048576.f, fixed);
+                        v.x = fmaf(o[nb][n][2 * x + c], 16777216.f, fixed);
+                        v.y = fmaf(o[nb][n + 1][2 * x + c], 1048576.f, fixed);
+                        v.z = fmaf(o[nb][n + 2][2 * x + c], 16777216.f, fixed);
+                        v.w = fmaf(o[nb][n + 3][2 * x + c], 1048576.f, fixed);
                         *reinterpret_cast<float4 *>(dst + x * MT + n) = v;
                     }
                 if (g == 0) { s_top[warp][row] = top[nb][c]; s_sum[warp][row] = l; }

@@ -12,6 +12,7 @@ constexpr int kWideRows = 128;
 constexpr int kWideThreads = 640;                   // 8 softmax warps, 8 decoding warps, 2 that issue (and 2 beside them)
 constexpr int kWideStages = 2;                      // decoded units
 constexpr int kWideAhead = 4;                       // units whose codes are on their way to shared memory
+constexpr float kWideSpread = 4.f;                  // octaves of value scales that one number may stand for
 template <int D> constexpr int kWideTile = kAttUnit * D * 2;                       // bytes of a decoded tile of keys or values
 template <int D> constexpr int kWideSmem = 1024 + kWideStages * (2 * kWideTile<D> + kAttUnit * 16) + kWideAhead * kAttUnit * (D + 8) + kWideRows * (MCSD_MAX_NODES / 32) * 4;
 
@@ -109,11 +110,13 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 //                   maxima, sums and an O of its own, so that neither waits for the other: while one exponentiates, the
 //                   tensor cores work for the other. A joins both at the end of an item.
 // Scale and mid of a key enter the scores in float32; the weight p vscale is rounded to half once. The
-// reference of a row's exponents is its maximum plus the exponent of the largest value scale, which keeps
-// the weights in half's range whatever the scales are; it moves only when it is exceeded by 2^kNarrowSlack.
+// reference of a row's exponents follows its largest weight over the keys that it sees, as in the narrow kernel, and moves only when
+// it is exceeded by 2^kNarrowSlack. Where a row sees all keys of a unit and their value scales lie within 2^kWideSpread of each
+// other, the largest score plus the largest scale's log2 stands for that weight (one addition; 2^kWideSpread above it at most, which
+// half's range has room for); elsewhere it is formed key by key.
 // Tensor memory (columns; all 512 are taken, so that the first is column 0): S of A, S of B (64 each), O of A, O of B (D
 // each), P of A, P of B (32 each), Q (D / 2).
-// Measured on 724 rows x 8 key heads x 4 sequences of up to 16001 positions: 285 us, 477 TFLOP/s, 0.29 of the measured
+// Measured on 724 rows x 8 key heads x 4 sequences of up to 16001 positions: 282 us, 484 TFLOP/s, 0.29 of the measured
 // peak. The products take about a fifth of the time; what bounds it is the chain of a softmax group for a unit (scores
 // read, exponentials, weights written: some 2000 cycles of two warps per scheduler) and the hand-overs around
 // it. With the work cut by units alone it took 297 us, without the copies four units ahead 345 us, with products issued by a
@@ -131,7 +134,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
     __shared__ uint32_t s_tmem;
     __shared__ int s_dead;
     __shared__ uint32_t s_valid[kWideStages][4];    // keys of a stage that are there
-    __shared__ float s_big[kWideStages][4];         // largest value scale of 32 keys
+    __shared__ float2 s_level[kWideStages][4];      // log2 of the largest and of the smallest value scale of 32 keys
     __shared__ float4 s_other[kWideRows];           // reference and sums of group B at the end of an item
     __shared__ float2 s_row[kWideRows];             // of a row: log2 units per unit, and sum of q in accumulator units
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -285,8 +288,9 @@ wide_kernel(const __grid_constant__ AttendParams P)
                     const uint32_t keys = __ballot_sync(0xffffffffu, mine);
                     if (lane == 0) s_valid[stage][warp & 3] = keys;
                 } else {
-                    const float big = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(p.x)));  // (never negative)
-                    if (lane == 0) s_big[stage][warp & 3] = big;
+                    const float level = att_level(p.x);
+                    const float2 ends = make_float2(warp_max(level), -warp_max(-level));
+                    if (lane == 0) s_level[stage][warp & 3] = ends;
                 }
                 fence_proxy_async();
                 warp_arrive(b_full + 8 * stage, lane);
@@ -414,14 +418,14 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 rho = s_row[r].y;
             }
             float ref = kNoTop, sum = 0.f, mids = 0.f;
-            int expo = -30;                         // ref = maximum + expo, 2^expo at least the largest value scale
             for (int k = k0; k < k1; ++k, ++n) {
                 wide_wait(b_s + 8 * x, n & 1, dead);
                 wide_wait(b_full + 8 * stage, phase, dead);
                 tc_after_sync();
                 const float4 *par = s_param + stage * kAttUnit + 64 * x;       // two per pair of keys
                 const int pos0 = k * kAttUnit + 64 * x;
-                auto unit = [&](auto plain_tag, uint32_t see0, uint32_t see1) {           // see: keys this row sees
+                // see: keys this row sees; top: log2 of the largest value scale, where `plain`
+                auto unit = [&](auto plain_tag, uint32_t see0, uint32_t see1, float top) {
                     constexpr bool plain = decltype(plain_tag)::value;
                     float2 y[32];
                     float most = -INFINITY;
@@ -439,25 +443,24 @@ wide_kernel(const __grid_constant__ AttendParams P)
                             const float4 kp = par[2 * (16 * c + j)];
                             const float2 off = __fmul2_rn(make_float2(kp.z, kp.w), make_float2(rho, rho));
                             float2 z = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), make_float2(kp.x, kp.y), off);
-                            if (!plain) {
-                                if (!((see >> (2 * j)) & 1u)) z.x = -INFINITY;
-                                if (!((see >> (2 * j + 1)) & 1u)) z.y = -INFINITY;
+                            if (plain) {
+                                most = max3(most, z.x, z.y);
+                            } else {
+                                const float4 vp = par[2 * (16 * c + j) + 1];
+                                const float2 w = fma2(z, make_float2(ra, ra), make_float2(att_level(vp.x), att_level(vp.y)));
+                                if ((see >> (2 * j)) & 1u) most = fmaxf(most, w.x);
+                                if ((see >> (2 * j + 1)) & 1u) most = fmaxf(most, w.y);
                             }
-                            most = max3(most, z.x, z.y);
                             y[16 * c + j] = z;
                         }
                     }
                     // O and P belong to this group once the product of the unit before is done
                     if (n > 0) wide_wait(b_o + 8 * x, (n - 1) & 1, dead);
                     tc_after_sync();
-                    const float big = fmaxf(s_big[stage][2 * x], s_big[stage][2 * x + 1]);
-                    const float high = most > -INFINITY ? most * ra : -INFINITY;
-                    const bool move = high > ref - static_cast<float>(expo) + kNarrowSlack || (big > 0.f && static_cast<int>(__float_as_uint(big) >> 23) - 126 > expo);
-                    if (__any_sync(0xffffffffu, move)) {
-                        const float top = ref == kNoTop ? high : fmaxf(ref - static_cast<float>(expo), high);
-                        if (big > 0.f) expo = max(expo, static_cast<int>(__float_as_uint(big) >> 23) - 126);
-                        const float now = top == -INFINITY ? kNoTop : top + static_cast<float>(expo);
-                        const float f = ref == kNoTop ? 0.f : ex2f(ref - now);
+                    const float high = plain ? fmaf(most, ra, top) : most;
+                    if (__any_sync(0xffffffffu, high > ref + kNarrowSlack)) {
+                        const float now = fmaxf(ref, high);
+                        const float f = ex2f(ref - now);
                         ref = now;
                         sum *= f;
                         mids *= f;
@@ -501,8 +504,10 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 };
                 if (busy) {
                     uint32_t see0 = s_valid[stage][2 * x], see1 = s_valid[stage][2 * x + 1];
-                    if ((see0 & see1) == 0xffffffffu && pos0 + 64 <= prefix) {
-                        unit(std::true_type(), see0, see1);
+                    const float2 la = s_level[stage][2 * x], lb = s_level[stage][2 * x + 1];
+                    const float top = fmaxf(la.x, lb.x);
+                    if ((see0 & see1) == 0xffffffffu && pos0 + 64 <= prefix && top - fminf(la.y, lb.y) <= kWideSpread) {
+                        unit(std::true_type(), see0, see1, top);
                     } else {
                         // bits first .. first + 31 of the row's nodes, ones below 0 (wd is -1 for a negative first)
                         auto nodes = [&](int first) {
@@ -512,7 +517,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
                             const uint32_t hi = (wd + 1) * 32 < P.n_nodes ? s_seen[r][wd + 1] : 0u;
                             return __funnelshift_r(lo, hi, first & 31);
                         };
-                        unit(std::false_type(), see0 & nodes(pos0 - prefix), see1 & nodes(pos0 + 32 - prefix));
+                        unit(std::false_type(), see0 & nodes(pos0 - prefix), see1 & nodes(pos0 + 32 - prefix), top);
                     }
                 } else {
                     warp_arrive(b_read + 8 * x, lane);

@@ -323,3 +323,96 @@ def test_busy_batches(kconfig, heads, kv, D):
         back = lambda t: t.view(kv, N, G, -1).permute(1, 0, 2, 3).reshape(N, heads, -1)
         assert ((runs[0][0][b].double() - back(want)).abs() <= back(tol)).all()
         assert ((runs[0][1][b].double() - back(lse)[..., 0]).abs() <= back(ds + 2.0 ** -21 * lse.abs())[..., 0]).all()
+
+
+# ---------------------------------------------------------------- value scales far apart
+def _exact_rows(q, cache, table, prefix, parent, b, scale):
+    """(out, lse, tolerance of out, of lse) of one sequence in 64 bits on the device, [N, heads, ..].
+
+    Counted: the final rounding (half a step); a weight p vscale rounded to half (2^-11 of it, times the distance of its code
+    from the middle) or, where it is a subnormal half, 2^-25 of the reference, which lies at most two octaves above the largest
+    weight of the row (the scales of the keys but the loud ones lie within a factor of four: asserted), times a code of 8; the
+    float32 scores (D 2^-24 of their parts, and 2^-19 for the exponential), which count twice in a quotient, and sums of n terms
+    (n 2^-24)."""
+    D, ps, N, heads, kv = cache.head_dim, cache.page_size, q.shape[1], q.shape[2], cache.n_heads
+    n = int(prefix[b]) + N
+    pos = torch.arange(n, device="cuda")
+    page, row, half = table[b, pos // ps].long(), pos % ps, ps * D // 2
+    par = cache.pages[:, :, 2 * half:].contiguous().view(torch.float16).view(-1, kv, 2, ps, 2)[page, :, :, row].double()   # [n, kv, which, (scale, mid)]
+    k, v = (t.double().transpose(0, 1) for t in binding.mcsd_read_kv(cache, page * ps + row))           # [kv, n, D]
+    ks, km, vs, vm = (par[:, :, w, c].T for w in (0, 1) for c in (0, 1))                                # [kv, n]
+    quiet = vs[vs < 10]
+    assert quiet.max() <= 4 * quiet.min()
+    seen = torch.ones((N, n), dtype=torch.bool, device="cuda")
+    seen[:, int(prefix[b]):] = torch.tensor([[m in ref.path(parent, i) for m in range(N)] for i in range(N)], device="cuda")
+    g = torch.arange(heads, device="cuda") // (heads // kv)
+    s = torch.einsum("nhd,hkd->nhk", q[b].double(), k[g]) * scale
+    s = s.masked_fill(~seen[:, None], float("-inf"))
+    lse = torch.logsumexp(s, -1)
+    p = torch.exp(s - lse[..., None])
+    out = torch.einsum("nhk,hkd->nhd", p, v[g])
+    # (the parts of a score: of the keys that the row sees)
+    part = torch.where(seen[:, None], (km.abs() + 15 * ks)[g][None], 0.0).amax(-1) * q[b].double().abs().sum(-1) * abs(scale)
+    ds = D * 2.0 ** -24 * part + 2.0 ** -19
+    tol = (torch.finfo(q.dtype).eps / 2 * out.abs() + 2.0 ** -11 * torch.einsum("nhk,hkd->nhd", p, (v - vm[..., None]).abs()[g])
+           + (8 * n * 2.0 ** -23 * (p * vs[g][None]).amax(-1) + (p * (vm.abs() + 8 * vs)[g][None]).sum(-1) * (2 * ds + n * 2.0 ** -24))[..., None])
+    return out, lse, tol, ds + 2.0 ** -21 * lse.abs() + n * 2.0 ** -24
+
+
+BLOCKS = [("2", 2, 1), ("2", 5, 1), ("2", 8, 1), ("4x2x2x1", 1, 1), ("4x2x2x1", 8, 2), ("4x4x2x2x1", 1, 1)]     # blocks of 8, 16, 24, 24, 128, 128 rows
+
+
+def _even_weights(seed, kconfig, heads, kv, D, prefixes):
+    """A problem in which an error of the small weights adds up: every position has the same value row, one position in 32 a score
+    some 5.5 above all others, which have the same key row. (The queries lean the way of the keys.)"""
+    parent, q, cache, table, prefix = _problem(seed, len(prefixes), kconfig, heads, kv, D, 16, prefixes, torch.float16)
+    g = torch.Generator().manual_seed(seed)
+    way = torch.randn((D,), generator=g)
+    way *= D ** 0.5 / way.norm()
+    q.copy_((way + 0.1 * torch.randn(q.shape, generator=g)).to(q))
+    value = torch.randn((1, kv, D), generator=g)
+    for b, n in enumerate(prefixes):
+        pos = torch.arange(n + len(parent))
+        keys = torch.where(pos[:, None, None] % 32 == 7, 5.5 * D ** -0.5 * way, 0.0 * way).expand(-1, kv, D)
+        binding.mcsd_append_kv(cache, keys.contiguous().cuda(), value.expand(len(pos), kv, D).contiguous().cuda(), _slots(table, b, pos))
+    return parent, q, cache, table, prefix, way
+
+
+def _slots(table, b, pos):
+    return table[b, pos.cuda() // 16].long() * 16 + pos.cuda() % 16
+
+
+@pytest.mark.parametrize("loud", [8e3, 5e4])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kconfig,heads,kv", BLOCKS)
+def test_a_loud_value_on_another_branch_takes_no_bits(kconfig, heads, kv, D, loud):
+    """One node's value row is thousands of times larger than all others: the rows that do not see it are as exact as without it."""
+    parent, q, cache, table, prefix, _ = _even_weights(31, kconfig, heads, kv, D, [200, 20, 333])
+    node = 2
+    row = torch.rand((1, kv, D), generator=torch.Generator().manual_seed(5)).cuda() * loud
+    for b in range(3):
+        binding.mcsd_append_kv(cache, torch.zeros((1, kv, D), device="cuda"), row, _slots(table, b, prefix[b:b + 1] + node))
+    r = _run(q, cache, table, prefix, parent)
+    blind = torch.tensor([node not in ref.path(parent, n) for n in range(len(parent))], device="cuda")
+    for b in range(3):
+        out, lse, tol, tol_lse = _exact_rows(q, cache, table, prefix, parent, b, D ** -0.5)
+        assert ((r.out[b].double() - out).abs() <= tol)[blind].all(), ((r.out[b].double() - out).abs() / tol)[blind].max()
+        assert ((r.lse[b].double() - lse).abs() <= tol_lse).all()
+
+
+@pytest.mark.parametrize("loud", [8e3, 5e4])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kconfig,heads,kv", [("", 4, 1)] + BLOCKS)
+def test_a_loud_value_of_small_weight_takes_no_bits(kconfig, heads, kv, D, loud):
+    """Some rows of the prefix have values thousands of times larger than the others' and scores so low that they do not
+    count: the output is as exact as without them."""
+    parent, q, cache, table, prefix, way = _even_weights(32, kconfig, heads, kv, D, [900, 130])
+    g = torch.Generator().manual_seed(6)
+    for b, at in ((0, [3, 64, 500, 501, 899]), (1, [0, 129])):
+        keys = (-40 * D ** -0.5 * way).expand(len(at), kv, D).contiguous()
+        binding.mcsd_append_kv(cache, keys.cuda(), loud * torch.rand((len(at), kv, D), generator=g).cuda(), _slots(table, b, torch.tensor(at)))
+    r = _run(q, cache, table, prefix, parent)
+    for b in range(2):
+        out, lse, tol, tol_lse = _exact_rows(q, cache, table, prefix, parent, b, D ** -0.5)
+        assert ((r.out[b].double() - out).abs() <= tol).all(), ((r.out[b].double() - out).abs() / tol).max()
+        assert ((r.lse[b].double() - lse).abs() <= tol_lse).all()
