@@ -88,8 +88,8 @@ template <int DT>
 int launch_rules(const RulesParams &p, dim3 grid, size_t smem, bool vec, cudaStream_t st)
 {
     void (*kernel)(const RulesParams) = vec ? rules_kernel<DT, true> : rules_kernel<DT, false>;
-    if (smem > 48 * 1024 &&                         // (trees some hundred levels deep)
-        !allow_smem(kernel, static_cast<int>(smem)))
+    // (trees some hundred levels deep; the kernel's own static part counts against the default of 48 KB as well)
+    if (smem > 40000 && !allow_smem(kernel, static_cast<int>(smem)))
         return MCSD_ERR_CUDA;
     kernel<<<grid, kRulesThreads, smem, st>>>(p);
     return launched(1);

@@ -208,3 +208,19 @@ def test_empty_calls():
     before = x["logits"].clone()
     binding.mcsd_apply_logit_rules(x["logits"], parent, cand, _rules(x), node_begin=1, node_end=1)
     assert torch.equal(before, x["logits"]) and binding.mcsd_last_launch_count() == 0
+
+
+@pytest.mark.parametrize("nodes,depth", [(448, 416), (447, 416), (448, 417), (512, 511)])
+def test_the_deepest_trees_in_the_widest_slice(nodes, depth):
+    """Shared memory of a call right at, below and above the default limit: 448 nodes, 416 levels and slices of 2048 tokens take
+    48 KB of it beside the kernel's static part."""
+    parent = np.concatenate([np.arange(-1, depth), np.full(nodes - depth - 1, depth - 1)]).astype(np.int32)   # a chain, the rest below its end
+    assert len(parent) == nodes
+    V, B, rows = 65536, 10, 3
+    g = torch.Generator().manual_seed(nodes)
+    x = {"logits": torch.randn((B, rows, V), generator=g).cuda(), "presence": torch.rand((B,), generator=g).cuda()}
+    cand = torch.randint(0, V, (B, nodes), generator=g, dtype=torch.int32).cuda()
+    cand[:, 2] = cand[:, 1]
+    want, size, _ = _reference(parent, x, cand)
+    got = binding.mcsd_apply_logit_rules(x["logits"], parent, cand, _rules(x), out=torch.empty_like(x["logits"]))
+    _close(got, want, size, torch.float32)
