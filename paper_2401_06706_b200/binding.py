@@ -746,7 +746,8 @@ class TreeAttention:
         d.max_pages, d.ld_table = self.max_pages, self.max_pages
         d.q_seq_stride, d.q_node_stride, d.q_head_stride = self.out.stride()[:3]
         d.out_seq_stride, d.out_node_stride, d.out_head_stride = self.out.stride()[:3]
-        ws = int(self.lib.mcsd_tree_attention_workspace_bytes(ctypes.byref(d), ctypes.byref(cache.desc)))
+        with _on_device(self.device):                # (the size goes by the device that the calls will run on)
+            ws = int(self.lib.mcsd_tree_attention_workspace_bytes(ctypes.byref(d), ctypes.byref(cache.desc)))
         if ws == 0:
             _check(self.lib.mcsd_tree_attention(ctypes.byref(d), ctypes.byref(cache.desc), None, None, self.parent.ctypes.data,
                                                 None, None, None))

@@ -2,9 +2,11 @@
 enqueued (fake pointers are never used), and the plain statements they are tested against hold by hand."""
 import ctypes
 import os
+import types
 
 import numpy as np
 import pytest
+import torch
 
 import ops_reference as ref
 from paper_2401_06706_b200 import binding, build, synth
@@ -105,6 +107,36 @@ def test_attention_refuses_missing_pointers_and_bad_trees(lib):
     assert lib.mcsd_tree_attention_workspace_bytes(None, ctypes.byref(c)) == 0
     d.n_heads = 3
     assert lib.mcsd_tree_attention_workspace_bytes(ctypes.byref(d), ctypes.byref(c)) == 0
+
+
+def test_attention_workspace_is_sized_on_the_device_of_the_cache(lib, monkeypatch):
+    """Its size depends on the device's multiprocessors, so the query runs where the calls will run, whatever is current."""
+    where, asked = [], []
+
+    class Guard:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            where.append(self.device)
+
+        def __exit__(self, *exc):
+            where.pop()
+
+    class Lib:
+        def __getattr__(self, name):
+            return getattr(lib, name)
+
+        def mcsd_tree_attention_workspace_bytes(self, d, c):
+            asked.append(list(where))
+            return lib.mcsd_tree_attention_workspace_bytes(d, c)
+
+    monkeypatch.setattr(binding, "_on_device", Guard)
+    monkeypatch.setattr(binding, "load_library", lambda path=None: Lib())
+    cpu = torch.device("cpu")                        # (stands for the device of the cache)
+    cache = types.SimpleNamespace(device=cpu, head_dim=128, page_size=16, n_heads=2, desc=_cache())
+    att = binding.TreeAttention(2, synth.tree_from_kconfig([2]), 4, torch.bfloat16, cache, 8)
+    assert asked == [[cpu]] and where == []
 
 
 def _page_desc(**kw):
