@@ -138,6 +138,10 @@ rules_kernel(const __grid_constant__ RulesParams P)
         if (m >= 0 && m < P.n_masks) mask = P.masks + m * P.ld_mask + (x0 >> 5);
         else if (m >= 0 && P.status && blockIdx.x == 0 && lane == 0) atomicOr(&P.status[b], MCSD_STATUS_BAD_MASK);
         auto allowed = [&](int i) { return !mask || ((__ldg(mask + (i >> 5)) >> (i & 31)) & 1u); };
+        auto mask_one = [&](int i) {
+            if (!allowed(i)) store_elem<DT>(dst, i, -INFINITY);
+            else if (!P.in_place) store_elem<DT>(dst, i, load_elem<DT>(src, i));
+        };
         // the path: lane i the i-th ancestor, root excluded
         int length = 0;
         if (penalise && P.cand) {
@@ -204,9 +208,9 @@ rules_kernel(const __grid_constant__ RulesParams P)
                     }
                 }
             const int i = n_vec * VE + lane;         // the last tokens of the vocabulary, one by one
-            if (i < n_el) store_elem<DT>(dst, i, allowed(i) ? load_elem<DT>(src, i) : -INFINITY);
-        } else {
-            for (int i = lane; i < n_el; i += 32) store_elem<DT>(dst, i, allowed(i) ? load_elem<DT>(src, i) : -INFINITY);
+            if (i < n_el) mask_one(i);
+        } else if (!P.in_place || mask) {
+            for (int i = lane; i < n_el; i += 32) mask_one(i);
         }
         __syncwarp();
         // the tokens some rule concerns

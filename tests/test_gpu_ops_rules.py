@@ -224,3 +224,34 @@ def test_the_deepest_trees_in_the_widest_slice(nodes, depth):
     want, size, _ = _reference(parent, x, cand)
     got = binding.mcsd_apply_logit_rules(x["logits"], parent, cand, _rules(x), out=torch.empty_like(x["logits"]))
     _close(got, want, size, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("V", [701, 704])
+@pytest.mark.parametrize("mask", [False, True])
+def test_in_place_leaves_what_no_rule_concerns(dtype, V, mask):
+    """Bit by bit, NaN payloads too, on rows that are read element by element (701) and by vectors with a ragged end."""
+    dt = DTYPES[dtype]
+    g = torch.Generator().manual_seed(V)
+    bits = torch.int32 if dt == torch.float32 else torch.int16
+    x = torch.randn((2, 3, V), generator=g).to(dt)
+    nan = torch.tensor(0x7f812345, dtype=torch.int32).view(torch.float32) if dt == torch.float32 else torch.tensor({"bf16": 0x7f91, "fp16": 0x7d23}[dtype], dtype=torch.int16).view(dt)
+    x.view(bits)[:, :, ::7] = nan.view(bits)
+    x = x.cuda()
+    ids = torch.tensor([[3, 700], [5, -1]], dtype=torch.int32, device="cuda")
+    kw = dict(bias_ids=ids, bias_values=torch.ones((2, 2), device="cuda"))
+    hidden = torch.zeros(V, dtype=torch.bool, device="cuda")
+    if mask:
+        hidden[[2, 64, 698]] = True
+        words = torch.full(((V + 31) // 32,), -1, dtype=torch.int64)
+        for i in (2, 64, 698):
+            words[i // 32] -= 1 << (i % 32)          # (from all ones: the bit goes out)
+        kw |= dict(masks=words.to(torch.int32)[None].cuda(), mask_index=torch.zeros((2, 3), dtype=torch.int32, device="cuda"))
+    before = x.view(bits).clone()
+    binding.mcsd_apply_logit_rules(x, _tree("2"), None, binding.LogitRules(**kw))
+    touched = hidden.expand(2, V).clone()
+    for b in range(2):
+        touched[b, [int(i) for i in ids[b] if i >= 0]] = True
+    same = x.view(bits) == before
+    assert same[~touched[:, None].expand(2, 3, V)].all()
+    assert torch.isneginf(x[:, :, hidden]).all() and (x[1, :, 5] == before.view(dt)[1, :, 5] + 1).all()
