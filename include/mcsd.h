@@ -124,10 +124,13 @@ extern "C" {
 #define MCSD_OPT_EPT 1           /* vocabulary elements per thread and row of the node kernel         */
 #define MCSD_OPT_DIRECT 2        /* 1: plain element loads even where rows are 16-byte aligned        */
 #define MCSD_OPT_SAMPLE_AHEAD 3  /* L2 look-ahead of the sampling kernel, percent of its default (100) */
-#define MCSD_OPT_WAIT_POLLS 4    /* poll budget of the node kernel's exchange wait (0: about 2 s)     */
+#define MCSD_OPT_WAIT_POLLS 4    /* poll budget of the node kernel's exchange wait, and of the waits of the tree
+                                    attention's kernel for many rows (0: about 2 s)                  */
 #define MCSD_OPT_TEST_EXTRA_TX 5 /* test of the expiry path only: the exchange barrier of every round
                                     expects this many bytes (a multiple of 16) that nobody sends, so
-                                    the bounded wait runs out and MCSD_STATUS_TIMEOUT is reported      */
+                                    the bounded wait runs out and MCSD_STATUS_TIMEOUT is reported; a
+                                    barrier of the tree attention's kernel for many rows expects an
+                                    arrival that never comes, and the rows are NaN                     */
 #define MCSD_OPT_PDL 6           /* 1 (default): the walk stage is launched as a programmatic dependent
                                     of the node stage; 0: plain stream order                         */
 #define MCSD_OPT_TEST_SHRINK_RANGES 7 /* checked build only, test of the checker: every registered extent is

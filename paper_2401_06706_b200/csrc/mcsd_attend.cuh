@@ -26,6 +26,8 @@ struct AttendParams {
     uint32_t lead;                                  // places of the cut an item costs beside its units
     int32_t q_vec, o_vec;                           // rows of q may be read, those of out written in 16-byte vectors
     float scale;
+    uint32_t wait_polls;                            // poll budget of the bounded waits (kWaitPolls unless a test shortens it)
+    uint32_t test_extra;                            // 0; a test of the expiry path has a barrier wait for this many more arrivals
     int16_t parent[MCSD_MAX_NODES];
 };
 

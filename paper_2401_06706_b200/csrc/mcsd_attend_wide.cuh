@@ -84,13 +84,13 @@ template <int N> __device__ __forceinline__ void regs_up() { asm volatile("setma
 template <int N> __device__ __forceinline__ void regs_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // Bounded wait of a warp of the roles below (every poll may suspend it for a microsecond, so the bound is a few
-// seconds).  Once one has given up every wait returns at once: the roles run to their end, whatever they compute, nobody
+// seconds unless a test shortens it).  Once one has given up every wait returns at once: the roles run to their end, whatever they compute, nobody
 // is left waiting, and the rows are written as NaN.
-__device__ __forceinline__ void wide_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
-    for (uint32_t i = 0; i < kWaitPolls; ++i) {
+__device__ __forceinline__ void wide_wait(uint32_t bar, uint32_t parity, volatile int *dead, uint32_t polls) {
+    for (uint32_t i = 0; i < polls; ++i) {
         if (mbar_try_wait(bar, parity)) break;
         if ((i & 31) == 31 && *dead) break;
-        if (i == kWaitPolls - 1) *dead = 1;
+        if (i == polls - 1) *dead = 1;
     }
     __syncwarp();
 }
@@ -116,7 +116,7 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 // half's range has room for); elsewhere it is formed key by key.
 // Tensor memory (columns; all 512 are taken, so that the first is column 0): S of A, S of B (64 each), O of A, O of B (D
 // each), P of A, P of B (32 each), Q (D / 2).
-// Measured on 724 rows x 8 key heads x 4 sequences of up to 16001 positions: 282 us, 484 TFLOP/s, 0.29 of the measured
+// Measured on 724 rows x 8 key heads x 4 sequences of up to 16001 positions: 283 us, 482 TFLOP/s, 0.29 of the measured
 // peak. The products take about a fifth of the time; what bounds it is the chain of a softmax group for a unit (scores
 // read, exponentials, weights written: some 2000 cycles of two warps per scheduler) and the hand-overs around
 // it. With the work cut by units alone it took 297 us, without the copies four units ahead 345 us, with products issued by a
@@ -161,7 +161,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
             mbar_init(b_p + 8 * i, 4);
             mbar_init(b_o + 8 * i, 1);
         }
-        mbar_init(b_ready, 4);
+        mbar_init(b_ready, 4 + P.test_extra);       // (0 but in a test of the expiry path: arrivals that never come)
         mbar_init(b_free, 4);
         mbar_init(b_merge, 4);
         mbar_init(b_end, 2);
@@ -251,7 +251,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
             for (; k < k1; ++k) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(kWideAhead - 1) : "memory");
                 const unsigned char *from = ring + slot * 32 * (RB + 4);
-                wide_wait(b_empty + 8 * stage, phase, dead);
+                wide_wait(b_empty + 8 * stage, phase, dead, P.wait_polls);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {      // 16 bytes of codes are four 16-byte chunks of operands
                     const int key = key0 + (i / (CH / 2)) * 16 + (i % (CH / 2)) * (32 / CH) + lane / CH;
@@ -308,7 +308,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
             int stage = 0;
             uint32_t phase = 0, n = 0, it = 0;      // n: units so far
             auto scores = [&](int stage, uint32_t phase) {
-                wide_wait(b_full + 8 * stage, phase, dead);
+                wide_wait(b_full + 8 * stage, phase, dead, P.wait_polls);
                 tc_after_sync();
                 const uint32_t at = tc_operand(smem_u32(s_tiles) + stage * 2 * TILE + x * 64 * 128, 16);
 #pragma unroll
@@ -317,16 +317,16 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 tc_commit(b_s + 8 * x);
             };
             for_items([&](int, int, int, int, int k0, int k1, bool) {
-                wide_wait(b_ready, it & 1, dead);
+                wide_wait(b_ready, it & 1, dead, P.wait_polls);
                 scores(stage, phase);
                 for (int k = k0; k < k1; ++k, ++n) {
                     const int here = stage;
                     if (++stage == kWideStages) { stage = 0; phase ^= 1; }
                     if (k + 1 < k1) {               // the group has read the scores of this unit: those of the next
-                        wide_wait(b_read + 8 * x, n & 1, dead);
+                        wide_wait(b_read + 8 * x, n & 1, dead, P.wait_polls);
                         scores(stage, phase);
                     }
-                    wide_wait(b_p + 8 * x, n & 1, dead);          // its weights are written
+                    wide_wait(b_p + 8 * x, n & 1, dead, P.wait_polls);          // its weights are written
                     tc_after_sync();
                     const uint32_t at = tc_operand(smem_u32(s_tiles) + (here * 2 + 1) * TILE + x * 64 * 128, kAttUnit * 128);
 #pragma unroll
@@ -337,11 +337,10 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 }
                 ++it;
             });
-            // (after an expired wait what was issued ends before its memory is given back)
-            if (__any_sync(0xffffffffu, *dead)) {
-                tc_commit(b_end);
-                for (uint32_t i = 0; i < kWaitPolls && !__all_sync(0xffffffffu, mbar_try_wait(b_end, 0)); ++i) {}
-            }
+            // What was issued, by both warps, ends before its memory is given back. (Where no wait expires, the softmax groups have
+            // waited for the products already; where one does, it may be the last of all, after this warp is through.)
+            tc_commit(b_end);
+            for (uint32_t i = 0; i < kWaitPolls && !__all_sync(0xffffffffu, mbar_try_wait(b_end, 0)); ++i) {}
         }
     } else {
         // ------------------------------------------------------------ softmax
@@ -413,14 +412,14 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 tc_before_sync();
                 warp_arrive(b_ready, lane);
             } else {
-                wide_wait(b_ready, it & 1, dead);
+                wide_wait(b_ready, it & 1, dead, P.wait_polls);
                 ra = s_row[r].x;
                 rho = s_row[r].y;
             }
             float ref = kNoTop, sum = 0.f, mids = 0.f;
             for (int k = k0; k < k1; ++k, ++n) {
-                wide_wait(b_s + 8 * x, n & 1, dead);
-                wide_wait(b_full + 8 * stage, phase, dead);
+                wide_wait(b_s + 8 * x, n & 1, dead, P.wait_polls);
+                wide_wait(b_full + 8 * stage, phase, dead, P.wait_polls);
                 tc_after_sync();
                 const float4 *par = s_param + stage * kAttUnit + 64 * x;       // two per pair of keys
                 const int pos0 = k * kAttUnit + 64 * x;
@@ -455,7 +454,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
                         }
                     }
                     // O and P belong to this group once the product of the unit before is done
-                    if (n > 0) wide_wait(b_o + 8 * x, (n - 1) & 1, dead);
+                    if (n > 0) wide_wait(b_o + 8 * x, (n - 1) & 1, dead, P.wait_polls);
                     tc_after_sync();
                     const float high = plain ? fmaf(most, ra, top) : most;
                     if (__any_sync(0xffffffffu, high > ref + kNarrowSlack)) {
@@ -522,16 +521,16 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 } else {
                     warp_arrive(b_read + 8 * x, lane);
                     // (no rows, but no running ahead either: an arrival must not count for a unit that others are still at)
-                    if (n > 0) wide_wait(b_o + 8 * x, (n - 1) & 1, dead);
+                    if (n > 0) wide_wait(b_o + 8 * x, (n - 1) & 1, dead, P.wait_polls);
                 }
-                if (x == 1 && k == k0 && it > 0) wide_wait(b_free, (it - 1) & 1, dead);   // A has read O of the item before
+                if (x == 1 && k == k0 && it > 0) wide_wait(b_free, (it - 1) & 1, dead, P.wait_polls);   // A has read O of the item before
                 tc_before_sync();
                 warp_arrive(b_p + 8 * x, lane);
                 warp_arrive(b_empty + 8 * stage, lane);           // the parameters are read
                 if (++stage == kWideStages) { stage = 0; phase ^= 1; }
             }
             // ---- the end of the item: B hands its rows to A
-            wide_wait(b_o + 8 * x, (n - 1) & 1, dead);
+            wide_wait(b_o + 8 * x, (n - 1) & 1, dead, P.wait_polls);
             tc_after_sync();
             if (x == 1) {
                 // (s_other is free: A has passed b_free for the item before, see above)
@@ -539,7 +538,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 tc_before_sync();
                 warp_arrive(b_merge, lane);
             } else {
-                wide_wait(b_merge, it & 1, dead);
+                wide_wait(b_merge, it & 1, dead, P.wait_polls);
                 tc_after_sync();
                 if (busy) {
                     const float4 other = s_other[r];
