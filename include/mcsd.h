@@ -99,7 +99,7 @@ extern "C" {
 #define MCSD_ERR_MODE (-4)
 #define MCSD_ERR_TEMPERATURE (-5) /* negative, NaN or infinite                        */
 #define MCSD_ERR_TREE (-6)        /* tree_parent breaks the layout contract           */
-#define MCSD_ERR_STRIDE (-7)      /* row stride smaller than vocab                    */
+#define MCSD_ERR_STRIDE (-7)      /* stride too small, or off its alignment (arrays too) */
 #define MCSD_ERR_WORKSPACE (-8)   /* workspace missing, misaligned or too small       */
 #define MCSD_ERR_CUDA (-9)        /* a CUDA runtime call or kernel launch failed      */
 #define MCSD_ERR_UNSUPPORTED (-10)/* beyond MCSD_MAX_*                                */
@@ -475,6 +475,7 @@ int mcsd_shard_commit(const mcsd_shard_desc *desc, const int32_t *tree_parent, c
  * the key/value cache, the cache in 4 bits, attention of a draft tree over it, and the move of the
  * accepted rows inside it.  As above: nothing is allocated, all work is enqueued on the given stream,
  * an error code means that nothing was enqueued, and every call can be captured in a CUDA graph.
+ * Device arrays lie on multiples of their elements' size (MCSD_ERR_STRIDE otherwise).
  */
 
 /*

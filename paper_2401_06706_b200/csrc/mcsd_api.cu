@@ -846,7 +846,7 @@ const char *mcsd_status_string(int code)
     case MCSD_ERR_MODE: return "unknown replacement mode";
     case MCSD_ERR_TEMPERATURE: return "temperature is negative, NaN or infinite";
     case MCSD_ERR_TREE: return "tree_parent breaks the layout contract";
-    case MCSD_ERR_STRIDE: return "row stride smaller than vocab";
+    case MCSD_ERR_STRIDE: return "a stride too small (a row stride below the vocabulary), or a stride or array off its alignment";
     case MCSD_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
     case MCSD_ERR_CUDA: return "a CUDA runtime call or kernel launch failed";
     case MCSD_ERR_UNSUPPORTED: return "size beyond the library limits";

@@ -52,6 +52,13 @@ int elem_size(int dtype) { return dtype == MCSD_DTYPE_F32 ? 4 : 2; }
 int shift_of(int page_size) { return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : 7; }
 bool good_page_size(int ps) { return ps == 16 || ps == 32 || ps == 64 || ps == 128; }
 
+// Whether device pointers lie on multiples of `bytes` (a null one does): the kernels would fault on others.
+template <typename... Ptr>
+bool on_multiples(unsigned bytes, const Ptr *...p)
+{
+    return ((reinterpret_cast<uintptr_t>(p) | ... | uintptr_t(0)) & (bytes - 1)) == 0;
+}
+
 int launched(int n)
 {
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
@@ -128,6 +135,7 @@ int rows_call(const mcsd_kv_cache *cache, const void *keys, int64_t key_token, i
     set_last_launches(0);
     if (n_tokens == 0 || cache->n_pages == 0) return MCSD_OK;
     if (!slots || (APPEND ? !keys || !values : !keys && !values)) return MCSD_ERR_NULL;
+    if (!on_multiples(static_cast<unsigned>(elem_size(dtype)), keys, values) || !on_multiples(8, slots)) return MCSD_ERR_STRIDE;
     const int64_t row = cache->head_dim;
     // rows must not overlap where they are written
     if (!APPEND && ((keys && cache->n_heads > 1 && key_head < row) || (values && cache->n_heads > 1 && value_head < row))) return MCSD_ERR_STRIDE;
@@ -273,6 +281,10 @@ int mcsd_apply_logit_rules(const mcsd_desc *desc, const mcsd_logit_rules *rules,
     if (desc->batch == 0 || n_rows == 0) return MCSD_OK;
     if (!logits || !out) return MCSD_ERR_NULL;
     if (logits == out && ld_in != ld_out) return MCSD_ERR_STRIDE;
+    if (!on_multiples(static_cast<unsigned>(elem_size(desc->dtype)), logits, out) ||
+        !on_multiples(4, cand_tokens, desc->out_status, rules->history, rules->history_len, rules->prompt_len, rules->repetition, rules->frequency,
+                      rules->presence, rules->bias_ids, rules->bias_values, rules->masks, rules->mask_index))
+        return MCSD_ERR_STRIDE;
     const bool penalise = rules->repetition || rules->frequency || rules->presence;
     if (penalise && !cand_tokens && depth > 0) return MCSD_ERR_NULL;
 
@@ -325,6 +337,9 @@ int mcsd_build_page_tables(const mcsd_page_desc *d)
     if (d->batch == 0) return MCSD_OK;
     if (!d->start || !d->held || !d->ring_state || !d->ring || (!d->page_table && d->max_pages > 0))
         return MCSD_ERR_NULL;
+    if (!on_multiples(4, d->start, d->count, d->page_table, d->held, d->held_out, d->ring, d->ring_state, d->ring_state_out, d->cu_tokens, d->status) ||
+        !on_multiples(8, d->slots))
+        return MCSD_ERR_STRIDE;
     PagesParams p = {};
     p.start = d->start; p.count = d->count; p.table = d->page_table;
     p.held = d->held; p.held_out = d->held_out ? d->held_out : d->held;
@@ -388,6 +403,7 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     set_last_launches(0);
     if (desc->batch == 0) return MCSD_OK;
     if (!prefix_len || !q || !out || (!page_table && desc->max_pages > 0)) return MCSD_ERR_NULL;
+    if (!on_multiples(2, q, out) || !on_multiples(4, page_table, prefix_len, lse)) return MCSD_ERR_STRIDE;
     if (!desc->workspace || reinterpret_cast<uintptr_t>(desc->workspace) % 256 != 0 ||
         desc->workspace_bytes < mcsd_tree_attention_workspace_bytes(desc, cache))
         return MCSD_ERR_WORKSPACE;
@@ -436,6 +452,7 @@ int mcsd_gather_accepted_pages(const mcsd_kv_cache *cache, int64_t n_layers, int
     set_last_launches(0);
     if (n_layers == 0 || batch == 0 || gamma == 0 || max_pages == 0 || cache->n_pages == 0) return MCSD_OK;
     if (!page_table || !prefix_len || !path_nodes || !accept_len) return MCSD_ERR_NULL;
+    if (!on_multiples(4, page_table, prefix_len, path_nodes, accept_len)) return MCSD_ERR_STRIDE;
     if (n_layers > (1LL << 40) / (static_cast<int64_t>(batch) * cache->n_heads)) return MCSD_ERR_UNSUPPORTED;
     MoveParams p = {};
     p.c = cache_params(cache);

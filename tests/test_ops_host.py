@@ -191,6 +191,32 @@ def test_logit_rule_refusals(lib):
     assert lib.mcsd_apply_logit_rules(None, None, None, None, None, 0, None, 0, 0, 0, 0) == -1
 
 
+def test_arrays_off_their_elements_are_refused(lib):
+    """A kernel would fault on them: every device array of every call, one byte (or half an element) off."""
+    b = ctypes.byref(_cache())
+    for f in (lib.mcsd_append_kv, lib.mcsd_read_kv):
+        for dtype, off in ((0, 2), (1, 1), (2, 1)):
+            assert f(b, FAKE + off, 256, 128, FAKE, 256, 128, dtype, 4, FAKE, None) == -7
+            assert f(b, FAKE, 256, 128, FAKE + off, 256, 128, dtype, 4, FAKE, None) == -7
+        assert f(b, FAKE, 256, 128, FAKE, 256, 128, 1, 4, FAKE + 4, None) == -7
+    for i in range(4):
+        a = [FAKE + 2 * (i == j) for j in range(4)]
+        assert lib.mcsd_gather_accepted_pages(b, 1, 0, a[0], 4, 4, 2, a[1], a[2], a[3], 3, None) == -7
+    parent = synth.tree_from_kconfig([2])
+    for i, off in enumerate((2, 2, 1, 1, 2)):
+        a = [FAKE + off * (i == j) for j in range(5)]
+        assert lib.mcsd_tree_attention(ctypes.byref(_attention()), b, a[0], a[1], parent.ctypes.data, a[2], a[3], a[4]) == -7
+    for name in ("start", "count", "page_table", "held", "held_out", "ring", "ring_state", "ring_state_out", "cu_tokens", "status"):
+        assert lib.mcsd_build_page_tables(ctypes.byref(_page_desc(**{name: FAKE + 2}))) == -7, name
+    assert lib.mcsd_build_page_tables(ctypes.byref(_page_desc(slots=FAKE + 4, n_slots=5))) == -7
+    for kw in ({"logits": FAKE + 2}, {"out": FAKE + 2}, {"cand": FAKE + 2}):
+        assert _rules_call(lib, **kw) == -7, kw
+    assert _rules_call(lib, {"dtype": 1}, logits=FAKE + 1) == -7 and _rules_call(lib, {"out_status": FAKE + 1}) == -7
+    whole = dict(history=FAKE, history_len=FAKE, n_history=4, ld_history=4, bias_ids=FAKE, bias_values=FAKE, n_bias=1, masks=FAKE, n_masks=6, ld_mask=2)
+    for name in ("history", "history_len", "prompt_len", "repetition", "frequency", "presence", "bias_ids", "bias_values", "masks", "mask_index"):
+        assert _rules_call(lib, (), {**whole, name: FAKE + 2}) == -7, name
+
+
 def test_status_bits_match_the_header():
     text = open(os.path.join(build.ROOT, "include", "mcsd.h")).read()
     for name, value in (("NO_PAGES", binding.STATUS_NO_PAGES), ("BAD_MASK", binding.STATUS_BAD_MASK)):
