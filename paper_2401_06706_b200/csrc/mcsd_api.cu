@@ -98,7 +98,7 @@ int plan_tree(const int32_t *parent, int n_nodes, int n_internal, TreePlan *plan
     if (n_nodes < 1) return MCSD_ERR_SHAPE;
     if (n_nodes > MCSD_MAX_NODES) return MCSD_ERR_UNSUPPORTED;
     if (parent[0] != -1) return MCSD_ERR_TREE;
-    std::vector<int> depth(n_nodes, 0);
+    int depth[MCSD_MAX_NODES] = {};
     std::memset(plan->child_first, 0, sizeof(plan->child_first));
     std::memset(plan->child_count, 0, sizeof(plan->child_count));
     int gamma = 0;

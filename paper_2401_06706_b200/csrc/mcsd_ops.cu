@@ -3,9 +3,6 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
-#include <map>
-#include <mutex>
-#include <utility>
 
 #include "mcsd_common.cuh"
 #include "mcsd_rules.cuh"
@@ -18,10 +15,11 @@
 namespace mcsd {
 namespace {
 
+constexpr int kDevices = 64;                        // whose properties are kept
+
 // Multiprocessors of the current device, 0 if there is none (asked once per device).
 int sm_count()
 {
-    constexpr int kDevices = 64;
     static std::atomic<int> known[kDevices];
     int dev = 0, n = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return 0;
@@ -31,19 +29,24 @@ int sm_count()
     return n;
 }
 
-// Shared memory beyond the default for a kernel, set once per kernel and device.
-template <typename Kernel>
-bool allow_smem(Kernel kernel, int bytes)
+// Shared memory beyond the default for a kernel, asked for when a device needs more than it has. (Nothing here or elsewhere
+// on the way of a call allocates or takes a lock: no exception reaches the C caller.)
+template <auto Kernel>
+bool allow_smem(int bytes)
 {
-    static std::mutex lock;
-    static std::map<std::pair<const void *, int>, int> known;
+    static std::atomic<int> known[kDevices];
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return false;
-    std::lock_guard<std::mutex> hold(lock);
-    int &have = known[{reinterpret_cast<const void *>(kernel), dev}];
-    if (have >= bytes) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-    have = bytes;
+    const bool keep = dev >= 0 && dev < kDevices;
+    if (keep && known[dev].load(std::memory_order_relaxed) >= bytes) return true;
+    // (always the most that a CTA may have, so that calls at the same time cannot lower each other's)
+    int most = 0;
+    if (cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, dev) != cudaSuccess) return false;
+    cudaFuncAttributes fa = {};
+    if (cudaFuncGetAttributes(&fa, Kernel) != cudaSuccess) return false;
+    most -= static_cast<int>(fa.sharedSizeBytes);
+    if (most < bytes || cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) return false;
+    if (keep) known[dev].store(most, std::memory_order_relaxed);
     return true;
 }
 
@@ -94,11 +97,15 @@ CacheParams cache_params(const mcsd_kv_cache *c)
 template <int DT>
 int launch_rules(const RulesParams &p, dim3 grid, size_t smem, bool vec, cudaStream_t st)
 {
-    void (*kernel)(const RulesParams) = vec ? rules_kernel<DT, true> : rules_kernel<DT, false>;
     // (trees some hundred levels deep; the kernel's own static part counts against the default of 48 KB as well)
-    if (smem > 40000 && !allow_smem(kernel, static_cast<int>(smem)))
-        return MCSD_ERR_CUDA;
-    kernel<<<grid, kRulesThreads, smem, st>>>(p);
+    const int more = smem > 40000 ? static_cast<int>(smem) : 0;
+    if (vec) {
+        if (more && !allow_smem<rules_kernel<DT, true>>(more)) return MCSD_ERR_CUDA;
+        rules_kernel<DT, true><<<grid, kRulesThreads, smem, st>>>(p);
+    } else {
+        if (more && !allow_smem<rules_kernel<DT, false>>(more)) return MCSD_ERR_CUDA;
+        rules_kernel<DT, false><<<grid, kRulesThreads, smem, st>>>(p);
+    }
     return launched(1);
 }
 
@@ -222,11 +229,11 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
 }
 
 // Launches the kernel that does the work and, as its programmatic dependent, the one that joins divided items.
-template <int DT, int D, int ROWS>
-int launch_with_join(void (*kernel)(const AttendParams), int threads, int smem, const AttendParams &p, cudaStream_t st)
+template <int DT, int D, int ROWS, auto Kernel>
+int launch_with_join(int threads, int smem, const AttendParams &p, cudaStream_t st)
 {
-    if (!allow_smem(kernel, smem)) return MCSD_ERR_CUDA;
-    kernel<<<p.n_ctas, threads, smem, st>>>(p);
+    if (!allow_smem<Kernel>(smem)) return MCSD_ERR_CUDA;
+    Kernel<<<p.n_ctas, threads, smem, st>>>(p);
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.batch * p.c.n_heads * p.n_blocks), ROWS / 8);
@@ -244,10 +251,10 @@ int launch_with_join(void (*kernel)(const AttendParams), int threads, int smem, 
 template <int DT, int D>
 int launch_attention(const AttendParams &p, int rows, cudaStream_t st)
 {
-    if (rows == 8) return launch_with_join<DT, D, 8>(narrow_kernel<DT, D, 1>, kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
-    if (rows == 16) return launch_with_join<DT, D, 16>(narrow_kernel<DT, D, 2>, kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
-    if (rows == 24) return launch_with_join<DT, D, 24>(narrow_kernel<DT, D, 3>, kNarrowWarps * 32, kNarrowSmem<D, 3>, p, st);
-    return launch_with_join<DT, D, kWideRows>(wide_kernel<DT, D>, kWideThreads, kWideSmem<D>, p, st);
+    if (rows == 8) return launch_with_join<DT, D, 8, narrow_kernel<DT, D, 1>>(kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
+    if (rows == 16) return launch_with_join<DT, D, 16, narrow_kernel<DT, D, 2>>(kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
+    if (rows == 24) return launch_with_join<DT, D, 24, narrow_kernel<DT, D, 3>>(kNarrowWarps * 32, kNarrowSmem<D, 3>, p, st);
+    return launch_with_join<DT, D, kWideRows, wide_kernel<DT, D>>(kWideThreads, kWideSmem<D>, p, st);
 }
 
 }  // namespace
@@ -357,7 +364,7 @@ int mcsd_build_page_tables(const mcsd_page_desc *d)
     if (ctas < (d->batch + 31) / 32) ctas = (d->batch + 31) / 32;
     if (ctas > sms) ctas = sms;
     const size_t smem = sizeof(int32_t) * (5 * static_cast<size_t>(d->batch) + 1);
-    if (smem > 40000 && !allow_smem(pages_kernel, static_cast<int>(smem))) return MCSD_ERR_CUDA;
+    if (smem > 40000 && !allow_smem<pages_kernel>(static_cast<int>(smem))) return MCSD_ERR_CUDA;
     pages_kernel<<<static_cast<unsigned>(ctas), kPagesThreads, smem, static_cast<cudaStream_t>(d->stream)>>>(p);
     return launched(1);
 }

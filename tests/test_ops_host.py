@@ -2,6 +2,8 @@
 enqueued (fake pointers are never used), and the plain statements they are tested against hold by hand."""
 import ctypes
 import os
+import subprocess
+import sys
 import types
 
 import numpy as np
@@ -215,6 +217,27 @@ def test_arrays_off_their_elements_are_refused(lib):
     whole = dict(history=FAKE, history_len=FAKE, n_history=4, ld_history=4, bias_ids=FAKE, bias_values=FAKE, n_bias=1, masks=FAKE, n_masks=6, ld_mask=2)
     for name in ("history", "history_len", "prompt_len", "repetition", "frequency", "presence", "bias_ids", "bias_values", "masks", "mask_index"):
         assert _rules_call(lib, (), {**whole, name: FAKE + 2}) == -7, name
+
+
+def test_trees_are_checked_without_an_allocation(lib, tmp_path):
+    """No C++ exception reaches a C caller: a process whose `operator new` throws still gets its answer."""
+    src, so = tmp_path / "no_new.cpp", tmp_path / "no_new.so"
+    src.write_text("#include <cstdlib>\n#include <new>\nextern \"C\" int refuse_new = 0;\n"
+                   "void *operator new(std::size_t n) { if (refuse_new) throw std::bad_alloc(); return std::malloc(n ? n : 1); }\n"
+                   "void operator delete(void *p) noexcept { std::free(p); }\nvoid operator delete(void *p, std::size_t) noexcept { std::free(p); }\n")
+    subprocess.run(["g++", "-shared", "-fPIC", "-O1", "-o", str(so), str(src)], check=True)
+    code = f"""
+import ctypes
+new = ctypes.CDLL({str(so)!r}, mode=ctypes.RTLD_GLOBAL)
+lib = ctypes.CDLL({binding.LIB_PATH!r})
+parent = (ctypes.c_int32 * 5)(-1, 0, 0, 1, 3)
+ctypes.c_int.in_dll(new, "refuse_new").value = 1
+depth = lib.mcsd_tree_depth(parent, 5)
+ctypes.c_int.in_dll(new, "refuse_new").value = 0
+print("depth", depth)
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, env={**os.environ, "LD_PRELOAD": str(so)})
+    assert r.returncode == 0 and r.stdout.strip() == "depth 3", (r.returncode, r.stdout, r.stderr[-500:])
 
 
 def test_status_bits_match_the_header():
