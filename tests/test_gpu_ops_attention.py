@@ -416,3 +416,39 @@ def test_a_loud_value_of_small_weight_takes_no_bits(kconfig, heads, kv, D, loud)
         out, lse, tol, tol_lse = _exact_rows(q, cache, table, prefix, parent, b, D ** -0.5)
         assert ((r.out[b].double() - out).abs() <= tol).all(), ((r.out[b].double() - out).abs() / tol).max()
         assert ((r.lse[b].double() - lse).abs() <= tol_lse).all()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("pad", [0, 8, 3])
+@pytest.mark.parametrize("prefixes", [[33, 64, 5], [2300, 900, 1500]])
+def test_strided_queries_and_outputs_of_many_rows(D, pad, prefixes):
+    """The same for the kernel of many rows: by vectors and by elements, items in one piece and divided ones."""
+    parent, q, cache, table, prefix = _problem(33, 3, "4x4x2x2x1", 2, 1, D, 16, prefixes, torch.bfloat16)
+    B, N, H, _ = q.shape
+    fused = torch.randn((B, N, H * D + 4 * D + pad), device="cuda").to(torch.bfloat16)
+    fused[:, :, pad:pad + H * D] = q.flatten(2)
+    qs = fused[:, :, pad:pad + H * D].unflatten(2, (H, D))
+    big = torch.full((B, N, H, D + pad), 2.0, device="cuda").to(torch.bfloat16)
+    want = _run(q, cache, table, prefix, parent)
+    att = binding.TreeAttention(B, parent, H, q.dtype, cache, table.shape[1])
+    r = att.mcsd_tree_attention(qs, cache, table, prefix, out=big[..., :D])
+    torch.cuda.synchronize()
+    assert torch.equal(r.out, want.out) and torch.equal(r.lse, want.lse) and (big[..., D:] == 2).all()
+    if max(prefixes) < 100:                          # (the statement goes position by position)
+        _check(q, cache, table, prefix, parent, r.out, r.lse)
+    else:
+        for b in range(B):
+            out, lse, tol, tol_lse = _exact_rows(q, cache, table, prefix, parent, b, D ** -0.5)
+            assert ((r.out[b].double() - out).abs() <= tol).all() and ((r.lse[b].double() - lse).abs() <= tol_lse).all()
+
+
+@pytest.mark.parametrize("kconfig,heads", [("", 8), ("2x2x2x2", 2), ("4x2x2x1", 6)])
+def test_a_sequence_is_right_in_any_batch(kconfig, heads):
+    """The cut of the work goes by the whole batch; a sequence's rows are right in every one: reversed, alone, among unused entries."""
+    parent, q, cache, table, prefix = _problem(34, 7, kconfig, heads, 2, 128, 16, [1500, 2, 90, 800, 1, 300, 77], torch.bfloat16)
+    for pick in (list(range(6, -1, -1)), [3], [0, 0, 5], [2, 4, 1]):
+        p = prefix[pick]
+        if pick == [2, 4, 1]:
+            p[1] = -1
+        r = _run(q[pick], cache, table[pick], p, parent)
+        _check(q[pick], cache, table[pick], p, parent, r.out, r.lse)

@@ -198,3 +198,64 @@ def test_one_layer_of_several_and_empty_calls():
     i32 = dict(dtype=torch.int32, device="cuda")
     binding.mcsd_gather_accepted_pages(cache, torch.zeros((1, 2), **i32), torch.zeros(1, **i32), torch.zeros((1, 1), **i32), torch.zeros(1, **i32))
     assert binding.mcsd_last_launch_count() == 0
+
+
+# ---------------------------------------------------------------- more tokens than one pass of the grid takes
+def _mixed(g, T, H, D, dtype):
+    """Rows of every kind, neighbouring tokens of different ones, so that the rows a thread works on together differ in all
+    that a row can differ in."""
+    kinds = ["plain", "offset", "ties", "extreme", "odd", "plain", "offset"]
+    x = torch.empty((T, H, D), dtype=dtype)
+    for i, kind in enumerate(kinds):
+        n = len(range(i, T, len(kinds)))
+        x[i::len(kinds)] = _rows(g, n, H, D, dtype, kind)
+    return x
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("T,H,D,ps,pad", [(4099, 8, 128, 16, 0), (4099, 8, 64, 32, 0), (1777, 32, 128, 64, 0), (4099, 5, 64, 16, 0), (2311, 8, 128, 16, 1), (2311, 7, 64, 128, 3)])
+def test_append_and_read_of_many_tokens(dtype, T, H, D, ps, pad):
+    """Every group of threads takes several tokens, several times over, and ends on a part of its last group; strides that
+    allow vectors and odd ones."""
+    dt = DTYPES[dtype]
+    g = torch.Generator().manual_seed(T + H + D)
+    k, v = _mixed(g, T, H, D, dt), _mixed(g, T, H, D, dt)
+    n_pages = T // ps + 4
+    slots = torch.randperm(n_pages * ps, generator=g)[:T]
+    slots[5::97] = -1
+    slots[6::131] = n_pages * ps + 5                 # (outside the cache as well)
+    fused = torch.zeros((T, 2 * H * D + pad), dtype=dt)
+    fused[:, pad:pad + H * D], fused[:, pad + H * D:] = k.flatten(1), v.flatten(1)
+    fused = fused.cuda()
+    before = torch.randint(0, 256, (n_pages, H, binding.mcsd_kv_block_bytes(D, ps)), generator=g, dtype=torch.uint8)
+    cache = binding.KvCache(before.cuda(), D, ps)
+    binding.mcsd_append_kv(cache, fused[:, pad:pad + H * D].unflatten(1, (H, D)), fused[:, pad + H * D:].unflatten(1, (H, D)), slots.cuda())
+    got, want = cache.pages.cpu().numpy(), before.numpy().copy()
+    s = slots.numpy()
+    here = (s >= 0) & (s < n_pages * ps)
+    page, row, half = s[here] // ps, s[here] % ps, ps * D // 2
+    params = []
+    for which, x in enumerate((k, v)):
+        codes, scale, mid = ref.quantise(_np(x)[here])
+        param = np.ascontiguousarray(np.stack([scale, mid], -1).astype(np.float16)).view(np.uint8)
+        for at, width, rows in ((which * half, D // 2, codes[..., 0::2] | codes[..., 1::2] << 4), (2 * half + which * 4 * ps, 4, param)):
+            part = want[:, :, at:at + ps * width].reshape(n_pages, H, ps, width)                 # (a copy)
+            part[page, :, row] = rows
+            want[:, :, at:at + ps * width] = part.reshape(n_pages, H, -1)
+        params.append((codes, scale, mid))
+    # a NaN mid may have any payload; everything else is equal byte by byte
+    halves = lambda a: np.ascontiguousarray(a[:, :, 2 * half:]).view(np.float16)
+    same = (got[:, :, 2 * half:].reshape(n_pages, H, -1, 2) == want[:, :, 2 * half:].reshape(n_pages, H, -1, 2)).all(-1)
+    assert np.array_equal(got[:, :, :2 * half], want[:, :, :2 * half])
+    assert (same | np.isnan(halves(got)) & np.isnan(halves(want))).all()
+    # and back, into rows at the same strides; what is skipped stays
+    for out_type in DTYPES.values():
+        out = torch.full((T, 2 * H * D + pad), 9.0, dtype=out_type).cuda()
+        binding.mcsd_read_kv(cache, slots.cuda(), keys=out[:, pad:pad + H * D].unflatten(1, (H, D)), values=out[:, pad + H * D:].unflatten(1, (H, D)))
+        out = out.cpu()
+        assert (out[:, :pad] == 9).all() and (out[~torch.from_numpy(here)] == 9).all()
+        for (codes, scale, mid), o in zip(params, (out[:, pad:pad + H * D], out[:, pad + H * D:])):
+            exact = mid.astype(np.float64)[..., None] + scale.astype(np.float64)[..., None] * (codes - 8.0)
+            w = torch.from_numpy(exact.astype(np.float32)).to(out_type).float()
+            o = o.unflatten(1, (H, D))[torch.from_numpy(here)].float()
+            assert ((o == w) | (torch.isnan(o) & torch.isnan(w))).all()

@@ -255,3 +255,66 @@ def test_in_place_leaves_what_no_rule_concerns(dtype, V, mask):
     same = x.view(bits) == before
     assert same[~touched[:, None].expand(2, 3, V)].all()
     assert torch.isneginf(x[:, :, hidden]).all() and (x[1, :, 5] == before.view(dt)[1, :, 5] + 1).all()
+
+
+# ---------------------------------------------------------------- the slices of large batches
+def _slice(B, V):
+    """Tokens of one CTA: the widest slice of at most 2048 that gives every SM two CTAs."""
+    sms, size = torch.cuda.get_device_properties(0).multi_processor_count, 2048
+    while size > 512 and -(-V // size) * B < 2 * sms:
+        size //= 2
+    return size
+
+
+def _device_reference(parent, x, cand, b):
+    """(values, size of what was added up) of one sequence in 64 bits, [N, V], on the device."""
+    V, N = x["logits"].shape[2], len(parent)
+    ids, inside = x["history"][b].long(), (x["history"][b] >= 0) & (x["history"][b] < V)
+    at = torch.arange(ids.numel(), device="cuda")
+    inside &= at < x["history_len"][b].clamp(0, ids.numel())
+    prompt = at < x["prompt_len"][b]
+    base = torch.bincount(ids[inside & ~prompt], minlength=V).double()
+    given = torch.bincount(ids[inside & prompt], minlength=V) > 0
+    count = base.expand(N, V).clone()
+    for n in range(N):
+        for m in ref.path(parent, n)[:-1]:
+            if 0 <= int(cand[b, m]) < V:
+                count[n, int(cand[b, m])] += 1
+    bias = torch.zeros(V, dtype=torch.float64, device="cuda")
+    for i, v in zip(x["bias_ids"][b].tolist(), x["bias_values"][b].tolist()):
+        if 0 <= i < V:
+            bias[i] = v
+    theta, f, p = (x[k][b].double() for k in ("repetition", "frequency", "presence"))
+    l = x["logits"][b].double()
+    pen = torch.where(l > 0, l / theta, l * theta)
+    size = torch.maximum(l.abs(), pen.abs()) + f.abs() * count + p.abs() * (count > 0) + bias.abs()
+    l = torch.where((count > 0) | given, pen, l) - f * count - p * (count > 0) + bias
+    if x["masks"] is not None:
+        token = torch.arange(V, device="cuda")
+        for n in range(N):
+            m = int(x["mask_index"][b, n])
+            if 0 <= m < x["masks"].shape[0]:
+                l[n, (x["masks"][m][token // 32] >> (token % 32)) & 1 == 0] = float("-inf")
+    return l, size
+
+
+@pytest.mark.parametrize("dtype", sorted(DTYPES))
+@pytest.mark.parametrize("B,kconfig,V,mask,slice_", [
+    (64, "2x2x2x2", 50272, "table", 2048), (40, "4x2x2x1", 32003, "table", 2048), (20, "2x2x2x2", 32000, "none", 2048),
+    (10, "4x2x2x1", 32000, "table", 1024), (12, "2x2x2x2", 32001, "table", 1024), (300, "3x3x1", 1100, "table", 2048)])
+def test_slices_of_large_batches(dtype, B, kconfig, V, mask, slice_):
+    """Slices of 1024 and 2048 tokens, the last one in part, several rows per warp; by vectors and by elements; both forms."""
+    assert _slice(B, V) == slice_
+    dt = DTYPES[dtype]
+    parent, x, cand = _inputs(B, kconfig, V, dt, B + V, history=1000, bias=60, mask=mask)
+    assert mask == "none" or len(x["mask_index"]) == B
+    got = binding.mcsd_apply_logit_rules(x["logits"], parent, cand, _rules(x), out=torch.full_like(x["logits"], 77.0))
+    inplace = x["logits"].clone()
+    binding.mcsd_apply_logit_rules(inplace, parent, cand, _rules(x))
+    assert torch.equal(inplace.view(torch.uint8), got.view(torch.uint8))
+    fi, cpu_cand = torch.finfo(dt), cand.cpu()
+    for b in range(0, B, max(B // 16, 1)):
+        want, size = _device_reference(parent, x, cpu_cand, b)
+        # one rounding to the type behind at most four in float32, as in _close
+        tol = fi.eps / 2 * want.abs().clamp(min=fi.tiny) + 4 * 2.0 ** -24 * size
+        assert (((got[b].double() - want).abs() <= tol) | (got[b].double() == want)).all()
