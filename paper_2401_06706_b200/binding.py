@@ -511,6 +511,13 @@ def _device_tensor(t: Optional[torch.Tensor], dtype, shape, device, name: str, c
     return t
 
 
+def _settle(device: torch.device) -> None:
+    """Waits until what was enqueued for new buffers (their fill, and what used their memory before) is done, so that
+    the first call that uses them may be on any stream.  (In a capture they belong to its graph: nothing to wait for.)"""
+    if not torch.cuda.is_current_stream_capturing():
+        torch.cuda.current_stream(device).synchronize()
+
+
 class LogitRules:
     """The rules of mcsd_apply_logit_rules (see mcsd.h); every argument is a device tensor or None.
     history [B, H] int32 with unit stride along a row; history_len, prompt_len [B] int32; repetition, frequency,
@@ -618,8 +625,10 @@ class PageTables:
     def empty(cls, batch: int, max_pages: int, n_pages: int, page_size: int, device="cuda"):
         """Tables of a batch that holds nothing yet, over a pool of n_pages free pages."""
         i32 = dict(dtype=torch.int32, device=device)
-        return cls(torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32), torch.arange(n_pages, **i32),
+        plan = cls(torch.full((batch, max_pages), -1, **i32), torch.zeros(batch, **i32), torch.arange(n_pages, **i32),
                    torch.tensor([0, n_pages, 0, 0], **i32), page_size)
+        _settle(plan.device)
+        return plan
 
     def mcsd_build_page_tables(self, start: torch.Tensor, count, *, slots: Optional[torch.Tensor] = None):
         """start [B] int32; count: tokens per sequence, an int for all or [B] int32; slots: [n] int64, filled in packed
@@ -671,7 +680,9 @@ class KvCache:
         block = mcsd_kv_block_bytes(head_dim, page_size)
         if block == 0:
             _check(-10)
-        return cls(torch.zeros(lead + (n_heads, block), dtype=torch.uint8, device=device), head_dim, page_size)
+        cache = cls(torch.zeros(lead + (n_heads, block), dtype=torch.uint8, device=device), head_dim, page_size)
+        _settle(cache.device)
+        return cache
 
     def layer(self, i: int) -> "KvCache":
         assert self.pages.dim() == 4
@@ -755,6 +766,7 @@ class TreeAttention:
         self.workspace = torch.empty(ws + 256, dtype=torch.uint8, device=self.device)
         d.workspace = (self.workspace.data_ptr() + 255) // 256 * 256
         d.workspace_bytes = ws
+        _settle(self.device)
 
     def mcsd_tree_attention(self, q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, prefix_len: torch.Tensor, *,
                             scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> AttentionOutput:

@@ -216,3 +216,41 @@ def test_a_captured_step():
         assert np.array_equal(history.cpu().numpy(), past)
         moved += int((accept > 0).sum())
     assert moved > 0
+
+
+def test_new_buffers_are_ready_for_any_stream():
+    """Objects made while their stream is busy, used on another stream at once: nothing that was enqueued for making them
+    comes after the call."""
+    parent = synth.tree_from_kconfig([2])
+    B, N, ps, D, heads = 2, 3, 16, 64, 2
+    g = torch.Generator().manual_seed(13)
+    rows = torch.randn((2 * ps * B, heads, D), generator=g).cuda()
+    q = torch.randn((B, N, heads, D), generator=g).to(torch.bfloat16).cuda()
+    lengths, start = torch.full((B,), 20, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda")
+    slots, tree_slots = (torch.empty(n, dtype=torch.int64, device="cuda") for n in (20 * B, N * B))
+
+    def use(make, stream):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            made = []
+            for f in make:                           # (each made on the busy stream, used on this one)
+                with torch.cuda.stream(torch.cuda.default_stream()):
+                    if stream != torch.cuda.default_stream():
+                        torch.cuda._sleep(20_000_000)        # about 10 ms
+                    made.append(f(*made))
+                if len(made) == 1:
+                    made[0].mcsd_build_page_tables(start, 20, slots=slots)
+                    made[0].mcsd_build_page_tables(lengths, N, slots=tree_slots)
+                elif len(made) == 2:
+                    binding.mcsd_append_kv(made[1], rows[:20 * B], rows[:20 * B].flip(0), slots)
+                    binding.mcsd_append_kv(made[1], rows[-N * B:], rows[:N * B], tree_slots)
+                else:
+                    r = made[2].mcsd_tree_attention(q, made[1], made[0].table, lengths)
+        torch.cuda.synchronize()
+        return r.out, r.lse, made[1].pages, made[0].table, made[0].ring_state
+
+    make = [lambda: binding.PageTables.empty(B, 4, 9, ps), lambda p: binding.KvCache.empty(9, heads, D, ps),
+            lambda p, c: binding.TreeAttention(B, parent, heads, q.dtype, c, 4)]
+    want = use(make, torch.cuda.default_stream())
+    got = use(make, torch.cuda.Stream())
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and (want[0] != 0).any()

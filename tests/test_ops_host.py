@@ -134,6 +134,7 @@ def test_attention_workspace_is_sized_on_the_device_of_the_cache(lib, monkeypatc
             return lib.mcsd_tree_attention_workspace_bytes(d, c)
 
     monkeypatch.setattr(binding, "_on_device", Guard)
+    monkeypatch.setattr(binding, "_settle", lambda device: None)
     monkeypatch.setattr(binding, "load_library", lambda path=None: Lib())
     cpu = torch.device("cpu")                        # (stands for the device of the cache)
     cache = types.SimpleNamespace(device=cpu, head_dim=128, page_size=16, n_heads=2, desc=_cache())
