@@ -602,7 +602,10 @@ int mcsd_read_kv(const mcsd_kv_cache *cache, void *keys, int64_t key_token_strid
  *   s_j = scale * <q, k_j>,  out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j)
  * with q and out per query head; query head h reads key/value head h / (n_heads / cache->n_heads).  A tree
  * of one node is plain decoding.  Positions beyond the table or in a page entry outside [0, n_pages)
- * are not there; a row that sees no position is 0 with lse = -inf.  prefix_len[b] < 0 marks an unused
+ * are not there; a row that sees no position is 0 with lse = -inf.  Products take 16-bit operands: a weight
+ * softmax(s)_j * value scale_j is rounded to half relative to the row's largest one (2^-11 of it, or 2^-20 of the largest for those
+ * far below), queries are scaled to half's range by a power of two per row (numbers above 2^112, which only bf16 has, count
+ * as infinite); all else is float32.  prefix_len[b] < 0 marks an unused
  * batch entry: its rows of out and lse are left as they were.  Calls that may overlap on the device need
  * workspaces of their own.  Waits inside the kernels are bounded; should one expire, the rows it concerns are NaN.
  */

@@ -196,9 +196,10 @@ __device__ __forceinline__ float att_factor(float m, float l, float top) { retur
 //
 // Measured: 64 sequences of up to 8191 positions, 8 key heads, 4 query heads each: 92 us, 3.9 TB/s of the algorithm's bytes,
 // 0.60 of the measured copy bandwidth; 8 sequences of up to 2050 positions x 32 heads, 45 rows: 77 us. The 32-bit logic
-// pipe bounds it (54 % busy: an AND for every two codes and row block, a byte permutation and a shift for every
+// pipe bounds it (53 % busy: an AND for every two codes and row block, a byte permutation and a shift for every
 // eight of the values), then the warps' own latencies; with queries as the long side (sixteen rows a block, a
-// maximum by shuffles in every chunk) the first took 165 us.
+// maximum by shuffles in every chunk) the first took 165 us. Blocks of 24 rows take 255 registers, eight warps per SM; with
+// D = 128 every form spills a few words (16 to 92 bytes a thread).
 //
 // Row c of a tile of eight keys is key kappa(c): with this order (and, where a row has four 16-byte chunks, those of
 // rows 4 to 7 exchanged by two) every shared-memory load of codes touches each bank once.

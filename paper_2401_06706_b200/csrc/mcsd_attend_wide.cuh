@@ -122,7 +122,8 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 // it. With the work cut by units alone it took 297 us, without the copies four units ahead 345 us, with products issued by a
 // single thread 390 us. Left out: sixteen
 // softmax warps of sixteen rows in fragment layout (a quarter of the parameter loads, 322 us; 20 % slower than this
-// form on prefixes of 2000, where the tree's own units weigh more), separate rings for keys and values (328 us).
+// form on prefixes of 2000, where the tree's own units weigh more), separate rings for keys and values (328 us). The softmax warps spill
+// 36 bytes a thread.
 template <int DT, int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
 wide_kernel(const __grid_constant__ AttendParams P)

@@ -61,12 +61,12 @@ __device__ __forceinline__ RowWalk row_walk(const RowsParams &P)
 // 8 and stores one word of codes.  Rows of a token's heads follow each other in the thread order, so that
 // loads are contiguous (a page's rows of one head are 32 to 64 contiguous bytes each).  Bound by HBM: 2 D
 // numbers read and D + 8 bytes written per key/value row pair; a thread takes kRowsAhead tokens at a time, so
-// that their slots, and then their numbers, are in flight together.  Measured on 40001 tokens x 8 heads x 128 halves: 92 us
-// (0.34 of the measured copy bandwidth; the loads of a thread wait for one another, and some 150 instructions for the two rows
-// of a warp are the other half of it), the way back 53 us (0.60). Other numbers of tokens at a time: 4 take 94 us, 2 take 98, and
+// that their slots, and then their numbers, are in flight together.  Measured on 40001 tokens x 8 heads x 128 halves: 87 us
+// alone, 91 in a pass that reads back as well (0.35 of the measured copy bandwidth; the loads of a thread wait for one another, and some 150
+// instructions for the two rows of a warp are the other half of it), the way back 51 us (0.61; every token's codes wait for its slot). Other numbers of tokens at a time: 4 take 94 us, 2 take 98, and
 // for the way back 2 take 55 us, 4 take 67; with a grid of eight CTAs per SM (not all resident) 106 and 68 us.
-// Scale, mid and codes are those of the definition in exact arithmetic: the two per-row numbers are formed
-// in double (by one of a row's threads), and where x / scale - mid / scale in float32 lies within 2^-18 + |mid / scale| 2^-23
+// Scale and mid are formed in double (by one of a row's threads), rounded to float32 and then to half, as the definition says; codes are
+// those of exact arithmetic on them: where x / scale - mid / scale in float32 lies within 2^-18 + |mid / scale| 2^-23
 // of a border between two codes (a reciprocal good to 2^-23 and the last rounding put a number up to 8.5 off by 2^-18.9 at most,
 // the rounding of mid / scale by |mid / scale| 2^-24) the thread's codes are decided in double; so no code depends on
 // how the compiler orders things.  Rounding to an integer is an addition of 1.5 2^23 (the conversion
@@ -303,9 +303,10 @@ struct MoveParams {
 // in ascending order never reads what it has overwritten; up to kBatch moves in each of kLayers layers are read before
 // one is written.
 // Where a row lies is the same in every layer, so a thread finds out once (three loads, each from the one before) and
-// uses it for its run of layers.  256 sequences, 32 layers, 8 heads: 21 us, with one layer at a time 24 us, with runs of one
-// layer instead of six 35 us. Some 90000 row pairs are four pieces of 4 to 64 bytes each there, read and written at
-// unrelated places: 32-byte sectors make that twice the bytes it moves, and the places bound it, not the rate.
+// uses it for its run of layers.  256 sequences, 32 layers, 8 heads: 23 us in a cold capture, 28 us a call; back to back on the same
+// rows it was 21 us, with one layer at a time 24 us, with runs of one layer instead of six 35 us. Some 90000 row pairs are four pieces
+// of 4 to 64 bytes each there, read and written at unrelated places (about 7 us in whole 32-byte sectors): what a thread has in flight
+// bounds it, and of sixteen threads six (D = 64) or ten work.
 template <int D>
 __global__ void __launch_bounds__(256)
 move_kernel(const MoveParams P)

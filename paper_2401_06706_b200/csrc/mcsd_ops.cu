@@ -212,10 +212,10 @@ AttentionPlan attention_plan(const mcsd_attention_desc *d, const mcsd_kv_cache *
     // or four), one of 128 takes about as long for few rows as for all.  Measured (128 numbers a head, 8 sequences x 32
     // key heads x 2000 positions | 4 sequences x 8 key heads x 16000 positions, us):
     //   rows   blocks of 16   blocks of 24   one of 128
-    //   24     69 | 66        52 | 52        94 | 83
-    //   32     72 | 67        83 | 79        96 | 85
-    //   45     96 | 89        91 | 81        94 | 87
-    //   60     121 | 109                     96 | 87
+    //   24     69 | 66        52 | 52        86 | 77
+    //   32     70 | 66        85 | 76        87 | 76
+    //   45     99 | 89        88 | 78        87 | 76
+    //   60     124 | 109      121 | 105      97 | 78
     plan.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 24 ? 24 : rows <= 32 ? 16 : rows <= 48 ? 24 : kWideRows;
     plan.blocks = static_cast<int>((rows + plan.rows - 1) / plan.rows);
     // Measured for 0, 1, 2, 3, 4, 6, 8 and 12 places an item: decoding is fastest with 2 or 3, blocks of 16 and 24 rows with 3 to 8,

@@ -60,7 +60,8 @@ __device__ __forceinline__ void pages_scan(long long (&v)[3], long long (&total)
 // the pages taken and the pages returned lie in different places, so reads and writes of a call never
 // meet.  New lengths and the new state are written by CTA 0, or, where they replace their inputs, by
 // the CTA that finishes last (counted in state[2], which goes back to 0).  Bound by latency: three dependent
-// loads and two block-wide scans; a call takes 10 us for 8 sequences, 15 us for 256 prompts and 1.05 M slots.
+// loads and two block-wide scans; a call takes 10 us for 8 sequences (of which only a
+// warp's worth has anything to scan), 15 us for 256 prompts and 1.05 M slots.
 __global__ void __launch_bounds__(kPagesThreads)
 pages_kernel(const PagesParams P)
 {

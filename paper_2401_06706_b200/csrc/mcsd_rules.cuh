@@ -36,8 +36,9 @@ struct RulesParams {
 // takes the tokens some rule concerns one by one from a list, and last the few on the row's path, from their
 // logits read before.  (With the rules applied while streaming, nearly every warp had a lane with a token
 // that needs them, and all lanes went through them: 215 us against 137 us on 64 x 31 rows of 50272 halves; the mask's words taken by shuffles from one load a
-// lane and four CTAs per SM instead of three made that 108 us, 3.7 TB/s or 0.57 of the measured copy bandwidth: the
-// starts of the CTAs, five dependent loads each, are what is left.)
+// lane and four CTAs per SM instead of three made that 108 us, 3.7 TB/s or 0.56 of the measured copy bandwidth.
+// What is left: a CTA asks for its first row behind five dependent loads and four barriers, and a warp for its next row when it is through
+// with one. In place the same takes 115 us, without masks 48 us.)
 template <int DT, bool VEC>
 __global__ void __launch_bounds__(kRulesThreads, 4)
 rules_kernel(const __grid_constant__ RulesParams P)
