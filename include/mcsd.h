@@ -642,6 +642,121 @@ int mcsd_gather_accepted_pages(const mcsd_kv_cache *cache, int64_t n_layers, int
                                const int32_t *prefix_len, const int32_t *path_nodes, const int32_t *accept_len,
                                int32_t gamma, void *stream);
 
+/*
+ * Prompts and long conversations over the same cache: attention of a chunk of new tokens of every sequence (a
+ * prompt, a part of one, a single token), the attention weight that cached rows gather, the eviction of the rows that
+ * gathered least, and log probabilities of tokens.
+ *
+ * A chunk: the new tokens of all sequences lie packed, token i of sequence b in row cu_tokens[b] + i (the cu_tokens of
+ * mcsd_build_page_tables), count = cu_tokens[b + 1] - cu_tokens[b] of them, at most max_new, as far as there are n_tokens
+ * rows.  Token i stands at position start[b] + i of its sequence and sees positions 0 .. start[b] + i: its own row and those before
+ * it, which mcsd_append_kv stored there.  start[b] < 0 marks an unused batch entry and a count of 0 a sequence without
+ * new tokens; rows that belong to no token are left as they were.  Positions beyond the table or in a page entry
+ * outside [0, n_pages) are not there.
+ */
+#define MCSD_MAX_GROUP 128 /* query heads per key/value head of a chunk */
+
+typedef struct mcsd_chunk_desc {
+    int32_t batch;
+    int32_t n_heads;         /* query heads, a multiple of cache->n_heads                              */
+    int32_t dtype;           /* of q and out: MCSD_DTYPE_BF16 or MCSD_DTYPE_F16                        */
+    int32_t max_pages;       /* columns of page_table that exist; max_pages * page_size < 2^31         */
+    int32_t max_new;         /* new tokens that a sequence has at most (rows of further ones are left
+                                as they were); <= 2^24                                                 */
+    int32_t reserved;        /* must be 0                                                             */
+    int64_t n_tokens;        /* rows of q, out and lse; <= 2^31 - 1                                    */
+    int64_t ld_table;        /* entries between rows of page_table, >= max_pages                       */
+    int64_t q_token_stride, q_head_stride;     /* in elements; the D numbers of a row                  */
+    int64_t out_token_stride, out_head_stride; /* follow each other                                    */
+    float scale;             /* finite                                                                */
+    void *stream;
+    void *workspace;         /* device scratch, 256-byte aligned, caller-owned; overwritten            */
+    size_t workspace_bytes;  /* >= mcsd_chunk_attention_workspace_bytes                                */
+} mcsd_chunk_desc;
+
+/* Depends on the sizes only, not on the lengths or n_tokens; 0 for a descriptor that is not valid. */
+size_t mcsd_chunk_attention_workspace_bytes(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache);
+
+/* s_j = scale * <q, k_j>,  out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j)  over the positions a token sees; query
+ * head h reads key/value head h / (n_heads / cache->n_heads), at most MCSD_MAX_GROUP to one.  A row that sees no
+ * position is 0 with lse = -inf.  q, out device [n_tokens][n_heads][D] with the given strides (out may be q, with the same strides; they
+ * must not overlap otherwise); lse device [n_tokens][n_heads] float32 or NULL; page_table [batch][ld_table], start
+ * [batch], cu_tokens [batch + 1] device int32.  Calls that may overlap on the device need workspaces of their own. */
+int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
+                         const int32_t *start, const int32_t *cu_tokens, const void *q, void *out, float *lse);
+
+/* What every cached row of the sequences with new tokens gathers of their attention, per key/value head:
+ *   weights[p] := (p < start[b] and decay != 0 ? decay * weights[p] : 0) + sum exp(s_p - lse)
+ * over the last `last_tokens` new tokens of the sequence (0: all of them) that see p and the query heads of the key head, with s as
+ * above and lse as mcsd_chunk_attention gave it (rows with lse = -inf count nothing).  weights: device float32 [n_pages][cache->n_heads]
+ * [page_size], a number for each row of the cache.  Rows of sequences without new tokens keep theirs.  Sums are float32 in a
+ * fixed order.  Of the descriptor the strides of out and the workspace are not read. */
+int mcsd_accumulate_weights(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
+                            const int32_t *start, const int32_t *cu_tokens, const void *q, const float *lse,
+                            float *weights, float decay, int32_t last_tokens);
+
+/*
+ * Eviction by gathered weight.  Sequence b holds len[b] rows and keeps keep_len[b] (or keep) of them; one that has no more
+ * than that, or a negative keep_len, or len[b] < 0 (an unused entry) is left alone.  Every key/value head of every layer
+ * keeps, for itself, the first min(sink, keep) rows, the last min(recent, keep - sink) ones and, of those between, the ones with the
+ * largest weights (of equal ones those at lower positions; a NaN counts as the smallest).  They move to positions 0 .. keep - 1
+ * in their order, keys, values and weights, in place; rows behind stay what they were.  (Keys are stored as they were rotated, so
+ * attention does not ask where a row stands.)  mcsd_build_page_tables with start = len_out and no new tokens then returns
+ * the pages that became free.  Rows whose position has no page (see above) weigh least and do not move.  No two sequences may share a page.
+ */
+typedef struct mcsd_evict_desc {
+    int32_t batch;
+    int32_t max_pages;           /* columns of page_table that exist; max_pages * page_size < 2^31     */
+    int32_t keep, sink, recent;  /* >= 0                                                              */
+    int32_t reserved;            /* must be 0                                                         */
+    int64_t n_layers;            /* >= 1                                                              */
+    int64_t layer_stride;        /* bytes between the layers' caches behind cache->pages, a multiple of 16 */
+    int64_t weight_stride;       /* numbers between the layers' weights, >= n_pages * n_heads * page_size  */
+    int64_t ld_table;            /* entries between rows of page_table, >= max_pages                   */
+    const int32_t *page_table;
+    const int32_t *len;          /* [B] rows held, clipped to max_pages * page_size                    */
+    const int32_t *keep_len;     /* [B] or NULL: keep                                                 */
+    float *weights;              /* [n_layers][n_pages][n_heads][page_size]                            */
+    int32_t *len_out;            /* [B] rows held afterwards, or NULL; must not be len                 */
+    void *stream;
+} mcsd_evict_desc;
+int mcsd_evict_rows(const mcsd_evict_desc *desc, const mcsd_kv_cache *cache);
+
+/*
+ * Log probabilities: for output row i, which reads row r of the logits, with p = softmax(logits[r] / temperature),
+ *   logprobs[i][g]    = log p(tokens[i][g])        (a token outside [0, vocab): NaN)
+ *   entropy[i]        = - sum_x p(x) log p(x)
+ *   top_ids[i][j], top_logprobs[i][j]              the n_top tokens with the largest logits, largest first (of equal ones
+ *                                                  the lowest token), and log p of them
+ * in float32.  A row from which no distribution can be formed (all -inf, a NaN or a +inf logit) gives NaN and top_ids of -1.
+ * r = row_index[i], or i where row_index is NULL; with path_nodes (mcsd_desc.out_path_nodes, [B][path_len], path_len = gamma + 1)
+ * instead, output row b * path_len + j reads the row that token j of sequence b's walk was drawn from: row b * nodes_per_tree + node, node =
+ * the root for j = 0 and path_nodes[b][j - 1] else.  Output rows whose r is not in [0, n_logits) (a node not in [0, nodes_per_tree), as behind the end
+ * of a walk) are left as they were.  As in mcsd_verify all ld elements of a row must be readable.
+ */
+#define MCSD_MAX_TOP 32
+typedef struct mcsd_logprob_desc {
+    int32_t vocab;
+    int32_t dtype;               /* MCSD_DTYPE_* of the logits                                        */
+    int32_t n_given;             /* tokens per output row                                             */
+    int32_t n_top;               /* <= MCSD_MAX_TOP, <= vocab                                         */
+    int32_t path_len, nodes_per_tree; /* with path_nodes                                              */
+    int64_t n_logits, ld;        /* rows of the logits, elements between them (>= vocab)               */
+    int64_t n_out;               /* output rows; with path_nodes a multiple of path_len                */
+    const void *logits;
+    const int32_t *row_index;    /* [n_out] or NULL                                                   */
+    const int32_t *path_nodes;   /* or NULL; not both                                                 */
+    const int32_t *tokens;       /* [n_out][n_given]                                                  */
+    float *logprobs;             /* [n_out][n_given]; NULL to skip                                    */
+    float *entropy;              /* [n_out]; NULL to skip                                             */
+    int32_t *top_ids;            /* [n_out][n_top]; NULL to skip                                      */
+    float *top_logprobs;         /* [n_out][n_top]; NULL to skip                                      */
+    float temperature;           /* > 0, finite                                                       */
+    int32_t reserved;            /* must be 0                                                         */
+    void *stream;
+} mcsd_logprob_desc;
+int mcsd_token_logprobs(const mcsd_logprob_desc *desc);
+
 /* Frees the device staging buffers and streams mcsd_verify_host keeps on the current
  * device (allocating again on its next call).  Returns MCSD_OK or MCSD_ERR_CUDA. */
 int mcsd_release_host_staging(void);

@@ -21,7 +21,7 @@ DEBUG_LIB_PATH = os.path.join(_HERE, "libmcsd_debug.so")      # the checked buil
 
 MCSD_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 STATUS_DEGENERATE, STATUS_BAD_TOKEN, STATUS_NO_MASS, STATUS_TIMEOUT, STATUS_NO_PAGES, STATUS_BAD_MASK = 1, 2, 4, 8, 16, 32
-MAX_NODES, MAX_CHILDREN, MAX_VOCAB, MAX_SEQUENCES = 512, 32, 65536, 4096
+MAX_NODES, MAX_CHILDREN, MAX_VOCAB, MAX_SEQUENCES, MAX_GROUP, MAX_TOP = 512, 32, 65536, 4096, 128, 32
 
 EXPORTS = ("mcsd_verify", "mcsd_verify_nodes", "mcsd_verify_walk", "mcsd_verify_host", "mcsd_verify_static", "mcsd_verify_path", "mcsd_sample_candidates", "mcsd_tree_attention_layout",
            "mcsd_gather_accepted_kv",
@@ -30,7 +30,8 @@ EXPORTS = ("mcsd_verify", "mcsd_verify_nodes", "mcsd_verify_walk", "mcsd_verify_
            "mcsd_shard_columns", "mcsd_shard_workspace_bytes", "mcsd_shard_rounds", "mcsd_shard_partials",
            "mcsd_shard_decide", "mcsd_shard_endpoint", "mcsd_shard_finish", "mcsd_shard_commit", "mcsd_debug_bounds_hits", "mcsd_last_kernel_times",
            "mcsd_apply_logit_rules", "mcsd_build_page_tables", "mcsd_kv_block_bytes", "mcsd_append_kv", "mcsd_read_kv",
-           "mcsd_tree_attention", "mcsd_tree_attention_workspace_bytes", "mcsd_gather_accepted_pages")
+           "mcsd_tree_attention", "mcsd_tree_attention_workspace_bytes", "mcsd_gather_accepted_pages",
+           "mcsd_chunk_attention", "mcsd_chunk_attention_workspace_bytes", "mcsd_accumulate_weights", "mcsd_evict_rows", "mcsd_token_logprobs")
 OPT_CLUSTER, OPT_EPT, OPT_DIRECT, OPT_SAMPLE_AHEAD, OPT_WAIT_POLLS, OPT_TEST_EXTRA_TX, OPT_PDL, OPT_TEST_SHRINK_RANGES, OPT_SPLIT, OPT_TIME_KERNELS, OPT_TRACE, OPT_WALK_CLUSTER = range(12)
 
 
@@ -84,6 +85,29 @@ class McsdAttentionDesc(ctypes.Structure):
                 ("q_head_stride", ctypes.c_int64), ("out_seq_stride", ctypes.c_int64),
                 ("out_node_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64), ("scale", ctypes.c_float),
                 ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class McsdChunkDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("dtype", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("reserved", ctypes.c_int32), ("n_tokens", ctypes.c_int64), ("ld_table", ctypes.c_int64),
+                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("out_token_stride", ctypes.c_int64),
+                ("out_head_stride", ctypes.c_int64), ("scale", ctypes.c_float), ("stream", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class McsdEvictDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("keep", ctypes.c_int32), ("sink", ctypes.c_int32),
+                ("recent", ctypes.c_int32), ("reserved", ctypes.c_int32), ("n_layers", ctypes.c_int64), ("layer_stride", ctypes.c_int64),
+                ("weight_stride", ctypes.c_int64), ("ld_table", ctypes.c_int64), ("page_table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("keep_len", ctypes.c_void_p), ("weights", ctypes.c_void_p), ("len_out", ctypes.c_void_p), ("stream", ctypes.c_void_p)]
+
+
+class McsdLogprobDesc(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("n_given", ctypes.c_int32), ("n_top", ctypes.c_int32),
+                ("path_len", ctypes.c_int32), ("nodes_per_tree", ctypes.c_int32), ("n_logits", ctypes.c_int64), ("ld", ctypes.c_int64),
+                ("n_out", ctypes.c_int64), ("logits", ctypes.c_void_p), ("row_index", ctypes.c_void_p), ("path_nodes", ctypes.c_void_p),
+                ("tokens", ctypes.c_void_p), ("logprobs", ctypes.c_void_p), ("entropy", ctypes.c_void_p), ("top_ids", ctypes.c_void_p),
+                ("top_logprobs", ctypes.c_void_p), ("temperature", ctypes.c_float), ("reserved", ctypes.c_int32), ("stream", ctypes.c_void_p)]
 
 
 class McsdError(RuntimeError):
@@ -181,6 +205,17 @@ def load_library(path: Optional[str] = None):
     lib.mcsd_tree_attention.restype = ctypes.c_int
     lib.mcsd_gather_accepted_pages.argtypes = [cp, i64, i64, vp, i64, i32, i32, vp, vp, vp, i32, vp]
     lib.mcsd_gather_accepted_pages.restype = ctypes.c_int
+    kp = ctypes.POINTER(McsdChunkDesc)
+    lib.mcsd_chunk_attention_workspace_bytes.argtypes = [kp, cp]
+    lib.mcsd_chunk_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.mcsd_chunk_attention.argtypes = [kp, cp, vp, vp, vp, vp, vp, vp]
+    lib.mcsd_chunk_attention.restype = ctypes.c_int
+    lib.mcsd_accumulate_weights.argtypes = [kp, cp, vp, vp, vp, vp, vp, vp, f32, i32]
+    lib.mcsd_accumulate_weights.restype = ctypes.c_int
+    lib.mcsd_evict_rows.argtypes = [ctypes.POINTER(McsdEvictDesc), cp]
+    lib.mcsd_evict_rows.restype = ctypes.c_int
+    lib.mcsd_token_logprobs.argtypes = [ctypes.POINTER(McsdLogprobDesc)]
+    lib.mcsd_token_logprobs.restype = ctypes.c_int
     if path is None:
         _lib = lib
     return lib
@@ -810,6 +845,185 @@ def mcsd_gather_accepted_pages(cache: KvCache, page_table: torch.Tensor, prefix_
             prefix_len.data_ptr(), path_nodes.data_ptr(), accept_len.data_ptr(), path_nodes.shape[1] - 1, stream)
     _check(rc)
     return cache.pages
+
+
+# ---------------------------------------------------------------- prompts and long conversations
+class ChunkAttention:
+    """Attention of a chunk of new tokens of every sequence over a paged 4-bit cache, and the weight that the cached rows
+    gather of it (see mcsd.h): holds the descriptor, the outputs and the workspace of one (batch, heads, dtype, cache geometry) shape and
+    up to max_tokens tokens, so that repeated calls allocate nothing. max_new: tokens that a sequence has at most (max_tokens if
+    None); the fewer, the better the kernels fit. One call at a time: calls that may overlap, from other threads or on other streams or
+    in captured graphs, take an object each."""
+
+    def __init__(self, batch: int, max_tokens: int, n_heads: int, dtype: torch.dtype, cache: KvCache, max_pages: int, *,
+                 max_new: Optional[int] = None, want_lse: bool = True):
+        self.lib = load_library()
+        self.device, self.dtype = cache.device, dtype
+        self.batch, self.max_tokens, self.n_heads = int(batch), int(max_tokens), int(n_heads)
+        self.max_new = self.max_tokens if max_new is None else int(max_new)
+        self.head_dim, self.max_pages = cache.head_dim, int(max_pages)
+        self.geometry = (cache.n_heads, cache.head_dim, cache.page_size)
+        self.out = torch.zeros((self.max_tokens, self.n_heads, self.head_dim), dtype=dtype, device=self.device)
+        self.lse = torch.zeros((self.max_tokens, self.n_heads), dtype=torch.float32, device=self.device) if want_lse else None
+        d = self.desc = McsdChunkDesc()
+        d.batch, d.n_heads, d.dtype, d.max_pages, d.max_new = self.batch, self.n_heads, MCSD_DTYPE[dtype], self.max_pages, self.max_new
+        d.ld_table, d.n_tokens, d.scale = self.max_pages, self.max_tokens, 1.0
+        d.q_token_stride, d.q_head_stride = d.out_token_stride, d.out_head_stride = self.out.stride()[:2]
+        with _on_device(self.device):                # (the size goes by the device that the calls will run on)
+            ws = int(self.lib.mcsd_chunk_attention_workspace_bytes(d, cache.desc))
+        if ws == 0:
+            _check(self.lib.mcsd_chunk_attention(d, cache.desc, None, None, None, None, None, None))
+            _check(-2)
+        self.workspace = torch.empty(ws + 256, dtype=torch.uint8, device=self.device)
+        d.workspace = (self.workspace.data_ptr() + 255) // 256 * 256
+        d.workspace_bytes = ws
+        _settle(self.device)
+
+    def _bind(self, q, cache, page_table, start, cu_tokens, scale):
+        """The arguments that both calls share, checked and put into the descriptor; returns it."""
+        d = self.desc
+        assert cache.pages.dim() == 3, "one layer at a time: cache.layer(i)"
+        assert cache.device == self.device and self.geometry == (cache.n_heads, cache.head_dim, cache.page_size)
+        T = q.shape[0]
+        assert q.device == self.device and q.dtype is self.dtype and T <= self.max_tokens and q.shape[1:] == (self.n_heads, self.head_dim), \
+            "q must be [tokens, heads, head_dim] of this object's type and device, with at most max_tokens tokens"
+        assert q.stride(2) == 1, "rows of q must be contiguous"
+        _device_tensor(page_table, torch.int32, (self.batch, self.max_pages), self.device, "page_table", contiguous=False)
+        assert self.max_pages <= 1 or page_table.stride(1) == 1
+        _device_tensor(start, torch.int32, (self.batch,), self.device, "start")
+        _device_tensor(cu_tokens, torch.int32, (self.batch + 1,), self.device, "cu_tokens")
+        d.ld_table = int(page_table.stride(0)) if self.batch > 1 else self.max_pages
+        d.n_tokens, d.q_token_stride, d.q_head_stride = T, q.stride(0), q.stride(1)
+        d.scale = float(scale) if scale is not None else self.head_dim ** -0.5
+        return d
+
+    def mcsd_chunk_attention(self, q: torch.Tensor, cache: KvCache, page_table: torch.Tensor, start: torch.Tensor, cu_tokens: torch.Tensor, *,
+                             scale: Optional[float] = None, out: Optional[torch.Tensor] = None) -> AttentionOutput:
+        """q [tokens, n_heads, head_dim] with contiguous rows, packed by sequence; page_table [B, max_pages], start [B] and cu_tokens
+        [B + 1] int32 (PageTables has them); scale: 1 / sqrt(head_dim) if None. out: a tensor like q to write to instead of
+        this object's. Returns out and lse [tokens, n_heads]."""
+        d = self._bind(q, cache, page_table, start, cu_tokens, scale)
+        T = q.shape[0]
+        out = self.out[:T] if out is None else out
+        assert out.device == self.device and out.dtype is self.dtype and out.shape == q.shape and out.stride(2) == 1
+        lse = None if self.lse is None else self.lse[:T]
+        d.out_token_stride, d.out_head_stride = out.stride(0), out.stride(1)
+        with _on_device(self.device) as stream:
+            d.stream = stream
+            rc = self.lib.mcsd_chunk_attention(d, cache.desc, page_table.data_ptr(), start.data_ptr(), cu_tokens.data_ptr(),
+                                               q.data_ptr(), out.data_ptr(), _ptr(lse))
+        _check(rc)
+        return AttentionOutput(out, lse)
+
+    def mcsd_accumulate_weights(self, q: torch.Tensor, lse: torch.Tensor, cache: KvCache, page_table: torch.Tensor, start: torch.Tensor,
+                                cu_tokens: torch.Tensor, weights: torch.Tensor, *, scale: Optional[float] = None, decay: float = 1.0,
+                                last_tokens: int = 0) -> torch.Tensor:
+        """Adds what the last last_tokens new tokens of every sequence (0: all) give to each cached row to weights
+        [n_pages, heads, page_size] float32, in place (rows from before are multiplied by decay first); lse [tokens, n_heads] as
+        mcsd_chunk_attention returned it, the other arguments as there. Returns weights."""
+        d = self._bind(q, cache, page_table, start, cu_tokens, scale)
+        _device_tensor(lse, torch.float32, (q.shape[0], self.n_heads), self.device, "lse")
+        _device_tensor(weights, torch.float32, (cache.n_pages, cache.n_heads, cache.page_size), self.device, "weights")
+        with _on_device(self.device) as stream:
+            d.stream = stream
+            rc = self.lib.mcsd_accumulate_weights(d, cache.desc, page_table.data_ptr(), start.data_ptr(), cu_tokens.data_ptr(), q.data_ptr(),
+                                                  lse.data_ptr(), weights.data_ptr(), float(decay), int(last_tokens))
+        _check(rc)
+        return weights
+
+
+def mcsd_evict_rows(cache: KvCache, weights: torch.Tensor, page_table: torch.Tensor, length: torch.Tensor, keep, *, sink: int = 0, recent: int = 0,
+                    len_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Cuts sequences of `length` [B] int32 cached rows down to `keep` (an int for all, or [B] int32, negative: left alone): every
+    head of every layer keeps its first `sink` rows, its last `recent` ones and the heaviest of the others, moved to the front in
+    order, in place. weights float32 [n_pages, heads, page_size], with a leading [layers] where the cache has several. Returns the
+    lengths afterwards (len_out if given)."""
+    B, W = page_table.shape
+    dev, layers = cache.device, cache.pages.dim() == 4
+    _device_tensor(page_table, torch.int32, None, dev, "page_table", contiguous=False)
+    assert W <= 1 or page_table.stride(1) == 1
+    _device_tensor(length, torch.int32, (B,), dev, "length")
+    _device_tensor(len_out, torch.int32, (B,), dev, "len_out")
+    shape = (cache.n_pages, cache.n_heads, cache.page_size)
+    _device_tensor(weights, torch.float32, ((cache.n_layers,) if layers else ()) + shape, dev, "weights")
+    len_out = torch.empty_like(length) if len_out is None else len_out
+    d = McsdEvictDesc()
+    d.batch, d.max_pages, d.sink, d.recent = B, W, int(sink), int(recent)
+    if isinstance(keep, torch.Tensor):
+        d.keep_len = _device_tensor(keep, torch.int32, (B,), dev, "keep").data_ptr()
+    else:
+        d.keep = int(keep)
+    d.n_layers, d.layer_stride, d.weight_stride = cache.n_layers, cache.layer_stride, shape[0] * shape[1] * shape[2]
+    d.ld_table = page_table.stride(0) if B > 1 else W
+    d.page_table, d.len, d.weights, d.len_out = page_table.data_ptr(), length.data_ptr(), weights.data_ptr(), len_out.data_ptr()
+    with _on_device(dev) as stream:
+        d.stream = stream
+        rc = cache.lib.mcsd_evict_rows(d, cache.desc)
+    _check(rc)
+    return len_out
+
+
+@dataclass
+class LogprobOutput:
+    logprobs: torch.Tensor                  # like the tokens, float32
+    entropy: Optional[torch.Tensor]         # [rows] (or [B, gamma + 1]) float32
+    top_ids: torch.Tensor                   # [rows, n_top] int32 (or [B, gamma + 1, n_top])
+    top_logprobs: torch.Tensor              # the same, float32
+
+
+class TokenLogprobs:
+    """Log probabilities of given tokens, the entropy and the n_top largest tokens of rows of logits (see mcsd.h): holds the outputs of
+    up to max_rows rows, so that repeated calls allocate nothing (one call at a time). Entries that a call does not write keep what
+    they hold, 0 at first."""
+
+    def __init__(self, max_rows: int, vocab: int, dtype: torch.dtype, *, n_given: int = 1, n_top: int = 0, want_entropy: bool = True, device="cuda"):
+        self.lib = load_library()
+        self.max_rows, self.vocab, self.dtype, self.n_given, self.n_top = int(max_rows), int(vocab), dtype, int(n_given), int(n_top)
+        f32 = dict(dtype=torch.float32, device=device)
+        self.logprobs = torch.zeros((self.max_rows, self.n_given), **f32)
+        self.device = self.logprobs.device
+        self.entropy = torch.zeros(self.max_rows, **f32) if want_entropy else None
+        self.top_ids = torch.zeros((self.max_rows, self.n_top), dtype=torch.int32, device=device)
+        self.top_logprobs = torch.zeros((self.max_rows, self.n_top), **f32)
+        d = self.desc = McsdLogprobDesc()
+        d.vocab, d.dtype, d.n_given, d.n_top = self.vocab, MCSD_DTYPE[dtype], self.n_given, self.n_top
+        d.logprobs, d.entropy = self.logprobs.data_ptr(), _ptr(self.entropy)
+        d.top_ids, d.top_logprobs = (self.top_ids.data_ptr(), self.top_logprobs.data_ptr()) if self.n_top else (None, None)
+        _settle(self.device)
+
+    def _call(self, rows, logits, ld, tokens, temperature, lead):
+        d, n = self.desc, rows
+        assert logits.device == self.device and logits.dtype is self.dtype and logits.shape[-1] == self.vocab
+        assert n <= self.max_rows, f"{n} rows, but this object holds {self.max_rows}"
+        d.n_out, d.logits, d.tokens, d.temperature = n, logits.data_ptr(), tokens.data_ptr(), float(temperature)
+        d.n_logits, d.ld = logits.numel() // self.vocab, ld
+        with _on_device(self.device) as stream:
+            d.stream = stream
+            rc = self.lib.mcsd_token_logprobs(d)
+        _check(rc)
+        return LogprobOutput(self.logprobs[:n].view(tokens.shape), None if self.entropy is None else self.entropy[:n].view(lead),
+                             self.top_ids[:n].view(lead + (self.n_top,)), self.top_logprobs[:n].view(lead + (self.n_top,)))
+
+    def mcsd_token_logprobs(self, logits: torch.Tensor, tokens: torch.Tensor, *, temperature: float = 1.0,
+                            row_index: Optional[torch.Tensor] = None) -> LogprobOutput:
+        """logits [R, V] (rows may be strided); tokens int32 [n] or [n, n_given]; row_index [n] int32: the row of the logits each output row
+        reads (row i if None; one that is not there leaves its outputs alone)."""
+        n = tokens.shape[0]
+        assert logits.dim() == 2 and (self.vocab == 1 or logits.stride(1) == 1), "rows of logits must be contiguous"
+        _device_tensor(tokens, torch.int32, (n,) if tokens.dim() == 1 and self.n_given == 1 else (n, self.n_given), self.device, "tokens")
+        _device_tensor(row_index, torch.int32, (n,), self.device, "row_index")
+        self.desc.row_index, self.desc.path_nodes = _ptr(row_index), None
+        return self._call(n, logits, logits.stride(0) if logits.shape[0] > 1 else self.vocab, tokens, temperature, (n,))
+
+    def mcsd_path_logprobs(self, logits: torch.Tensor, path_nodes: torch.Tensor, tokens: torch.Tensor, *, temperature: float = 1.0) -> LogprobOutput:
+        """The tokens [B, gamma + 1] of verified walks (path_nodes and tokens as mcsd_verify returns them), each against the row of logits
+        [B, n_nodes, V] it was drawn from; entries behind the end of a walk are left alone."""
+        assert self.n_given == 1 and logits.dim() == 3 and path_nodes.dim() == 2 and path_nodes.shape[0] == logits.shape[0]
+        _device_tensor(path_nodes, torch.int32, None, self.device, "path_nodes")
+        _device_tensor(tokens, torch.int32, path_nodes.shape, self.device, "tokens")
+        d = self.desc
+        d.row_index, d.path_nodes, d.path_len, d.nodes_per_tree = None, path_nodes.data_ptr(), path_nodes.shape[1], logits.shape[1]
+        return self._call(path_nodes.numel(), logits, _row_stride(logits) if logits.numel() else self.vocab, tokens, temperature, tuple(path_nodes.shape))
 
 
 # ---------------------------------------------------------------- vocabulary split over several devices

@@ -14,7 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmcsd.so")
 DEBUG_LIB = os.path.join(HERE, "libmcsd_debug.so")
-SOURCES = [os.path.join(CSRC, "mcsd_api.cu"), os.path.join(CSRC, "mcsd_ops.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("mcsd_api.cu", "mcsd_ops.cu", "mcsd_prompts.cu")]
 HEADERS = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))) + [os.path.join(ROOT, "include", "mcsd.h")]
 
 
