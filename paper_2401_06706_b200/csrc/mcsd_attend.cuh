@@ -154,20 +154,91 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {            // of an
     return r;
 }
 
+// What a CTA has of an item: units [k0, k1) of one block of rows of one (sequence, key/value head). Rows row0 .. rows - 1 of the head's
+// are the block's (or fewer: a block has at most as many as the kernel's), the first `tail` positions are seen by all of them;
+// whole: all of the item's units.
+struct AttItem { int b, head, len, tail, row0, rows, k0, k1; bool whole; };
+// Where a part of an item goes: a CTA has one that others began and one that others end at most.
+__device__ __forceinline__ long long att_slot(int k0) { return 2 * blockIdx.x + (k0 > 0 ? 0 : 1); }
+
+// The rows of a tree: those of all nodes, as the narrow kernel and its like see them.
+struct TreeRows {
+    typedef AttendParams Params;
+    struct Walk {
+        AttCut cut;
+        AttCursor cur;
+        uint32_t u, u_end, places, items;
+        __device__ __forceinline__ bool begin(const AttendParams &P, int lane)
+        {
+            items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
+            cut = att_cut(P, items, lane);
+            if (cut.span == 0 || blockIdx.x > (cut.span - 1) / cut.per) return false;      // (runs before the last one are whole)
+            u = blockIdx.x * cut.per;
+            u_end = cut.span - u < cut.per ? cut.span : u + cut.per;
+            cur = att_find(P, cut, u, items, lane);
+            places = 0u;
+            return true;
+        }
+        template <int ROWS>
+        __device__ __forceinline__ bool next(const AttendParams &P, int lane, AttItem &it)
+        {
+            u += places;
+            cur.at += places;
+            if (u >= u_end) return false;
+            if (places > 0u && cur.at >= cur.places * items) cur = att_find(P, cut, u, items, lane);
+            const AttPiece piece = att_piece(cut, cur, u_end - u);
+            if (piece.k1 <= 0) return false;
+            places = piece.places;
+            it.b = cur.b;
+            it.len = cur.len;
+            it.head = piece.item / P.n_blocks;
+            it.row0 = (piece.item - it.head * P.n_blocks) * ROWS;
+            it.rows = P.n_rows;
+            it.tail = P.prefix_len[it.b];
+            it.k0 = piece.k0;
+            it.k1 = piece.k1;
+            it.whole = piece.k0 == 0 && piece.k1 == piece.units;
+            return true;
+        }
+    };
+    static __device__ __forceinline__ long long q_at(const AttendParams &P, const AttItem &it, int row)
+    {
+        const int node = row / P.group, h = it.head * P.group + (row - node * P.group);
+        return it.b * P.q_seq + node * P.q_node + h * P.q_head;
+    }
+    // Positions behind `tail` that a row sees, a bit each.
+    static __device__ __forceinline__ void see(const AttendParams &P, const AttItem &it, int row, uint32_t *seen)
+    {
+        for (int i = 0; i * 32 < P.n_nodes; ++i) seen[i] = 0u;
+        int a = row < it.rows ? row / P.group : -1;
+        while (a >= 0) {
+            seen[a >> 5] |= 1u << (a & 31);
+            a = P.parent[a];
+        }
+    }
+    static __device__ __forceinline__ long long out_at(const AttendParams &P, const AttItem &it, int row)
+    {
+        const int node = row / P.group, h = it.head * P.group + (row - node * P.group);
+        return it.b * P.o_seq + node * P.o_node + h * P.o_head;
+    }
+    static __device__ __forceinline__ long long lse_at(const AttendParams &P, const AttItem &it, int row)
+    {
+        const int node = row / P.group;
+        return (static_cast<long long>(it.b) * P.n_nodes + node) * P.n_heads + it.head * P.group + (row - node * P.group);
+    }
+};
+
 // Stores four numbers of a finished row, and its log-sum.
-template <int DT>
-__device__ __forceinline__ void att_store(const AttendParams &P, int b, int head, int row, int c, float4 a, float m, float l)
+template <int DT, class Rows>
+__device__ __forceinline__ void att_store(const typename Rows::Params &P, const AttItem &it, int row, int c, float4 a, float m, float l)
 {
-    const int node = row / P.group, h = head * P.group + (row - node * P.group);
-    const long long at = b * P.o_seq + node * P.o_node + h * P.o_head + c;
+    const long long at = Rows::out_at(P, it, row) + c;
     const float inv = l == 0.f ? 0.f : 1.f / l;     // (nothing seen: zeros)
     store_elem<DT>(P.out, at, a.x * inv);
     store_elem<DT>(P.out, at + 1, a.y * inv);
     store_elem<DT>(P.out, at + 2, a.z * inv);
     store_elem<DT>(P.out, at + 3, a.w * inv);
-    if (P.lse && c == 0)
-        P.lse[(static_cast<long long>(b) * P.n_nodes + node) * P.n_heads + h] =
-            l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    if (P.lse && c == 0) P.lse[Rows::lse_at(P, it, row)] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 __device__ __forceinline__ float lg2f(float x) { float r; asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 // log2 of a value scale (a row without a range counts as the smallest scale, so that its probability stays in range; what is
@@ -203,9 +274,9 @@ __device__ __forceinline__ float att_factor(float m, float l, float top) { retur
 //
 // Row c of a tile of eight keys is key kappa(c): with this order (and, where a row has four 16-byte chunks, those of
 // rows 4 to 7 exchanged by two) every shared-memory load of codes touches each bank once.
-template <int DT, int D, int NB>
+template <int DT, int D, int NB, class Rows>
 __global__ void __launch_bounds__(kNarrowWarps * 32, kNarrowCtas<NB>)
-narrow_kernel(const __grid_constant__ AttendParams P)
+narrow_kernel(const __grid_constant__ typename Rows::Params P)
 {
     constexpr int MT = D / 16;                      // m16 tiles of the output
     constexpr int KS = D / 16;                      // k16 steps of the scores
@@ -221,25 +292,16 @@ narrow_kernel(const __grid_constant__ AttendParams P)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
     const int ps = 1 << P.c.page_shift;
-    const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
-    const AttCut cut = att_cut(P, items, lane);
-    if (cut.span == 0 || blockIdx.x > (cut.span - 1) / cut.per) return;    // (runs before the last one are whole)
-    uint32_t u = blockIdx.x * cut.per;
-    const uint32_t u_end = cut.span - u < cut.per ? cut.span : u + cut.per;
-    AttCursor cur = att_find(P, cut, u, items, lane);
+    typename Rows::Walk walk;
+    if (!walk.begin(P, lane)) return;
+    AttItem it;
     unsigned char *ring = s_ring + warp * STAGES * STAGE;
     auto kappa = [](int c) { return D == 128 ? c ^ ((c >> 1) & 1) : c ^ ((c >> 2) & 1); };
     auto swizzle = [](int row, int chunk) { return D == 128 ? chunk ^ ((row >> 1) & 2) : chunk; };
     const int kg = kappa(g), ka = kappa(2 * t), kb = kappa(2 * t + 1);
 
-    while (u < u_end) {
-        const AttPiece piece = att_piece(cut, cur, u_end - u);
-        if (piece.k1 <= 0) break;
-        const int k0 = piece.k0, k1 = piece.k1;
-        const int b = cur.b, len = cur.len, head = piece.item / P.n_blocks, block = piece.item - head * P.n_blocks;
-        const int row0 = block * ROWS;
-        const int prefix = P.prefix_len[b];
-        const bool whole = k0 == 0 && k1 == piece.units;
+    while (walk.template next<ROWS>(P, lane, it)) {
+        const int k0 = it.k0, k1 = it.k1, b = it.b, len = it.len, head = it.head, row0 = it.row0, prefix = it.tail;
 
         __syncthreads();                            // the shared memory of the item before is free
         // this warp's chunks: keys [128 k + 32 warp, + 32) for k = k0 .. k1 - 1, as far as there are keys
@@ -287,14 +349,7 @@ narrow_kernel(const __grid_constant__ AttendParams P)
 #pragma unroll
         for (int i = 0; i < STAGES - 1; ++i) issue(i, i);
 
-        if (tid < ROWS) {
-            for (int i = 0; i * 32 < P.n_nodes; ++i) s_seen[tid][i] = 0u;
-            int a = row0 + tid < P.n_rows ? (row0 + tid) / P.group : -1;
-            while (a >= 0) {
-                s_seen[tid][a >> 5] |= 1u << (a & 31);
-                a = P.parent[a];
-            }
-        }
+        if (tid < ROWS) Rows::see(P, it, row0 + tid, s_seen[tid]);
         // queries: this lane's D / 4 numbers of row g of every tile, scaled to the top of half's range
         uint32_t qb[NB][KS][2];
         float ra[NB][2], rb[NB][2];                 // of rows 2 t and 2 t + 1: log2 units per unit of an accumulator, and per unit of mid - 8 scale
@@ -304,9 +359,8 @@ narrow_kernel(const __grid_constant__ AttendParams P)
             float x[D / 4];
 #pragma unroll
             for (int i = 0; i < D / 4; ++i) x[i] = 0.f;
-            if (r < P.n_rows) {
-                const int node = r / P.group, h = head * P.group + (r - node * P.group);
-                const long long at = b * P.q_seq + node * P.q_node + h * P.q_head + t * (D / 4);
+            if (r < it.rows) {
+                const long long at = Rows::q_at(P, it, r) + t * (D / 4);
                 if (P.q_vec) {
                     const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + at * 2);
 #pragma unroll
@@ -551,10 +605,10 @@ narrow_kernel(const __grid_constant__ AttendParams P)
             }
         __syncthreads();
         // the four warps' results joined: D / 4 threads a row, four numbers each
-        float *part = P.part + static_cast<long long>(2 * blockIdx.x + (k0 > 0 ? 0 : 1)) * part_floats(ROWS, D);
+        float *part = P.part + att_slot(k0) * part_floats(ROWS, D);
         for (int x = tid; x < ROWS * (D / 4); x += kNarrowWarps * 32) {
             const int r = x / (D / 4), c = (x % (D / 4)) * 4;
-            if (row0 + r >= P.n_rows) break;
+            if (row0 + r >= it.rows) break;
             float m = kNoTop;
 #pragma unroll
             for (int w = 0; w < kNarrowWarps; ++w) m = fmaxf(m, s_top[w][r]);
@@ -567,16 +621,13 @@ narrow_kernel(const __grid_constant__ AttendParams P)
                 l = fmaf(f, s_sum[w][r], l);
                 a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
             }
-            if (whole) {
-                att_store<DT>(P, b, head, row0 + r, c, a, m, l);
+            if (it.whole) {
+                att_store<DT, Rows>(P, it, row0 + r, c, a, m, l);
             } else {
                 *reinterpret_cast<float4 *>(part + r * D + c) = a;
                 if (c == 0) { part[ROWS * D + r] = m; part[ROWS * (D + 1) + r] = l; }
             }
         }
-        u += piece.places;
-        cur.at += piece.places;
-        if (u < u_end && cur.at >= cur.places * items) cur = att_find(P, cut, u, items, lane);
     }
 }
 
@@ -595,7 +646,10 @@ join_kernel(const __grid_constant__ AttendParams P)
     const int first = static_cast<int>(u0 / cut.per), last = static_cast<int>((u0 + units - 1) / cut.per);
     asm volatile("griddepcontrol.wait;" ::: "memory");   // (every thread: this kernel must not end before the one it follows)
     if (units == 0 || first == last) return;
-    const int head = item / P.n_blocks, row0 = (item - head * P.n_blocks) * ROWS, r0 = blockIdx.y * 8;
+    AttItem it = {};
+    it.b = b;
+    it.head = item / P.n_blocks;
+    const int row0 = (item - it.head * P.n_blocks) * ROWS, r0 = blockIdx.y * 8;
     auto part_of = [&](int cta) { return P.part + static_cast<long long>(2 * cta + (cta == first ? 1 : 0)) * part_floats(ROWS, D); };
     for (int x = tid; x < 8 * (D / 4); x += 128) {
         const int r = r0 + x / (D / 4), c = (x % (D / 4)) * 4;
@@ -613,7 +667,7 @@ join_kernel(const __grid_constant__ AttendParams P)
             l = fmaf(f, lk, l);
             a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
         }
-        att_store<DT>(P, b, head, row0 + r, c, a, m, l);
+        att_store<DT, TreeRows>(P, it, row0 + r, c, a, m, l);
     }
 }
 

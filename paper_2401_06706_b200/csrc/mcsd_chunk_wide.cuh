@@ -1,0 +1,519 @@
+// Attention of chunks with many rows per key/value head: two tiles of 128 rows a block on the tcgen05 tensor cores.
+#pragma once
+
+#include "mcsd_attend_wide.cuh"
+#include "mcsd_chunk.cuh"
+
+namespace mcsd {
+
+#define MCSD_INLINE __attribute__((always_inline))
+
+constexpr int kChunkRows = 256;                     // rows of a block: tiles A and B of 128
+constexpr int kChunkThreads = 640;                  // 8 softmax warps, 8 decoding warps, 2 that issue (and 2 beside them)
+constexpr float kChunkHead = 7.f;                   // log2 of a row's largest weight: half holds 2^15, a weight may exceed it by 2^kNarrowSlack, and by 16 (below)
+template <int D> constexpr int kChunkAhead = D == 128 ? 1 : 3;         // units whose codes are on their way to shared memory
+template <int D> constexpr int kChunkSmem = 1024 + 6 * kWideTile<D> + 2 * kAttUnit * 8 + kChunkAhead<D> * kAttUnit * (D + 8);
+
+// D (tensor memory) (+)= A (shared memory, 128 rows x 16) * B (shared memory), halves in, float32 out.
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t high, uint32_t idesc, bool add) {
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\telect.sync _|e, 0xffffffff;\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}"
+                 ::"r"(d), "r"(a_low), "r"(b_low), "r"(high), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+}
+
+// Four codes of a value row as numbers: two nibbles of every byte pair, `odd` the higher ones. 1024 + c (or 1024 + 16 c) has the code in
+// its lowest bits; both lines below are exact, the last rounds scale (c - 8) + mid once.
+template <bool odd>
+__device__ __forceinline__ __half2 value_pair(uint32_t w, __half2 scale, __half2 mid)
+{
+    const uint32_t bits = (w & (odd ? 0x00f000f0u : 0x000f000fu)) | 0x64006400u;
+    const __half2 c = *reinterpret_cast<const __half2 *>(&bits);
+    const __half2 n = odd ? __hfma2(c, __float2half2_rn(0.0625f), __float2half2_rn(-72.f)) : __hsub2(c, __float2half2_rn(1032.f));
+    return __hfma2(n, scale, mid);
+}
+
+template <int DT, int D>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+chunk_wide_kernel(const __grid_constant__ ChunkParams P)
+{
+    constexpr int TILE = kWideTile<D>, RB = D / 2, AHEAD = kChunkAhead<D>;
+    constexpr uint32_t kS = 0, kO = 256, kColumns = 512;                // P of a tile: over its S, one half of the keys after the other
+    extern __shared__ unsigned char s_raw[];
+    __shared__ __align__(8) unsigned long long s_bar[21];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_dead;
+    __shared__ uint32_t s_valid[2][4], s_bad[2][4], s_far[2][4];        // keys of a stage that are there; values that are no numbers, or far from one
+    // Each warp goes over the CTA's blocks for itself; where it stands is kept here, since registers are short.
+    __shared__ ChunkRows::Walk s_walk[kChunkThreads / 32];
+    __shared__ AttItem s_item[kChunkThreads / 32];
+    __shared__ int s_any;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+    unsigned char *base = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
+    unsigned char *s_q = base, *s_k = base + 2 * TILE, *s_v = base + 4 * TILE;  // Q of both tiles, two stages each of keys and values
+    float4 *s_param = reinterpret_cast<float4 *>(base + 6 * TILE);              // [stages][64 pairs of keys]
+    unsigned char *s_codes = reinterpret_cast<unsigned char *>(s_param + 2 * (kAttUnit / 2));   // [decoding warps][AHEAD]{codes, parameters}
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t bars = smem_u32(s_bar);
+    const uint32_t b_kfull = bars, b_kempty = bars + 16, b_vfull = bars + 32, b_vempty = bars + 48, b_s = bars + 64, b_ready = bars + 80,
+                   b_p = bars + 96, b_o = bars + 128, b_end = bars + 160;       // b_p, b_o: [tile][half of the keys]
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(b_kfull + 8 * i, 4);          // (arrivals of warps)
+            mbar_init(b_kempty + 8 * i, 10);        // the products of both tiles, and the softmax warps, which read the parameters
+            mbar_init(b_vfull + 8 * i, 4);
+            mbar_init(b_vempty + 8 * i, 2);
+            mbar_init(b_s + 8 * i, 1);
+            mbar_init(b_ready + 8 * i, 4 + P.test_extra);       // (0 but in a test of the expiry path: arrivals that never come)
+            for (int h = 0; h < 2; ++h) {
+                mbar_init(b_p + 16 * i + 8 * h, 4);
+                mbar_init(b_o + 16 * i + 8 * h, 1);
+            }
+        }
+        mbar_init(b_end, 2);
+        fence_mbar_init();
+        s_dead = 0;
+    }
+    if (warp == 16) tmem_alloc(smem_u32(&s_tmem), kColumns);
+    if (warp == 17) {
+        ChunkRows::Walk walk;
+        const bool any = walk.begin(P, lane);
+        if (lane == 0) s_any = any;
+        if (any && lane < kChunkThreads / 32) s_walk[lane] = walk;
+    }
+    tc_before_sync();
+    __syncthreads();
+    tc_after_sync();
+    constexpr uint32_t tmem = 0;
+    volatile int *dead = &s_dead;
+    if (s_tmem != tmem) *dead = 1;                  // (cannot be: all columns are this CTA's)
+
+    const int ps = 1 << P.c.page_shift;
+    // Every role goes over the same blocks.
+    auto for_items = [&](auto f) MCSD_INLINE {
+        if (!s_any) return;
+        for (;;) {
+            int more = 0;
+            __syncwarp();
+            if (lane == 0) more = s_walk[warp].template next<kChunkRows>(P, lane, s_item[warp]);
+            if (!__shfl_sync(0xffffffffu, more, 0)) break;
+            __syncwarp();
+            f(s_item[warp]);
+        }
+    };
+    // Units of a block that tile x has work in: those its last row sees (its rows' tokens end before the block's where it is tile A).
+    auto tile_units = [&](const AttItem &it, int x) MCSD_INLINE {
+        const int row = min(it.row0 + 128 * x + 127, it.rows - 1);
+        if (it.row0 + 128 * x >= it.rows) return 0;
+        const long long sees = static_cast<long long>(it.tail) + row / P.group - it.row0 / P.group;
+        return chunk_units(static_cast<int>(min(sees, static_cast<long long>(it.len))));
+    };
+
+    if (warp >= 8 && warp < 16) {
+        // ------------------------------------------------------------ decoding
+        regs_down<56>();
+        // Four warps have the key rows of every unit, four the value rows, 32 each: lane by lane, 16 bytes of codes at
+        // 16 (lane + 32 i) of the rows of sixteen keys, so that a load is contiguous, and the parameters of key `lane`.
+        constexpr int CH = RB / 16;                 // 16-byte chunks of a row: 2 or 4
+        const int which = (warp >> 2) & 1, key0 = (warp & 3) * 32;       // which: 0 key rows, 1 value rows
+        const int c = lane % CH;
+        const uint32_t full = which ? b_vfull : b_kfull, empty = which ? b_vempty : b_kempty;
+        unsigned char *ring = s_codes + (warp & 7) * AHEAD * 32 * (RB + 4);
+        int stage = 0;
+        uint32_t phase = 1;                         // (the first round of stages is free)
+        for_items([&](const AttItem &it) MCSD_INLINE {
+            const int len = it.len, k1 = it.k1;
+            const int32_t *table = P.table + it.b * P.ld_table;
+            const unsigned char *pool = P.c.pages + static_cast<long long>(it.head) * kv_block_bytes(D, ps);
+            // page of this lane's half (lanes 0..15: the first sixteen keys)
+            auto page_of = [&](int k) MCSD_INLINE {
+                const int pos = k * kAttUnit + key0 + (lane & 16);
+                return k < k1 && pos < len ? __ldg(table + (pos >> P.c.page_shift)) : -1;
+            };
+            uint32_t there = 0u;                    // bit `slot`: this lane's key of that unit is in the cache
+            int page = -1;                          // of the unit asked for next
+            auto issue = [&](int unit, int slot) MCSD_INLINE {
+                const int pos = unit * kAttUnit + key0 + lane;
+                unsigned char *to = ring + slot * 32 * (RB + 4);
+                if (unit < k1) {
+                    const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(P.c.n_pages) && pos < len;
+                    there = (there & ~(1u << slot)) | static_cast<uint32_t>(ok) << slot;
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const int p = __shfl_sync(0xffffffffu, page, 16 * hf);
+                        if (static_cast<unsigned>(p) < static_cast<unsigned>(P.c.n_pages)) {
+                            const unsigned char *src = pool + p * P.c.page_stride + (which * ps + ((unit * kAttUnit + key0 + 16 * hf) & (ps - 1))) * RB + lane * 16;
+#pragma unroll
+                            for (int i = 0; i < CH / 2; ++i) cp_async16(smem_u32(to + (hf * (CH / 2) + i) * 512 + lane * 16), src + 512 * i);
+                        }
+                    }
+                    if (ok) cp_async4(to + 32 * RB + lane * 4, pool + page * P.c.page_stride + ps * D + (which * ps + (pos & (ps - 1))) * 4);
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+            int pages[AHEAD + 1];
+#pragma unroll
+            for (int i = 0; i <= AHEAD; ++i) pages[i] = page_of(it.k0 + i);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                page = pages[i];
+                issue(it.k0 + i, i);
+            }
+            page = pages[AHEAD];
+            int slot = 0;
+            for (int k = it.k0; k < k1; ++k) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+                unsigned char *from = ring + slot * 32 * (RB + 4);
+                // what this lane copied itself: its codes, and the parameters of its key
+                uint4 code[CH];
+#pragma unroll
+                for (int i = 0; i < CH; ++i) code[i] = *reinterpret_cast<const uint4 *>(from + i * 512 + lane * 16);
+                const bool mine = (there >> slot) & 1u;
+                const uint32_t raw = *reinterpret_cast<const uint32_t *>(from + 32 * RB + lane * 4);
+                issue(k + AHEAD, slot);
+                page = page_of(k + AHEAD + 1);      // (in flight until the next unit is asked for)
+                slot = slot == AHEAD - 1 ? 0 : slot + 1;
+                wide_wait(empty + 8 * stage, phase, dead, P.wait_polls);
+                const float2 p = mine ? __half22float2(*reinterpret_cast<const __half2 *>(&raw)) : make_float2(0.f, 0.f);
+                unsigned char *tiles = (which ? s_v : s_k) + stage * TILE;
+                auto place = [&](int i, int j) MCSD_INLINE {            // where 16 bytes of operands go: chunk i of the lane, its word j
+                    const int key = key0 + (i / (CH / 2)) * 16 + (i % (CH / 2)) * (32 / CH) + lane / CH;
+                    const int chunk = 4 * c + j;
+                    return reinterpret_cast<uint4 *>(tiles + key * 128 + (chunk >> 3) * (kAttUnit * 128) + (((chunk & 7) ^ (key & 7)) << 4));
+                };
+                // (with four chunks a row, lanes 2 and 3 take their words in another order: no two lanes of eight meet in a bank)
+                const bool turn = CH == 4 && (c & 2);
+                auto word = [&](const uint4 &v, int j) MCSD_INLINE {
+                    return j == 0 ? (turn ? v.z : v.x) : j == 1 ? (turn ? v.w : v.y) : j == 2 ? (turn ? v.x : v.z) : (turn ? v.y : v.w);
+                };
+                if (which == 0) {
+                    // keys: codes as subnormal halves (one AND for two of them); scale and mid enter the scores in float32
+#pragma unroll
+                    for (int i = 0; i < CH; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t w = word(code[i], j), y = w >> 8;
+                            *place(i, turn ? j ^ 2 : j) = make_uint4(w & 0x000f000fu, w & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
+                        }
+                    const int key = key0 + lane;
+                    float *par = reinterpret_cast<float *>(s_param + stage * (kAttUnit / 2) + (key >> 1)) + (key & 1);
+                    par[0] = p.x;
+                    par[2] = fmaf(-8.f, p.x, p.y);
+                    const uint32_t keys = __ballot_sync(0xffffffffu, mine);
+                    if (lane == 0) s_valid[stage][warp & 3] = keys;
+                } else {
+                    // values: numbers in half, rounded once. Rows that are no numbers are marked, and zeros here; those that may leave half's
+                    // range are stored as a sixteenth and marked, and their weights are sixteen times as large
+                    const bool sound = fabsf(p.x) <= 65504.f && fabsf(p.y) <= 65504.f;
+                    const uint32_t ok = __ballot_sync(0xffffffffu, mine && sound), bad = __ballot_sync(0xffffffffu, mine && !sound);
+                    const uint32_t far = __ballot_sync(0xffffffffu, mine && sound && fmaf(8.f, fabsf(p.x), fabsf(p.y)) > 65000.f);
+                    uint32_t own = (ok >> lane) & 1u ? raw : 0u;
+                    if ((far >> lane) & 1u) own = half2_bits(p.x * 0.0625f, p.y * 0.0625f);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        const uint32_t both = __shfl_sync(0xffffffffu, own, (i / (CH / 2)) * 16 + (i % (CH / 2)) * (32 / CH) + lane / CH);
+                        const __half2 h = *reinterpret_cast<const __half2 *>(&both), scale = __low2half2(h), mid = __high2half2(h);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t w = word(code[i], j), y = w >> 8;
+                            const __half2 x[4] = {value_pair<false>(w, scale, mid), value_pair<true>(w, scale, mid), value_pair<false>(y, scale, mid),
+                                            value_pair<true>(y, scale, mid)};
+                            *place(i, turn ? j ^ 2 : j) = *reinterpret_cast<const uint4 *>(x);
+                        }
+                    }
+                    if (lane == 0) { s_bad[stage][warp & 3] = bad; s_far[stage][warp & 3] = far; }
+                }
+                fence_proxy_async();
+                warp_arrive(full + 8 * stage, lane);
+                if (++stage == 2) { stage = 0; phase ^= 1; }
+            }
+        });
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (warp >= 16) {
+        // ------------------------------------------------------------ issuing
+        regs_down<32>();
+        const int x = warp - 16;                    // the tile it issues for
+        if (x < 2) {
+            int stage = 0;
+            uint32_t phase = 0, n = 0, items = 0;   // n: units of this tile so far
+            const uint32_t q_at = tc_operand(smem_u32(s_q) + x * TILE, 16);
+            for_items([&](const AttItem &it) MCSD_INLINE {
+                const int mine = tile_units(it, x), k0 = it.k0, k1 = it.k1;
+                if (k0 < mine) {                    // (a tile without work has no queries either: nobody may run ahead of this barrier)
+                    wide_wait(b_ready + 8 * x, items & 1, dead, P.wait_polls);
+                    ++items;
+                }
+                for (int k = k0; k < k1; ++k) {
+                    const bool work = k < mine;
+                    wide_wait(b_kfull + 8 * stage, phase, dead, P.wait_polls);
+                    if (work) {
+                        // the scores overwrite the weights of the unit before: its products are done first (both barriers, so that
+                        // whoever sees the scores knows that neither is a phase behind)
+                        if (n > 0) {
+                            wide_wait(b_o + 16 * x, (n - 1) & 1, dead, P.wait_polls);
+                            wide_wait(b_o + 16 * x + 8, (n - 1) & 1, dead, P.wait_polls);
+                        }
+                        tc_after_sync();
+                        const uint32_t at = tc_operand(smem_u32(s_k) + stage * TILE, 16);
+#pragma unroll
+                        for (int s = 0; s < D / 16; ++s) {
+                            const uint32_t off = (s >> 2) * (kAttUnit * 128 / 16) + (s & 3) * 2;
+                            tc_mma_ss(tmem + kS + 128 * x, q_at + off, at + off, kOperandHigh, tc_shape(kAttUnit, false), s > 0);
+                        }
+                        tc_commit(b_s + 8 * x);
+                    }
+                    tc_commit(b_kempty + 8 * stage);
+                    wide_wait(b_vfull + 8 * stage, phase, dead, P.wait_polls);
+                    if (work) {
+                        const uint32_t at = tc_operand(smem_u32(s_v) + stage * TILE, kAttUnit * 128);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            wide_wait(b_p + 16 * x + 8 * h, n & 1, dead, P.wait_polls);
+                            tc_after_sync();
+#pragma unroll
+                            for (int s = 0; s < 4; ++s)
+                                tc_mma(tmem + kO + D * x, tmem + kS + 128 * x + 32 * h + 8 * s, at + (4 * h + s) * (16 * 128 / 16), kOperandHigh, tc_shape(D, true),
+                                       k > k0 || h > 0 || s > 0);
+                            tc_commit(b_o + 16 * x + 8 * h);
+                        }
+                        ++n;
+                    }
+                    tc_commit(b_vempty + 8 * stage);
+                    if (++stage == 2) { stage = 0; phase ^= 1; }
+                }
+            });
+            // What was issued, by both warps, ends before its memory is given back. (Where no wait expires, the softmax groups have
+            // waited for the products already; where one does, it may be the last of all, after this warp is through.)
+            tc_commit(b_end);
+            for (uint32_t i = 0; i < kWaitPolls && !__all_sync(0xffffffffu, mbar_try_wait(b_end, 0)); ++i) {}
+        }
+    } else {
+        // ------------------------------------------------------------ softmax
+        regs_up<168>();
+        const int x = warp >> 2;                    // tile
+        const int r = tid & 127;                    // row of the tile = lane of tensor memory
+        const uint32_t mine = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + mine + kS + 128 * x, t_o = tmem + mine + kO + D * x;
+        int stage = 0;
+        uint32_t phase = 0, n = 0;
+        for_items([&](const AttItem &it) MCSD_INLINE {
+            const int row = it.row0 + 128 * x + r;
+            const bool live = row < it.rows;
+            const int units = tile_units(it, x);
+            // positions this row sees (a row that is none sees what the last one does), and those that all rows of the tile see
+            const int token = min(row, it.rows - 1) / P.group - it.row0 / P.group;
+            const int sees = static_cast<int>(min(static_cast<long long>(it.tail) + token, static_cast<long long>(it.len)));
+            const int all = static_cast<int>(min(static_cast<long long>(it.tail) + min(it.row0 + 128 * x, it.rows - 1) / P.group - it.row0 / P.group, static_cast<long long>(it.len)));
+            float rho = 0.f, ra = 0.f;              // score in log2 units: ra (scale acc + (mid - 8 scale) rho)
+            const int k0 = it.k0, k1 = it.k1;
+            const bool any = k0 < units;            // (of the tile)
+            if (any) {
+                // Q to shared memory, scaled by a power of two to the top of half's range (and to a positive softmax scale), in the order that
+                // the ANDs of the keys give
+                uint4 raw[D / 8];
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) raw[c] = make_uint4(0u, 0u, 0u, 0u);
+                if (live) {
+                    const long long at = ChunkRows::q_at(P, it, row);
+                    if (P.q_vec) {
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c) raw[c] = (reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + 2 * at))[c];   // (not the read-only path: out may be q)
+                    } else {
+                        const unsigned short *src = static_cast<const unsigned short *>(P.q) + at;
+#pragma unroll
+                        for (int c = 0; c < D / 8; ++c)
+                            raw[c] = make_uint4(src[8 * c] | src[8 * c + 1] << 16, src[8 * c + 2] | src[8 * c + 3] << 16,
+                                                src[8 * c + 4] | src[8 * c + 5] << 16, src[8 * c + 6] | src[8 * c + 7] << 16);
+                    }
+                }
+                float most = 0.f, sum = 0.f;
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    float v[8];
+                    Elem<DT>::unpack(raw[c], v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { most = fmaxf(most, fabsf(v[i])); sum += v[i]; }
+                }
+                int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 126 : 0;
+                e = max(min(e, 112), -110);
+                const float up = __int_as_float((127 + 15 - e) << 23) * (P.scale < 0.f ? -1.f : 1.f);
+                ra = ldexpf(fabsf(P.scale) * 1.4426950408889634f, e - 15 + 24);
+                rho = sum * up * 5.9604644775390625e-8f;          // 2^-24
+                unsigned char *to = s_q + x * TILE + r * 128;
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {                 // eight numbers, one word of codes
+                    float v[8];
+                    Elem<DT>::unpack(raw[c], v);
+                    uint32_t out[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float f = i & 1 ? up * 0.0625f : up;
+                        out[i] = half2_bits(v[i] * f, v[i + 4] * f);
+                    }
+                    *reinterpret_cast<uint4 *>(to + (c >> 3) * (kAttUnit * 128) + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
+                }
+                fence_proxy_async();
+                tc_before_sync();
+                warp_arrive(b_ready + 8 * x, lane);
+            }
+            float ref = kNoTop, sum = 0.f;
+            for (int k = k0; k < k1; ++k) {
+                wide_wait(b_kfull + 8 * stage, phase, dead, P.wait_polls);
+                if (k < units) {
+                    const float4 *par = s_param + stage * (kAttUnit / 2);
+                    // One half of the unit's keys; see0, see1: the keys of it that this row sees, bad, far: values that are no numbers, or far from one.
+                    auto half = [&](auto plain_tag, int h, uint32_t see0, uint32_t see1) MCSD_INLINE {
+                        constexpr bool plain = decltype(plain_tag)::value;
+                        float2 y[32];
+                        float most = -INFINITY;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t acc[32];
+                            tmem_load32(t_s + 64 * h + 32 * c, acc);
+                            const uint32_t see = c ? see1 : see0;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                const float4 kp = par[32 * h + 16 * c + j];
+                                const float2 off = __fmul2_rn(make_float2(kp.z, kp.w), make_float2(rho, rho));
+                                const float2 z = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), make_float2(kp.x, kp.y), off);
+                                if (plain) {
+                                    most = max3(most, z.x, z.y);
+                                } else {
+                                    if ((see >> (2 * j)) & 1u) most = fmaxf(most, z.x);
+                                    if ((see >> (2 * j + 1)) & 1u) most = fmaxf(most, z.y);
+                                }
+                                y[16 * c + j] = z;
+                            }
+                        }
+                        const float high = most * ra;
+                        if (__any_sync(0xffffffffu, high > ref + (kChunkHead + kNarrowSlack))) {
+                            const float now = fmaxf(ref, high - kChunkHead);
+                            const float f = ex2f(ref - now);
+                            ref = now;
+                            sum *= f;
+                            if (h == 1) {           // (for the first half the products so far are done: the scores came after them)
+                                wide_wait(b_o + 16 * x, n & 1, dead, P.wait_polls);
+                                tc_after_sync();
+                            }
+                            if (k > k0 || h > 0) {
+#pragma unroll 1
+                                for (int c = 0; c < D / 8; ++c) {     // (eight columns at a time: y holds most registers)
+                                    uint32_t o[8];
+                                    __syncwarp();
+                                    tmem_load8(t_o + 8 * c, o);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                    tmem_store8(t_o + 8 * c, o);
+                                }
+                            }
+                        }
+                        float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            uint32_t w[16];
+                            const uint32_t see = c ? see1 : see0, bad = plain ? 0u : s_bad[stage][2 * h + c], far = plain ? 0u : s_far[stage][2 * h + c];
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                const float2 e = fma2(y[16 * c + j], make_float2(ra, ra), make_float2(-ref, -ref));
+                                float2 p = make_float2(ex2f(e.x), ex2f(e.y));
+                                if (!plain) {
+                                    if (!((see >> (2 * j)) & 1u)) p.x = 0.f;
+                                    if (!((see >> (2 * j + 1)) & 1u)) p.y = 0.f;
+                                }
+                                s2 = add2(s2, p);
+                                if (!plain) {       // (a value that is no number makes its rows none)
+                                    if ((far >> (2 * j)) & 1u) p.x *= 16.f;
+                                    if ((far >> (2 * j + 1)) & 1u) p.y *= 16.f;
+                                    if ((see & bad) >> (2 * j) & 1u) p.x = __int_as_float(0x7fffffff);
+                                    if ((see & bad) >> (2 * j + 1) & 1u) p.y = __int_as_float(0x7fffffff);
+                                }
+                                w[j] = half2_bits(p.x, p.y);
+                            }
+                            __syncwarp();
+                            tmem_store16(t_s + 32 * h + 16 * c, w);
+                        }
+                        sum += s2.x + s2.y;
+                        tc_wait_st();
+                    };
+                    wide_wait(b_s + 8 * x, n & 1, dead, P.wait_polls);
+                    tc_after_sync();
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        const int pos0 = k * kAttUnit + 64 * h;
+                        const uint32_t there0 = s_valid[stage][2 * h], there1 = s_valid[stage][2 * h + 1];
+                        if (h == 0) wide_wait(b_vfull + 8 * stage, phase, dead, P.wait_polls);   // (the marks of the values)
+                        const uint32_t odd = s_bad[stage][2 * h] | s_bad[stage][2 * h + 1] | s_far[stage][2 * h] | s_far[stage][2 * h + 1];
+                        if ((there0 & there1) == 0xffffffffu && odd == 0u && pos0 + 64 <= all) {
+                            half(std::true_type(), h, 0u, 0u);
+                        } else {
+                            auto first = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
+                            half(std::false_type(), h, there0 & first(sees - pos0), there1 & first(sees - pos0 - 32));
+                        }
+                        tc_before_sync();
+                        warp_arrive(b_p + 16 * x + 8 * h, lane);
+                    }
+                    ++n;
+                }
+                warp_arrive(b_kempty + 8 * stage, lane);        // the parameters are read
+                if (++stage == 2) { stage = 0; phase ^= 1; }
+            }
+            // ---- the end of the block
+            if (any) wide_wait(b_o + 16 * x + 8, (n - 1) & 1, dead, P.wait_polls);
+            tc_after_sync();
+            float l = sum;
+            if (*dead) l = __int_as_float(0x7fffffff);
+            const float inv = l == 0.f ? 0.f : 1.f / l;         // (nothing seen: zeros)
+            const int at_row = 128 * x + r;
+            const long long out = live ? ChunkRows::out_at(P, it, row) : 0;
+            float *part = P.part + att_slot(it.k0) * part_floats(kChunkRows, D);
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t o[16];
+                __syncwarp();
+                tmem_load16(t_o + 16 * c, o);
+                if (live) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 8) {           // eight columns: one word's codes, in the operands' order
+                        float v[8];
+#pragma unroll
+                        for (int p = 0; p < 8; ++p) v[(p >> 1) + 4 * (p & 1)] = any ? __uint_as_float(o[i + p]) : 0.f;
+                        if (it.whole) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) v[e] *= inv;
+                            if (P.o_vec) {
+                                *reinterpret_cast<uint4 *>(static_cast<char *>(P.out) + 2 * (out + 16 * c + i)) = pack_elems<DT>(v);
+                            } else {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) store_elem<DT>(P.out, out + 16 * c + i + e, v[e]);
+                            }
+                        } else {
+                            float4 *to = reinterpret_cast<float4 *>(part + at_row * D + 16 * c + i);
+                            to[0] = make_float4(v[0], v[1], v[2], v[3]);
+                            to[1] = make_float4(v[4], v[5], v[6], v[7]);
+                        }
+                    }
+                }
+            }
+            if (live) {
+                if (!it.whole) {
+                    part[kChunkRows * D + at_row] = ref;
+                    part[kChunkRows * (D + 1) + at_row] = l;
+                } else if (P.lse) {
+                    P.lse[ChunkRows::lse_at(P, it, row)] = l == 0.f ? -INFINITY : (ref + log2f(l)) * 0.6931471805599453f;
+                }
+            }
+            __syncwarp();
+            tc_before_sync();
+        });
+    }
+    tc_before_sync();
+    __syncthreads();
+    if (warp == 16) {
+        tc_after_sync();
+        tmem_free(tmem, kColumns);
+    }
+}
+
+#undef MCSD_INLINE
+
+}  // namespace mcsd

@@ -171,9 +171,9 @@ int launch_with_join(int threads, int smem, const AttendParams &p, cudaStream_t 
 template <int DT, int D>
 int launch_attention(const AttendParams &p, int rows, cudaStream_t st)
 {
-    if (rows == 8) return launch_with_join<DT, D, 8, narrow_kernel<DT, D, 1>>(kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
-    if (rows == 16) return launch_with_join<DT, D, 16, narrow_kernel<DT, D, 2>>(kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
-    if (rows == 24) return launch_with_join<DT, D, 24, narrow_kernel<DT, D, 3>>(kNarrowWarps * 32, kNarrowSmem<D, 3>, p, st);
+    if (rows == 8) return launch_with_join<DT, D, 8, narrow_kernel<DT, D, 1, TreeRows>>(kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
+    if (rows == 16) return launch_with_join<DT, D, 16, narrow_kernel<DT, D, 2, TreeRows>>(kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
+    if (rows == 24) return launch_with_join<DT, D, 24, narrow_kernel<DT, D, 3, TreeRows>>(kNarrowWarps * 32, kNarrowSmem<D, 3>, p, st);
     return launch_with_join<DT, D, kWideRows, wide_kernel<DT, D>>(kWideThreads, kWideSmem<D>, p, st);
 }
 

@@ -3,6 +3,7 @@
 #include <cmath>
 
 #include "mcsd_chunk.cuh"
+#include "mcsd_chunk_wide.cuh"
 #include "mcsd_evict.cuh"
 #include "mcsd_launch.cuh"
 #include "mcsd_logprobs.cuh"
@@ -35,15 +36,84 @@ ChunkParams chunk_params(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache, c
     p.batch = d->batch; p.n_heads = d->n_heads; p.max_pages = d->max_pages; p.max_new = d->max_new;
     p.group = d->n_heads / cache->n_heads;
     p.scale = d->scale;
+    p.q_vec = (reinterpret_cast<uintptr_t>(q) | 2ull * static_cast<unsigned long long>(d->q_token_stride | d->q_head_stride)) % 16 == 0;
     return p;
 }
 
-template <int DT, int D>
-int launch_chunk(const ChunkParams &p, cudaStream_t st)
+// How a call is laid out; depends on the sizes only.
+struct ChunkPlan {
+    int narrow;     // rows of the narrow kernel's blocks, 0: it is not needed
+    bool wide;
+    int most;       // rows of a sequence up to which it is the narrow kernel's (of a call that has both)
+    int ctas[2];    // CTAs the work of the narrow and of the wide kernel is cut for
+};
+ChunkPlan chunk_plan(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache, bool may_mix)
 {
-    const unsigned z = static_cast<unsigned>(p.max_new < 8 ? 1 : p.max_new > 512 ? 64 : p.max_new / 8);
-    chunk_kernel<DT, D><<<dim3(p.n_heads, p.batch < 65535 ? p.batch : 65535, z), 256, 0, st>>>(p);
-    return launched(1);
+    ChunkPlan plan = {};
+    int sms = sm_count();
+    if (sms <= 0) sms = 148;
+    const int group = d->n_heads / cache->n_heads;
+    const long long rows = static_cast<long long>(d->max_new) * group;
+    // rows of a sequence that the narrow kernel is for: one token's, or what a block or two of 24 hold
+    const int narrow = group <= 8 ? 8 : group <= 16 ? 16 : group <= 24 ? 24 : 0;
+    if (rows <= 48 && narrow) {
+        plan.narrow = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 24 ? 24 : rows <= 32 && group <= 16 ? 16 : 24;
+        plan.most = 48;
+    } else {
+        plan.wide = true;
+        if (may_mix && narrow) {
+            plan.narrow = narrow;
+            plan.most = narrow;
+        }
+    }
+    plan.ctas[0] = plan.narrow ? sms * (plan.narrow == 8 ? kNarrowCtas<1> : plan.narrow == 16 ? kNarrowCtas<2> : kNarrowCtas<3>) : 0;
+    plan.ctas[1] = plan.wide ? sms : 0;
+    return plan;
+}
+
+// Launches the kernel that does the work and, as its programmatic dependent, the one that joins divided blocks.
+template <int DT, int D, int ROWS, auto Kernel>
+int launch_with_join(int threads, int smem, const ChunkParams &p, cudaStream_t st)
+{
+    if (!allow_smem<Kernel>(smem)) return MCSD_ERR_CUDA;
+    Kernel<<<p.n_ctas, threads, smem, st>>>(p);
+    if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
+    if (p.n_ctas < 2) return MCSD_OK;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.n_ctas - 1), ROWS / 8);
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, chunk_join_kernel<DT, D, ROWS>, p) == cudaSuccess ? MCSD_OK : MCSD_ERR_CUDA;
+}
+
+template <int DT, int D>
+int launch_chunk(ChunkParams p, const ChunkPlan &plan, cudaStream_t st)
+{
+    int rc = MCSD_OK;
+    if (plan.wide) {
+        p.tokens = kChunkRows / p.group;
+        p.least = plan.narrow ? plan.most + 1 : 0;
+        p.most = 0x7fffffff;
+        p.lead = 256;
+        p.n_ctas = plan.ctas[1];
+        rc = launch_with_join<DT, D, kChunkRows, chunk_wide_kernel<DT, D>>(kChunkThreads, kChunkSmem<D>, p, st);
+    }
+    if (plan.narrow && rc == MCSD_OK) {
+        p.tokens = plan.narrow / p.group;
+        p.least = 0;
+        p.most = plan.wide ? plan.most : 0x7fffffff;
+        p.lead = plan.narrow == 8 ? 256 : 512;
+        p.n_ctas = plan.ctas[0];
+        if (plan.narrow == 8) rc = launch_with_join<DT, D, 8, narrow_kernel<DT, D, 1, ChunkRows>>(kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
+        else if (plan.narrow == 16) rc = launch_with_join<DT, D, 16, narrow_kernel<DT, D, 2, ChunkRows>>(kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
+        else rc = launch_with_join<DT, D, 24, narrow_kernel<DT, D, 3, ChunkRows>>(kNarrowWarps * 32, kNarrowSmem<D, 3>, p, st);
+    }
+    return rc == MCSD_OK ? launched(plan.wide && plan.narrow ? 4 : 2) : rc;
 }
 
 template <int DT, int D>
@@ -63,7 +133,10 @@ extern "C" {
 size_t mcsd_chunk_attention_workspace_bytes(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache)
 {
     if (check_chunk(desc, cache) != MCSD_OK) return 0;
-    return 256;
+    const ChunkPlan plan = chunk_plan(desc, cache, true);
+    const size_t narrow = static_cast<size_t>(plan.ctas[0]) * part_floats(plan.narrow, cache->head_dim);
+    const size_t wide = static_cast<size_t>(plan.ctas[1]) * part_floats(kChunkRows, cache->head_dim);
+    return (2 * sizeof(float) * (narrow > wide ? narrow : wide) + 255) / 256 * 256;
 }
 
 int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table, const int32_t *start,
@@ -86,10 +159,20 @@ int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache
     ChunkParams p = chunk_params(desc, cache, page_table, start, cu_tokens, q);
     p.out = out;
     p.lse = lse;
+    p.part = static_cast<float *>(desc->workspace);
+    p.o_vec = (reinterpret_cast<uintptr_t>(out) | 2ull * static_cast<unsigned long long>(desc->out_token_stride | desc->out_head_stride)) % 16 == 0;
+    const int polls = mcsd_get_option(MCSD_OPT_WAIT_POLLS);
+    p.wait_polls = polls > 0 ? static_cast<uint32_t>(polls) : kWaitPolls;
+    p.test_extra = mcsd_get_option(MCSD_OPT_TEST_EXTRA_TX) > 0 ? 1u : 0u;
+    // Sequences with a token or so get the narrow kernel beside long chunks only where there can be many of them.
+    const ChunkPlan plan = chunk_plan(desc, cache, desc->n_tokens < static_cast<int64_t>(desc->batch) * desc->max_new / 2);
+    // (the cut counts places of all blocks in 64 bits)
+    const double blocks = static_cast<double>(desc->n_tokens) + desc->batch;
+    if (blocks * cache->n_heads * (static_cast<double>(desc->max_pages) * cache->page_size + desc->max_new + 1024.0) > 4e18) return MCSD_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(desc->stream);
     const bool bf = desc->dtype == MCSD_DTYPE_BF16;
-    if (cache->head_dim == 128) return bf ? launch_chunk<MCSD_DTYPE_BF16, 128>(p, st) : launch_chunk<MCSD_DTYPE_F16, 128>(p, st);
-    return bf ? launch_chunk<MCSD_DTYPE_BF16, 64>(p, st) : launch_chunk<MCSD_DTYPE_F16, 64>(p, st);
+    if (cache->head_dim == 128) return bf ? launch_chunk<MCSD_DTYPE_BF16, 128>(p, plan, st) : launch_chunk<MCSD_DTYPE_F16, 128>(p, plan, st);
+    return bf ? launch_chunk<MCSD_DTYPE_BF16, 64>(p, plan, st) : launch_chunk<MCSD_DTYPE_F16, 64>(p, plan, st);
 }
 
 int mcsd_accumulate_weights(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table, const int32_t *start,
