@@ -123,6 +123,24 @@ int launch_weigh(const ChunkParams &p, cudaStream_t st)
     return launched(1);
 }
 
+// Rows that leave multiprocessors idle get CTAs of 1024 threads (their latency counts), others 256, six to a multiprocessor.
+template <int DT>
+int launch_logprobs(const LogprobParams &p, bool vec, cudaStream_t st)
+{
+    const long long sms = sm_count();
+    if (sms <= 0) return MCSD_ERR_CUDA;
+    const bool few = p.n_out <= 2 * sms;
+    const unsigned grid = static_cast<unsigned>(few || p.n_out < 6 * sms ? p.n_out : 6 * sms);
+    if (few) {
+        if (vec) logprob_kernel<DT, 1024, true><<<grid, 1024, 0, st>>>(p);
+        else logprob_kernel<DT, 1024, false><<<grid, 1024, 0, st>>>(p);
+    } else {
+        if (vec) logprob_kernel<DT, 256, true><<<grid, 256, 0, st>>>(p);
+        else logprob_kernel<DT, 256, false><<<grid, 256, 0, st>>>(p);
+    }
+    return launched(1);
+}
+
 }  // namespace
 }  // namespace mcsd
 
@@ -218,11 +236,14 @@ int mcsd_evict_rows(const mcsd_evict_desc *d, const mcsd_kv_cache *cache)
     p.n_layers = d->n_layers; p.layer_stride = d->layer_stride; p.weight_stride = d->weight_stride; p.ld_table = d->ld_table;
     p.table = d->page_table; p.len = d->len; p.keep_len = d->keep_len; p.weights = d->weights; p.len_out = d->len_out;
     p.batch = d->batch; p.max_pages = d->max_pages; p.keep = d->keep; p.sink = d->sink; p.recent = d->recent;
-    const long long items = d->n_layers * d->batch * cache->n_heads;
-    const unsigned grid = static_cast<unsigned>(items < 1 << 20 ? items : 1 << 20);
+    const long long items = d->n_layers * d->batch * cache->n_heads, room = static_cast<long long>(d->max_pages) * cache->page_size;
+    const int sms = sm_count();
+    if (sms <= 0) return MCSD_ERR_CUDA;
+    p.n_keys = static_cast<int>(room < kEvictKeys ? room : kEvictKeys);
+    const unsigned grid = static_cast<unsigned>(items < 4LL * sms ? items : 4LL * sms);
     cudaStream_t st = static_cast<cudaStream_t>(d->stream);
-    if (cache->head_dim == 128) evict_kernel<128><<<grid, kEvictThreads, 0, st>>>(p);
-    else evict_kernel<64><<<grid, kEvictThreads, 0, st>>>(p);
+    if (cache->head_dim == 128) evict_kernel<128><<<grid, kEvictThreads, 4 * p.n_keys, st>>>(p);
+    else evict_kernel<64><<<grid, kEvictThreads, 4 * p.n_keys, st>>>(p);
     return launched(1);
 }
 
@@ -248,14 +269,14 @@ int mcsd_token_logprobs(const mcsd_logprob_desc *d)
     p.logprobs = d->n_given > 0 ? d->logprobs : nullptr; p.entropy = d->entropy; p.top_ids = d->top_ids; p.top_logprobs = d->top_logprobs;
     p.V = d->vocab; p.n_given = d->n_given; p.n_top = d->top_ids || d->top_logprobs ? d->n_top : 0; p.path_len = d->path_len; p.nodes_per_tree = d->nodes_per_tree;
     p.inv_t = 1.f / d->temperature;
-    const unsigned grid = static_cast<unsigned>(d->n_out < 1 << 20 ? d->n_out : 1 << 20);
+    p.scale = 1.4426950408889634f / d->temperature;
+    const bool vec = (reinterpret_cast<uintptr_t>(d->logits) | static_cast<unsigned long long>(elem_size(d->dtype)) * static_cast<unsigned long long>(d->ld)) % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(d->stream);
     switch (d->dtype) {
-    case MCSD_DTYPE_F32: logprob_kernel<MCSD_DTYPE_F32><<<grid, kLogprobThreads, 0, st>>>(p); break;
-    case MCSD_DTYPE_BF16: logprob_kernel<MCSD_DTYPE_BF16><<<grid, kLogprobThreads, 0, st>>>(p); break;
-    default: logprob_kernel<MCSD_DTYPE_F16><<<grid, kLogprobThreads, 0, st>>>(p); break;
+    case MCSD_DTYPE_F32: return launch_logprobs<MCSD_DTYPE_F32>(p, vec, st);
+    case MCSD_DTYPE_BF16: return launch_logprobs<MCSD_DTYPE_BF16>(p, vec, st);
+    default: return launch_logprobs<MCSD_DTYPE_F16>(p, vec, st);
     }
-    return launched(1);
 }
 
 }  // extern "C"
