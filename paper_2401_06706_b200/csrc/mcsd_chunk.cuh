@@ -269,55 +269,4 @@ chunk_join_kernel(const __grid_constant__ ChunkParams P)
     }
 }
 
-// This lane's D / 32 numbers of the key (0) or value (1) row at `pos`; false if there is none.
-template <int D>
-__device__ __forceinline__ bool chunk_row(const CacheParams &c, const int32_t *table, int pos, int head, int which, int lane, float *x)
-{
-    const int page = table[pos >> c.page_shift];
-    if (page < 0 || page >= c.n_pages) return false;
-    unsigned char *codes;
-    __half2 *param;
-    kv_row<D>(c, (static_cast<long long>(page) << c.page_shift) + (pos & ((1 << c.page_shift) - 1)), head, which, codes, param);
-    const float2 p = __half22float2(*param);
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        const int d = lane * (D / 32) + i;
-        x[i] = fmaf(p.x, static_cast<float>((codes[d >> 1] >> (4 * (d & 1))) & 15) - 8.f, p.y);
-    }
-    return true;
-}
-
-// A warp per (position, key head).
-template <int DT, int D>
-__global__ void __launch_bounds__(256)
-weigh_kernel(const __grid_constant__ ChunkParams P)
-{
-    const int lane = threadIdx.x & 31, head = blockIdx.x, ps = 1 << P.c.page_shift;
-    for (int b = blockIdx.y; b < P.batch; b += gridDim.y) {
-        const ChunkSeq s = chunk_seq(P, b);
-        const int32_t *table = P.table + b * P.ld_table;
-        if (s.count == 0) continue;
-        const int first = P.last > 0 ? max(s.count - P.last, 0) : 0;
-        for (int pos = blockIdx.z * 8 + (threadIdx.x >> 5); pos < s.len; pos += gridDim.z * 8) {
-            float k[D / 32];
-            if (!chunk_row<D>(P.c, table, pos, head, 0, lane, k)) continue;
-            float sum = 0.f;
-            for (int i = max(first, pos - s.start); i < s.count; ++i)
-                for (int h = head * P.group; h < (head + 1) * P.group; ++h) {
-                    const long long at = (s.row + i) * P.q_token + h * P.q_head + lane * (D / 32);
-                    float z = 0.f;
-#pragma unroll
-                    for (int d = 0; d < D / 32; ++d) z = fmaf(load_elem<DT>(P.q, at + d), k[d], z);
-                    z = warp_sum(z) * P.scale;
-                    const float lse = P.lse[(s.row + i) * P.n_heads + h];
-                    if (lse != -INFINITY) sum += expf(z - lse);
-                }
-            if (lane == 0) {
-                float *w = P.weights + (static_cast<long long>(table[pos >> P.c.page_shift]) * P.c.n_heads + head) * ps + (pos & (ps - 1));
-                *w = pos < s.start && P.decay != 0.f ? fmaf(P.decay, *w, sum) : sum;
-            }
-        }
-    }
-}
-
 }  // namespace mcsd

@@ -65,7 +65,7 @@ __device__ __forceinline__ LogprobSums join_sums(const LogprobSums &a, const Log
 // Sums of a thread (V / THREADS terms) and their joining are float32: an error of 2^-22 of the result or so; a distance from the maximum
 // is formed before it is scaled, so that the lowest finite logits (a mask) do not overflow against one another.
 template <int DT, int THREADS, bool VEC>
-__global__ void __launch_bounds__(THREADS, 2048 / THREADS > 6 ? 6 : 2048 / THREADS)
+__global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : 6)
 logprob_kernel(const __grid_constant__ LogprobParams P)
 {
     typedef Elem<DT> E;

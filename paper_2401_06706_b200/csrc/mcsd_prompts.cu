@@ -7,6 +7,7 @@
 #include "mcsd_evict.cuh"
 #include "mcsd_launch.cuh"
 #include "mcsd_logprobs.cuh"
+#include "mcsd_weigh.cuh"
 
 namespace mcsd {
 namespace {
@@ -20,6 +21,10 @@ int check_chunk(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache)
     if (d->n_heads % cache->n_heads != 0) return MCSD_ERR_SHAPE;
     if (d->n_heads / cache->n_heads > MCSD_MAX_GROUP || d->max_new > 1 << 24 || d->n_tokens > 0x7fffffffLL) return MCSD_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(d->max_pages) * cache->page_size > 0x7fffffffLL - 512) return MCSD_ERR_UNSUPPORTED;
+    // (the cuts count places of all blocks, and of all units with their rows, in 64 bits)
+    const double room = static_cast<double>(d->max_pages) * cache->page_size + d->max_new + 1024.0;
+    if ((static_cast<double>(d->n_tokens) + d->batch) * cache->n_heads * room > 4e18) return MCSD_ERR_UNSUPPORTED;
+    if (static_cast<double>(d->batch) * d->n_heads * room * (static_cast<double>(d->max_new) + 64.0) > 4e18) return MCSD_ERR_UNSUPPORTED;
     if (d->dtype != MCSD_DTYPE_BF16 && d->dtype != MCSD_DTYPE_F16) return MCSD_ERR_DTYPE;
     if (d->ld_table < d->max_pages || d->q_token_stride < 0 || d->q_head_stride < 0) return MCSD_ERR_STRIDE;
     return MCSD_OK;
@@ -39,6 +44,17 @@ ChunkParams chunk_params(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache, c
     p.q_vec = (reinterpret_cast<uintptr_t>(q) | 2ull * static_cast<unsigned long long>(d->q_token_stride | d->q_head_stride)) % 16 == 0;
     return p;
 }
+
+void wait_limits(ChunkParams &p)
+{
+    const int polls = mcsd_get_option(MCSD_OPT_WAIT_POLLS);
+    p.wait_polls = polls > 0 ? static_cast<uint32_t>(polls) : kWaitPolls;
+    p.test_extra = mcsd_get_option(MCSD_OPT_TEST_EXTRA_TX) > 0 ? 1u : 0u;
+}
+
+// Whether many sequences can have far fewer tokens than the longest chunk: those get the kernel for few rows beside the one for many. (Where
+// most have as many, the second launch would be for nothing, 2 to 3 us.)
+bool mixed(const mcsd_chunk_desc *d) { return d->n_tokens < static_cast<int64_t>(d->batch) * d->max_new / 2; }
 
 // How a call is laid out; depends on the sizes only.
 struct ChunkPlan {
@@ -116,11 +132,43 @@ int launch_chunk(ChunkParams p, const ChunkPlan &plan, cudaStream_t st)
     return rc == MCSD_OK ? launched(plan.wide && plan.narrow ? 4 : 2) : rc;
 }
 
-template <int DT, int D>
-int launch_weigh(const ChunkParams &p, cudaStream_t st)
+template <int DT, int D, int NB>
+int launch_weigh_narrow(ChunkParams p, int sms, cudaStream_t st)
 {
-    weigh_kernel<DT, D><<<dim3(p.c.n_heads, p.batch < 65535 ? p.batch : 65535, 64), 256, 0, st>>>(p);
-    return launched(1);
+    if (!allow_smem<weigh_narrow_kernel<DT, D, NB>>(kWeighSmem<D>)) return MCSD_ERR_CUDA;
+    p.lead = 128;
+    p.n_ctas = sms * kWeighCtas<NB>;
+    weigh_narrow_kernel<DT, D, NB><<<p.n_ctas, kNarrowWarps * 32, kWeighSmem<D>, st>>>(p);
+    return cudaGetLastError() == cudaSuccess ? MCSD_OK : MCSD_ERR_CUDA;
+}
+
+// Sequences of few rows (their tokens that count x query heads of a key head) go to the narrow kernel, others to the wide one; a call with rows for
+// the wide one launches both only where there can be many sequences of the other kind.
+template <int DT, int D>
+int launch_weigh(ChunkParams p, bool may_mix, cudaStream_t st)
+{
+    const int sms = sm_count();
+    if (sms <= 0) return MCSD_ERR_CUDA;
+    const long long rows = static_cast<long long>(p.last > 0 && p.last < p.max_new ? p.last : p.max_new) * p.group;
+    const int narrow = rows <= 24 ? static_cast<int>(rows) : may_mix && p.group <= 24 ? p.group : 0;
+    int rc = MCSD_OK, n = 0;
+    if (rows > 24) {
+        if (!allow_smem<weigh_wide_kernel<DT, D>>(kWeighWideSmem<D>)) return MCSD_ERR_CUDA;
+        p.least = narrow ? narrow + 1 : 0;
+        p.most = 0x7fffffff;
+        p.lead = 256;
+        p.n_ctas = sms;
+        weigh_wide_kernel<DT, D><<<p.n_ctas, kWeighThreads, kWeighWideSmem<D>, st>>>(p);
+        if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
+        ++n;
+    }
+    if (narrow) {
+        p.least = 0;
+        p.most = rows > 24 ? narrow : 0x7fffffff;
+        rc = narrow <= 8 ? launch_weigh_narrow<DT, D, 1>(p, sms, st) : narrow <= 16 ? launch_weigh_narrow<DT, D, 2>(p, sms, st) : launch_weigh_narrow<DT, D, 3>(p, sms, st);
+        ++n;
+    }
+    return rc == MCSD_OK ? launched(n) : rc;
 }
 
 // Rows that leave multiprocessors idle get CTAs of 1024 threads (their latency counts), others 256, six to a multiprocessor.
@@ -179,14 +227,8 @@ int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache
     p.lse = lse;
     p.part = static_cast<float *>(desc->workspace);
     p.o_vec = (reinterpret_cast<uintptr_t>(out) | 2ull * static_cast<unsigned long long>(desc->out_token_stride | desc->out_head_stride)) % 16 == 0;
-    const int polls = mcsd_get_option(MCSD_OPT_WAIT_POLLS);
-    p.wait_polls = polls > 0 ? static_cast<uint32_t>(polls) : kWaitPolls;
-    p.test_extra = mcsd_get_option(MCSD_OPT_TEST_EXTRA_TX) > 0 ? 1u : 0u;
-    // Sequences with a token or so get the narrow kernel beside long chunks only where there can be many of them.
-    const ChunkPlan plan = chunk_plan(desc, cache, desc->n_tokens < static_cast<int64_t>(desc->batch) * desc->max_new / 2);
-    // (the cut counts places of all blocks in 64 bits)
-    const double blocks = static_cast<double>(desc->n_tokens) + desc->batch;
-    if (blocks * cache->n_heads * (static_cast<double>(desc->max_pages) * cache->page_size + desc->max_new + 1024.0) > 4e18) return MCSD_ERR_UNSUPPORTED;
+    wait_limits(p);
+    const ChunkPlan plan = chunk_plan(desc, cache, mixed(desc));
     cudaStream_t st = static_cast<cudaStream_t>(desc->stream);
     const bool bf = desc->dtype == MCSD_DTYPE_BF16;
     if (cache->head_dim == 128) return bf ? launch_chunk<MCSD_DTYPE_BF16, 128>(p, plan, st) : launch_chunk<MCSD_DTYPE_F16, 128>(p, plan, st);
@@ -208,10 +250,12 @@ int mcsd_accumulate_weights(const mcsd_chunk_desc *desc, const mcsd_kv_cache *ca
     p.weights = weights;
     p.decay = decay;
     p.last = last_tokens;
+    wait_limits(p);
+    const bool mix = mixed(desc);
     cudaStream_t st = static_cast<cudaStream_t>(desc->stream);
     const bool bf = desc->dtype == MCSD_DTYPE_BF16;
-    if (cache->head_dim == 128) return bf ? launch_weigh<MCSD_DTYPE_BF16, 128>(p, st) : launch_weigh<MCSD_DTYPE_F16, 128>(p, st);
-    return bf ? launch_weigh<MCSD_DTYPE_BF16, 64>(p, st) : launch_weigh<MCSD_DTYPE_F16, 64>(p, st);
+    if (cache->head_dim == 128) return bf ? launch_weigh<MCSD_DTYPE_BF16, 128>(p, mix, st) : launch_weigh<MCSD_DTYPE_F16, 128>(p, mix, st);
+    return bf ? launch_weigh<MCSD_DTYPE_BF16, 64>(p, mix, st) : launch_weigh<MCSD_DTYPE_F16, 64>(p, mix, st);
 }
 
 int mcsd_evict_rows(const mcsd_evict_desc *d, const mcsd_kv_cache *cache)
