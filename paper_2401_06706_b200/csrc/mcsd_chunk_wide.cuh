@@ -10,7 +10,8 @@ namespace mcsd {
 
 constexpr int kChunkRows = 256;                     // rows of a block: tiles A and B of 128
 constexpr int kChunkThreads = 640;                  // 8 softmax warps, 8 decoding warps, 2 that issue (and 2 beside them)
-constexpr float kChunkHead = 7.f;                   // log2 of a row's largest weight: half holds 2^15, a weight may exceed it by 2^kNarrowSlack, and by 16 (below)
+constexpr float kChunkHead = 4.f;                   // log2 of a row's largest weight when its reference is set
+constexpr float kChunkMost = 2048.f;                // sum of the weights of half a unit above which the reference moves (half holds 2^15, and 16 times this)
 template <int D> constexpr int kChunkAhead = D == 128 ? 1 : 3;         // units whose codes are on their way to shared memory
 template <int D> constexpr int kChunkSmem = 1024 + 6 * kWideTile<D> + 2 * kAttUnit * 8 + kChunkAhead<D> * kAttUnit * (D + 8);
 
@@ -20,6 +21,19 @@ __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a_low, uint32_t b
                  "@e tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}"
                  ::"r"(d), "r"(a_low), "r"(b_low), "r"(high), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
 }
+
+#define MCSD_R16(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7]), \
+    "=r"(v[i + 8]), "=r"(v[i + 9]), "=r"(v[i + 10]), "=r"(v[i + 11]), "=r"(v[i + 12]), "=r"(v[i + 13]), "=r"(v[i + 14]), "=r"(v[i + 15])
+// 64 columns of this warp's 32 lanes, lane i of the warp row i.
+__device__ __forceinline__ void tmem_load64(uint32_t at, uint32_t (&v)[64]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+                 "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+                 "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+                 "tcgen05.wait::ld.sync.aligned;"   // (in the same statement: the registers hold nothing before it)
+                 : MCSD_R16(v, 0), MCSD_R16(v, 16), MCSD_R16(v, 32), MCSD_R16(v, 48) : "r"(at) : "memory");
+}
+#undef MCSD_R16
 
 // Four codes of a value row as numbers: two nibbles of every byte pair, `odd` the higher ones. 1024 + c (or 1024 + 16 c) has the code in
 // its lowest bits; both lines below are exact, the last rounds scale (c - 8) + mid once.
@@ -37,9 +51,9 @@ __global__ void __launch_bounds__(kChunkThreads, 1)
 chunk_wide_kernel(const __grid_constant__ ChunkParams P)
 {
     constexpr int TILE = kWideTile<D>, RB = D / 2, AHEAD = kChunkAhead<D>;
-    constexpr uint32_t kS = 0, kO = 256, kColumns = 512;                // P of a tile: over its S, one half of the keys after the other
+    constexpr uint32_t kS = 0, kO = 256, kColumns = 512;                // S: 64 columns per tile and half of a unit's keys; P over the first 32 of them
     extern __shared__ unsigned char s_raw[];
-    __shared__ __align__(8) unsigned long long s_bar[21];
+    __shared__ __align__(8) unsigned long long s_bar[23];
     __shared__ uint32_t s_tmem;
     __shared__ int s_dead;
     __shared__ uint32_t s_valid[2][4], s_bad[2][4], s_far[2][4];        // keys of a stage that are there; values that are no numbers, or far from one
@@ -56,17 +70,17 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bars = smem_u32(s_bar);
-    const uint32_t b_kfull = bars, b_kempty = bars + 16, b_vfull = bars + 32, b_vempty = bars + 48, b_s = bars + 64, b_ready = bars + 80,
-                   b_p = bars + 96, b_o = bars + 128, b_end = bars + 160;       // b_p, b_o: [tile][half of the keys]
+    const uint32_t b_kfull = bars, b_kempty = bars + 16, b_vfull = bars + 32, b_vempty = bars + 48, b_ready = bars + 64, b_s = bars + 80,
+                   b_p = bars + 112, b_o = bars + 144, b_end = bars + 176;      // b_s, b_p, b_o: [tile][half of the keys]
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(b_kfull + 8 * i, 4);          // (arrivals of warps)
             mbar_init(b_kempty + 8 * i, 10);        // the products of both tiles, and the softmax warps, which read the parameters
             mbar_init(b_vfull + 8 * i, 4);
             mbar_init(b_vempty + 8 * i, 2);
-            mbar_init(b_s + 8 * i, 1);
             mbar_init(b_ready + 8 * i, 4 + P.test_extra);       // (0 but in a test of the expiry path: arrivals that never come)
             for (int h = 0; h < 2; ++h) {
+                mbar_init(b_s + 16 * i + 8 * h, 1);
                 mbar_init(b_p + 16 * i + 8 * h, 4);
                 mbar_init(b_o + 16 * i + 8 * h, 1);
             }
@@ -235,35 +249,41 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
         regs_down<32>();
         const int x = warp - 16;                    // the tile it issues for
         if (x < 2) {
-            int stage = 0;
-            uint32_t phase = 0, n = 0, items = 0;   // n: units of this tile so far
+            int stage = 0, ahead = 0;               // stages of the unit whose weights are next, and of the one whose scores are
+            uint32_t phase = 0, ahead_phase = 0, n = 0, items = 0;      // n: units of this tile so far
             const uint32_t q_at = tc_operand(smem_u32(s_q) + x * TILE, 16);
+            // Scores of half h of the unit at `ahead`, the tile's unit m: over the weights of the unit before, whose products are done first.
+            auto scores = [&](int h, uint32_t m) MCSD_INLINE {
+                if (h == 0) wide_wait(b_kfull + 8 * ahead, ahead_phase, dead, P.wait_polls);
+                if (m > 0) wide_wait(b_o + 16 * x + 8 * h, (m - 1) & 1, dead, P.wait_polls);
+                tc_after_sync();
+                const uint32_t at = tc_operand(smem_u32(s_k) + ahead * TILE + h * 64 * 128, 16);
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s) {
+                    const uint32_t off = (s >> 2) * (kAttUnit * 128 / 16) + (s & 3) * 2;
+                    tc_mma_ss(tmem + kS + 128 * x + 64 * h, q_at + off, at + off, kOperandHigh, tc_shape(64, false), s > 0);
+                }
+                tc_commit(b_s + 16 * x + 8 * h);
+                if (h == 1) {
+                    tc_commit(b_kempty + 8 * ahead);
+                    if (++ahead == 2) { ahead = 0; ahead_phase ^= 1; }
+                }
+            };
             for_items([&](const AttItem &it) MCSD_INLINE {
-                const int mine = tile_units(it, x), k0 = it.k0, k1 = it.k1;
+                const int k0 = it.k0, k1 = it.k1, mine = min(tile_units(it, x), k1);
                 if (k0 < mine) {                    // (a tile without work has no queries either: nobody may run ahead of this barrier)
                     wide_wait(b_ready + 8 * x, items & 1, dead, P.wait_polls);
                     ++items;
+                    scores(0, n);
+                    scores(1, n);
                 }
                 for (int k = k0; k < k1; ++k) {
                     const bool work = k < mine;
-                    wide_wait(b_kfull + 8 * stage, phase, dead, P.wait_polls);
-                    if (work) {
-                        // the scores overwrite the weights of the unit before: its products are done first (both barriers, so that
-                        // whoever sees the scores knows that neither is a phase behind)
-                        if (n > 0) {
-                            wide_wait(b_o + 16 * x, (n - 1) & 1, dead, P.wait_polls);
-                            wide_wait(b_o + 16 * x + 8, (n - 1) & 1, dead, P.wait_polls);
-                        }
-                        tc_after_sync();
-                        const uint32_t at = tc_operand(smem_u32(s_k) + stage * TILE, 16);
-#pragma unroll
-                        for (int s = 0; s < D / 16; ++s) {
-                            const uint32_t off = (s >> 2) * (kAttUnit * 128 / 16) + (s & 3) * 2;
-                            tc_mma_ss(tmem + kS + 128 * x, q_at + off, at + off, kOperandHigh, tc_shape(kAttUnit, false), s > 0);
-                        }
-                        tc_commit(b_s + 8 * x);
+                    if (!work) {                    // (a tile's units are the first ones: nothing is ahead here)
+                        wide_wait(b_kfull + 8 * ahead, ahead_phase, dead, P.wait_polls);
+                        tc_commit(b_kempty + 8 * ahead);
+                        if (++ahead == 2) { ahead = 0; ahead_phase ^= 1; }
                     }
-                    tc_commit(b_kempty + 8 * stage);
                     wide_wait(b_vfull + 8 * stage, phase, dead, P.wait_polls);
                     if (work) {
                         const uint32_t at = tc_operand(smem_u32(s_v) + stage * TILE, kAttUnit * 128);
@@ -273,13 +293,16 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                             tc_after_sync();
 #pragma unroll
                             for (int s = 0; s < 4; ++s)
-                                tc_mma(tmem + kO + D * x, tmem + kS + 128 * x + 32 * h + 8 * s, at + (4 * h + s) * (16 * 128 / 16), kOperandHigh, tc_shape(D, true),
+                                tc_mma(tmem + kO + D * x, tmem + kS + 128 * x + 64 * h + 8 * s, at + (4 * h + s) * (16 * 128 / 16), kOperandHigh, tc_shape(D, true),
                                        k > k0 || h > 0 || s > 0);
                             tc_commit(b_o + 16 * x + 8 * h);
+                            if (h == 1) tc_commit(b_vempty + 8 * stage);
+                            if (k + 1 < mine) scores(h, n + 1);
                         }
                         ++n;
+                    } else {
+                        tc_commit(b_vempty + 8 * stage);
                     }
-                    tc_commit(b_vempty + 8 * stage);
                     if (++stage == 2) { stage = 0; phase ^= 1; }
                 }
             });
@@ -362,43 +385,69 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                 wide_wait(b_kfull + 8 * stage, phase, dead, P.wait_polls);
                 if (k < units) {
                     const float4 *par = s_param + stage * (kAttUnit / 2);
-                    // One half of the unit's keys; see0, see1: the keys of it that this row sees, bad, far: values that are no numbers, or far from one.
+                    // One half of the unit's keys; see0, see1: the keys of it that this row sees, bad, far: values that are no numbers, or far
+                    // from one. The weights are formed with the reference as it is; should their sum be too large for half, the
+                    // largest score is looked for, the reference moved and the half done again.
                     auto half = [&](auto plain_tag, int h, uint32_t see0, uint32_t see1) MCSD_INLINE {
                         constexpr bool plain = decltype(plain_tag)::value;
-                        float2 y[32];
-                        float most = -INFINITY;
+                        uint32_t w[32];
+                        float2 s2;
+                        auto weights = [&]() MCSD_INLINE {
+                            uint32_t acc[64];
+                            tmem_load64(t_s + 64 * h, acc);
+                            s2 = make_float2(0.f, 0.f);
+                            const float rr = rho * ra;
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t acc[32];
-                            tmem_load32(t_s + 64 * h + 32 * c, acc);
-                            const uint32_t see = c ? see1 : see0;
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const float4 kp = par[32 * h + 16 * c + j];
-                                const float2 off = __fmul2_rn(make_float2(kp.z, kp.w), make_float2(rho, rho));
-                                const float2 z = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), make_float2(kp.x, kp.y), off);
-                                if (plain) {
-                                    most = max3(most, z.x, z.y);
-                                } else {
-                                    if ((see >> (2 * j)) & 1u) most = fmaxf(most, z.x);
-                                    if ((see >> (2 * j + 1)) & 1u) most = fmaxf(most, z.y);
+                            for (int j = 0; j < 32; ++j) {
+                                const uint32_t see = j < 16 ? see0 : see1;
+                                const int bit = 2 * (j & 15);
+                                const float4 kp = par[32 * h + j];
+                                const float2 a = __fmul2_rn(make_float2(kp.x, kp.y), make_float2(ra, ra));
+                                const float2 m = fma2(make_float2(kp.z, kp.w), make_float2(rr, rr), make_float2(-ref, -ref));
+                                const float2 e = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), a, m);
+                                float2 p = make_float2(ex2f(e.x), ex2f(e.y));
+                                if (!plain) {
+                                    if (!((see >> bit) & 1u)) p.x = 0.f;
+                                    if (!((see >> (bit + 1)) & 1u)) p.y = 0.f;
                                 }
-                                y[16 * c + j] = z;
+                                s2 = add2(s2, p);
+                                if (!plain) {       // (a value that is no number makes its rows none)
+                                    const uint32_t bad = s_bad[stage][2 * h + (j >> 4)], far = s_far[stage][2 * h + (j >> 4)];
+                                    if ((far >> bit) & 1u) p.x *= 16.f;
+                                    if ((far >> (bit + 1)) & 1u) p.y *= 16.f;
+                                    if ((see & bad) >> bit & 1u) p.x = __int_as_float(0x7fffffff);
+                                    if ((see & bad) >> (bit + 1) & 1u) p.y = __int_as_float(0x7fffffff);
+                                }
+                                w[j] = half2_bits(p.x, p.y);
                             }
-                        }
-                        const float high = most * ra;
-                        if (__any_sync(0xffffffffu, high > ref + (kChunkHead + kNarrowSlack))) {
-                            const float now = fmaxf(ref, high - kChunkHead);
+                        };
+                        weights();
+                        if (__any_sync(0xffffffffu, s2.x + s2.y > kChunkMost)) {
+                            float most = -INFINITY;
+#pragma unroll 1
+                            for (int c = 0; c < 64; c += 16) {
+                                uint32_t acc[16];
+                                tmem_load16(t_s + 64 * h + c, acc);
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    const uint32_t see = plain ? 0xffffffffu : (c < 32 ? see0 : see1) >> (c & 31);
+                                    const float4 kp = par[32 * h + c / 2 + j];
+                                    const float zx = fmaf(__uint_as_float(acc[2 * j]), kp.x, kp.z * rho), zy = fmaf(__uint_as_float(acc[2 * j + 1]), kp.y, kp.w * rho);
+                                    if ((see >> (2 * j)) & 1u) most = fmaxf(most, zx);
+                                    if ((see >> (2 * j + 1)) & 1u) most = fmaxf(most, zy);
+                                }
+                            }
+                            // (a row whose own sum is small, and one that has no finite score, keep their reference)
+                            const float now = s2.x + s2.y > kChunkMost ? fmaxf(ref, most * ra - kChunkHead) : ref;
                             const float f = ex2f(ref - now);
                             ref = now;
                             sum *= f;
-                            if (h == 1) {           // (for the first half the products so far are done: the scores came after them)
-                                wide_wait(b_o + 16 * x, n & 1, dead, P.wait_polls);
-                                tc_after_sync();
-                            }
+                            // the product of the half before is done (those before that are: these scores came after them)
+                            if (n > 0 || h > 0) wide_wait(b_o + 16 * x + 8 * (h ^ 1), (h == 0 ? n - 1 : n) & 1, dead, P.wait_polls);
+                            tc_after_sync();
                             if (k > k0 || h > 0) {
 #pragma unroll 1
-                                for (int c = 0; c < D / 8; ++c) {     // (eight columns at a time: y holds most registers)
+                                for (int c = 0; c < D / 8; ++c) {
                                     uint32_t o[8];
                                     __syncwarp();
                                     tmem_load8(t_o + 8 * c, o);
@@ -407,39 +456,19 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                                     tmem_store8(t_o + 8 * c, o);
                                 }
                             }
-                        }
-                        float2 s2 = make_float2(0.f, 0.f);
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t w[16];
-                            const uint32_t see = c ? see1 : see0, bad = plain ? 0u : s_bad[stage][2 * h + c], far = plain ? 0u : s_far[stage][2 * h + c];
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const float2 e = fma2(y[16 * c + j], make_float2(ra, ra), make_float2(-ref, -ref));
-                                float2 p = make_float2(ex2f(e.x), ex2f(e.y));
-                                if (!plain) {
-                                    if (!((see >> (2 * j)) & 1u)) p.x = 0.f;
-                                    if (!((see >> (2 * j + 1)) & 1u)) p.y = 0.f;
-                                }
-                                s2 = add2(s2, p);
-                                if (!plain) {       // (a value that is no number makes its rows none)
-                                    if ((far >> (2 * j)) & 1u) p.x *= 16.f;
-                                    if ((far >> (2 * j + 1)) & 1u) p.y *= 16.f;
-                                    if ((see & bad) >> (2 * j) & 1u) p.x = __int_as_float(0x7fffffff);
-                                    if ((see & bad) >> (2 * j + 1) & 1u) p.y = __int_as_float(0x7fffffff);
-                                }
-                                w[j] = half2_bits(p.x, p.y);
-                            }
                             __syncwarp();
-                            tmem_store16(t_s + 32 * h + 16 * c, w);
+                            weights();
                         }
                         sum += s2.x + s2.y;
+                        __syncwarp();
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) tmem_store16(t_s + 64 * h + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         tc_wait_st();
                     };
-                    wide_wait(b_s + 8 * x, n & 1, dead, P.wait_polls);
-                    tc_after_sync();
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {
+                        wide_wait(b_s + 16 * x + 8 * h, n & 1, dead, P.wait_polls);
+                        tc_after_sync();
                         const int pos0 = k * kAttUnit + 64 * h;
                         const uint32_t there0 = s_valid[stage][2 * h], there1 = s_valid[stage][2 * h + 1];
                         if (h == 0) wide_wait(b_vfull + 8 * stage, phase, dead, P.wait_polls);   // (the marks of the values)
@@ -459,7 +488,10 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                 if (++stage == 2) { stage = 0; phase ^= 1; }
             }
             // ---- the end of the block
-            if (any) wide_wait(b_o + 16 * x + 8, (n - 1) & 1, dead, P.wait_polls);
+            if (any) {
+                wide_wait(b_o + 16 * x, (n - 1) & 1, dead, P.wait_polls);
+                wide_wait(b_o + 16 * x + 8, (n - 1) & 1, dead, P.wait_polls);
+            }
             tc_after_sync();
             float l = sum;
             if (*dead) l = __int_as_float(0x7fffffff);
