@@ -220,44 +220,53 @@ struct ChunkRows {
     }
 };
 
-// Joins the partial results of blocks that the cut divided: for every border between two runs a few CTAs of eight rows each; the
-// block that a border lies in belongs to its first one.
+// Joins the partial results of blocks that the cut divided: for every border between two runs a CTA, or a few for blocks of many
+// rows; the block that a border lies in belongs to its first one.
+constexpr int kChunkJoinThreads = 256;
 template <int DT, int D, int ROWS>
-__global__ void __launch_bounds__(128)
+__global__ void __launch_bounds__(kChunkJoinThreads)
 chunk_join_kernel(const __grid_constant__ ChunkParams P)
 {
-    const int tid = threadIdx.x, lane = tid & 31;
-    const ChunkCut cut = chunk_cut(P, lane);
-    const ChunkPlace border = (blockIdx.x + 1) * cut.per;
-    AttItem it = {};
-    ChunkPlace first = 0, last = 0;
-    bool mine = border < cut.span;
-    if (mine) {
-        const ChunkSpot t = chunk_find(P, border, lane);
-        const ChunkPlace begin = border - t.at + P.lead;        // of the block's first unit
-        it.len = chunk_len(P, t);
-        it.k1 = chunk_units(it.len);
-        first = begin / cut.per;
-        last = (begin + static_cast<ChunkPlace>(it.k1 - 1) * kAttUnit) / cut.per;
-        mine = first == blockIdx.x && last > first;
-        it.b = t.b;
-        it.head = t.head;
-        it.row0 = t.block * P.tokens * P.group;
-        it.rows = min((t.block + 1) * P.tokens, t.s.count) * P.group;
+    constexpr int TPR = D / 4;                      // threads of a row, four numbers each
+    __shared__ AttItem s_it;
+    __shared__ int s_first, s_last;
+    const int tid = threadIdx.x;
+    if (tid < 32) {
+        const ChunkCut cut = chunk_cut(P, tid);
+        const ChunkPlace border = (blockIdx.x + 1) * cut.per;
+        AttItem it = {};
+        int first = 0, last = -1;
+        if (border < cut.span) {
+            const ChunkSpot t = chunk_find(P, border, tid);
+            const ChunkPlace begin = border - t.at + P.lead;    // of the block's first unit
+            const int units = chunk_units(chunk_len(P, t));
+            first = static_cast<int>(begin / cut.per);
+            last = static_cast<int>((begin + static_cast<ChunkPlace>(units - 1) * kAttUnit) / cut.per);
+            if (first != static_cast<int>(blockIdx.x) || last == first) last = -1;
+            it.b = t.b;
+            it.head = t.head;
+            it.row0 = t.block * P.tokens * P.group;
+            it.rows = min((t.block + 1) * P.tokens, t.s.count) * P.group;
+        }
+        if (tid == 0) {
+            s_it = it;
+            s_first = first;
+            s_last = last;
+        }
     }
+    __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");   // (every thread: this kernel must not end before the one it follows)
-    const int r0 = blockIdx.y * 8;
-    if (!mine || it.row0 + r0 >= it.rows) return;
-    auto part_of = [&](ChunkPlace cta) { return P.part + static_cast<long long>(2 * cta + (cta == first ? 1 : 0)) * part_floats(ROWS, D); };
-    for (int x = tid; x < 8 * (D / 4); x += 128) {
-        const int r = r0 + x / (D / 4), c = (x % (D / 4)) * 4;
-        if (it.row0 + r >= it.rows) break;
+    const AttItem it = s_it;
+    const int first = s_first, last = s_last, c = (tid % TPR) * 4;
+    const int rows = min(ROWS, it.rows - it.row0), step = gridDim.y * (kChunkJoinThreads / TPR);
+    auto part_of = [&](int cta) { return P.part + static_cast<long long>(2 * cta + (cta == first ? 1 : 0)) * part_floats(ROWS, D); };
+    for (int r = blockIdx.y * (kChunkJoinThreads / TPR) + tid / TPR; first <= last && r < rows; r += step) {
         float m = kNoTop;
-        for (ChunkPlace k = first; k <= last; ++k) m = fmaxf(m, __ldcg(part_of(k) + ROWS * D + r));
+        for (int k = first; k <= last; ++k) m = fmaxf(m, __ldcg(part_of(k) + ROWS * D + r));
         float l = 0.f;
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (ChunkPlace k = first; k <= last; ++k) {
+        for (int k = first; k <= last; ++k) {
             const float *part = part_of(k);
             const float lk = __ldcg(part + ROWS * (D + 1) + r);
             const float f = att_factor(__ldcg(part + ROWS * D + r), lk, m);

@@ -110,7 +110,9 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
         for (;;) {
             int more = 0;
             __syncwarp();
-            if (lane == 0) more = s_walk[warp].template next<kChunkRows>(P, lane, s_item[warp]);
+            if (lane == 0) {
+                more = s_walk[warp].template next<kChunkRows>(P, lane, s_item[warp]);
+            }
             if (!__shfl_sync(0xffffffffu, more, 0)) break;
             __syncwarp();
             f(s_item[warp]);
@@ -333,49 +335,57 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
             const bool any = k0 < units;            // (of the tile)
             if (any) {
                 // Q to shared memory, scaled by a power of two to the top of half's range (and to a positive softmax scale), in the order that
-                // the ANDs of the keys give
-                uint4 raw[D / 8];
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c) raw[c] = make_uint4(0u, 0u, 0u, 0u);
-                if (live) {
-                    const long long at = ChunkRows::q_at(P, it, row);
-                    if (P.q_vec) {
-#pragma unroll
-                        for (int c = 0; c < D / 8; ++c) raw[c] = (reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + 2 * at))[c];   // (not the read-only path: out may be q)
-                    } else {
-                        const unsigned short *src = static_cast<const unsigned short *>(P.q) + at;
-#pragma unroll
-                        for (int c = 0; c < D / 8; ++c)
-                            raw[c] = make_uint4(src[8 * c] | src[8 * c + 1] << 16, src[8 * c + 2] | src[8 * c + 3] << 16,
-                                                src[8 * c + 4] | src[8 * c + 5] << 16, src[8 * c + 6] | src[8 * c + 7] << 16);
+                // the ANDs of the keys give. The rows come side by side, sixteen bytes a lane, to where their operands go; then each thread
+                // turns its own, sixteen bytes at a time.
+                constexpr int CR = D / 8;           // 16-byte chunks of a row
+                auto place = [&](int rr, int c) MCSD_INLINE { return s_q + x * TILE + rr * 128 + (c >> 3) * (kAttUnit * 128) + (((c & 7) ^ (rr & 7)) << 4); };
+                const long long at = live ? ChunkRows::q_at(P, it, row) : -1;
+                if (P.q_vec) {
+#pragma unroll 4
+                    for (int i = 0; i < CR; ++i) {
+                        const int rr = i * (32 / CR) + lane / CR, c = lane % CR;
+                        const long long from = __shfl_sync(0xffffffffu, at, rr);
+                        if (from >= 0) cp_async16(smem_u32(place((warp & 3) * 32 + rr, c)), static_cast<const char *>(P.q) + 2 * (from + 8 * c));
                     }
+                    asm volatile("cp.async.wait_all;" ::: "memory");
+                    __syncwarp();
+                } else if (live) {
+                    const unsigned short *src = static_cast<const unsigned short *>(P.q) + at;
+#pragma unroll 1
+                    for (int c = 0; c < CR; ++c)
+                        *reinterpret_cast<uint4 *>(place(r, c)) =
+                            make_uint4(src[8 * c] | src[8 * c + 1] << 16, src[8 * c + 2] | src[8 * c + 3] << 16,
+                                       src[8 * c + 4] | src[8 * c + 5] << 16, src[8 * c + 6] | src[8 * c + 7] << 16);
                 }
-                float most = 0.f, sum = 0.f;
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    float v[8];
-                    Elem<DT>::unpack(raw[c], v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) { most = fmaxf(most, fabsf(v[i])); sum += v[i]; }
+                auto chunk = [&](int c) MCSD_INLINE { return live ? *reinterpret_cast<const uint4 *>(place(r, c)) : make_uint4(0u, 0u, 0u, 0u); };
+                uint32_t big = 0u;                  // largest magnitudes of two numbers
+#pragma unroll 4
+                for (int c = 0; c < CR; ++c) {
+                    const uint4 v = chunk(c);
+                    big = Elem<DT>::mx(Elem<DT>::mx(big, v.x & 0x7fff7fffu), Elem<DT>::mx(v.y & 0x7fff7fffu, Elem<DT>::mx(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
                 }
+                const float most = Elem<DT>::max_final(big);
                 int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 126 : 0;
                 e = max(min(e, 112), -110);
                 const float up = __int_as_float((127 + 15 - e) << 23) * (P.scale < 0.f ? -1.f : 1.f);
                 ra = ldexpf(fabsf(P.scale) * 1.4426950408889634f, e - 15 + 24);
-                rho = sum * up * 5.9604644775390625e-8f;          // 2^-24
-                unsigned char *to = s_q + x * TILE + r * 128;
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c) {                 // eight numbers, one word of codes
+                float2 sum = make_float2(0.f, 0.f);
+                const float2 f0 = make_float2(up, up), f1 = make_float2(up * 0.0625f, up * 0.0625f);
+#pragma unroll 2
+                for (int c = 0; c < CR; ++c) {      // eight numbers, one word of codes
                     float v[8];
-                    Elem<DT>::unpack(raw[c], v);
+                    Elem<DT>::unpack(chunk(c), v);
                     uint32_t out[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float f = i & 1 ? up * 0.0625f : up;
-                        out[i] = half2_bits(v[i] * f, v[i + 4] * f);
+                        const float2 pair = make_float2(v[i], v[i + 4]);
+                        sum = add2(sum, pair);
+                        const float2 q = __fmul2_rn(pair, i & 1 ? f1 : f0);
+                        out[i] = half2_bits(q.x, q.y);
                     }
-                    *reinterpret_cast<uint4 *>(to + (c >> 3) * (kAttUnit * 128) + (((c & 7) ^ (r & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
+                    *reinterpret_cast<uint4 *>(place(r, c)) = make_uint4(out[0], out[1], out[2], out[3]);
                 }
+                rho = (sum.x + sum.y) * up * 5.9604644775390625e-8f;            // 2^-24
                 fence_proxy_async();
                 tc_before_sync();
                 warp_arrive(b_ready + 8 * x, lane);
@@ -385,85 +395,99 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                 wide_wait(b_kfull + 8 * stage, phase, dead, P.wait_polls);
                 if (k < units) {
                     const float4 *par = s_param + stage * (kAttUnit / 2);
-                    // One half of the unit's keys; see0, see1: the keys of it that this row sees, bad, far: values that are no numbers, or far
-                    // from one. The weights are formed with the reference as it is; should their sum be too large for half, the
-                    // largest score is looked for, the reference moved and the half done again.
-                    auto half = [&](auto plain_tag, int h, uint32_t see0, uint32_t see1) MCSD_INLINE {
-                        constexpr bool plain = decltype(plain_tag)::value;
-                        uint32_t w[32];
-                        float2 s2;
-                        auto weights = [&]() MCSD_INLINE {
-                            uint32_t acc[64];
-                            tmem_load64(t_s + 64 * h, acc);
-                            s2 = make_float2(0.f, 0.f);
-                            const float rr = rho * ra;
+                    // One half of the unit's keys, where every row of the tile sees them and nothing is odd about the values: the
+                    // weights with the reference as it is; false (and nothing stored) should their sum be too large for half.
+                    auto swift = [&](int h) MCSD_INLINE {
+                        uint32_t acc[64], w[32];
+                        tmem_load64(t_s + 64 * h, acc);
+                        float2 s2 = make_float2(0.f, 0.f);
+                        const float rr = rho * ra;
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) {
-                                const uint32_t see = j < 16 ? see0 : see1;
-                                const int bit = 2 * (j & 15);
-                                const float4 kp = par[32 * h + j];
+                        for (int j = 0; j < 32; ++j) {
+                            const float4 kp = par[32 * h + j];
+                            const float2 a = __fmul2_rn(make_float2(kp.x, kp.y), make_float2(ra, ra));
+                            const float2 m = fma2(make_float2(kp.z, kp.w), make_float2(rr, rr), make_float2(-ref, -ref));
+                            const float2 e = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), a, m);
+                            const float2 p = make_float2(ex2f(e.x), ex2f(e.y));
+                            s2 = add2(s2, p);
+                            w[j] = half2_bits(p.x, p.y);
+                        }
+                        if (__any_sync(0xffffffffu, s2.x + s2.y > kChunkMost)) return false;
+                        sum += s2.x + s2.y;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) tmem_store16(t_s + 64 * h + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
+                        return true;
+                    };
+                    // The same wherever the first does not do: the largest score, the reference moved where that leaves it by too much, then
+                    // the weights, sixteen keys at a time. see0, see1: the keys that this row sees; bad, far: values that are no numbers (their
+                    // rows are none), or far from one.
+                    auto careful = [&](int h, uint32_t see0, uint32_t see1) MCSD_INLINE {
+                        const float4 *at = par + 32 * h;
+                        float most = -INFINITY;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            const uint32_t see = (c < 2 ? see0 : see1) >> (16 * (c & 1));
+                            uint32_t acc[16];
+                            __syncwarp();
+                            tmem_load16(t_s + 64 * h + 16 * c, acc);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const float4 kp = at[8 * c + j];
+                                const float2 z = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), make_float2(kp.x, kp.y),
+                                                      __fmul2_rn(make_float2(kp.z, kp.w), make_float2(rho, rho)));
+                                if ((see >> (2 * j)) & 1u) most = fmaxf(most, z.x);
+                                if ((see >> (2 * j + 1)) & 1u) most = fmaxf(most, z.y);
+                            }
+                        }
+                        const float high = most * ra - kChunkHead;
+                        if (__any_sync(0xffffffffu, high > ref + kNarrowSlack)) {
+                            const float now = high > ref + kNarrowSlack ? high : ref;
+                            const float f = ex2f(ref - now);
+                            ref = now;
+                            sum *= f;
+                            if (k > k0 || h > 0) {
+                                // the product of the half before is done (those before that are: these scores came after them)
+                                wide_wait(b_o + 16 * x + 8 * (h ^ 1), (h == 0 ? n - 1 : n) & 1, dead, P.wait_polls);
+                                tc_after_sync();
+#pragma unroll 1
+                                for (int c = 0; c < D / 16; ++c) {
+                                    uint32_t o[16];
+                                    __syncwarp();
+                                    tmem_load16(t_o + 16 * c, o);
+#pragma unroll
+                                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                    tmem_store16(t_o + 16 * c, o);
+                                }
+                            }
+                        }
+                        const float rr = rho * ra;
+                        float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {           // (what is stored lies over scores that are read)
+                            const uint32_t see = (c < 2 ? see0 : see1) >> (16 * (c & 1));
+                            const uint32_t bad = see & s_bad[stage][2 * h + (c >> 1)] >> (16 * (c & 1)), far = s_far[stage][2 * h + (c >> 1)] >> (16 * (c & 1));
+                            uint32_t acc[16], w[8];
+                            __syncwarp();
+                            tmem_load16(t_s + 64 * h + 16 * c, acc);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const float4 kp = at[8 * c + j];
                                 const float2 a = __fmul2_rn(make_float2(kp.x, kp.y), make_float2(ra, ra));
                                 const float2 m = fma2(make_float2(kp.z, kp.w), make_float2(rr, rr), make_float2(-ref, -ref));
                                 const float2 e = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), a, m);
                                 float2 p = make_float2(ex2f(e.x), ex2f(e.y));
-                                if (!plain) {
-                                    if (!((see >> bit) & 1u)) p.x = 0.f;
-                                    if (!((see >> (bit + 1)) & 1u)) p.y = 0.f;
-                                }
+                                if (!((see >> (2 * j)) & 1u)) p.x = 0.f;
+                                if (!((see >> (2 * j + 1)) & 1u)) p.y = 0.f;
                                 s2 = add2(s2, p);
-                                if (!plain) {       // (a value that is no number makes its rows none)
-                                    const uint32_t bad = s_bad[stage][2 * h + (j >> 4)], far = s_far[stage][2 * h + (j >> 4)];
-                                    if ((far >> bit) & 1u) p.x *= 16.f;
-                                    if ((far >> (bit + 1)) & 1u) p.y *= 16.f;
-                                    if ((see & bad) >> bit & 1u) p.x = __int_as_float(0x7fffffff);
-                                    if ((see & bad) >> (bit + 1) & 1u) p.y = __int_as_float(0x7fffffff);
-                                }
+                                if ((far >> (2 * j)) & 1u) p.x *= 16.f;
+                                if ((far >> (2 * j + 1)) & 1u) p.y *= 16.f;
+                                if ((bad >> (2 * j)) & 1u) p.x = __int_as_float(0x7fffffff);
+                                if ((bad >> (2 * j + 1)) & 1u) p.y = __int_as_float(0x7fffffff);
                                 w[j] = half2_bits(p.x, p.y);
                             }
-                        };
-                        weights();
-                        if (__any_sync(0xffffffffu, s2.x + s2.y > kChunkMost)) {
-                            float most = -INFINITY;
-#pragma unroll 1
-                            for (int c = 0; c < 64; c += 16) {
-                                uint32_t acc[16];
-                                tmem_load16(t_s + 64 * h + c, acc);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) {
-                                    const uint32_t see = plain ? 0xffffffffu : (c < 32 ? see0 : see1) >> (c & 31);
-                                    const float4 kp = par[32 * h + c / 2 + j];
-                                    const float zx = fmaf(__uint_as_float(acc[2 * j]), kp.x, kp.z * rho), zy = fmaf(__uint_as_float(acc[2 * j + 1]), kp.y, kp.w * rho);
-                                    if ((see >> (2 * j)) & 1u) most = fmaxf(most, zx);
-                                    if ((see >> (2 * j + 1)) & 1u) most = fmaxf(most, zy);
-                                }
-                            }
-                            // (a row whose own sum is small, and one that has no finite score, keep their reference)
-                            const float now = s2.x + s2.y > kChunkMost ? fmaxf(ref, most * ra - kChunkHead) : ref;
-                            const float f = ex2f(ref - now);
-                            ref = now;
-                            sum *= f;
-                            // the product of the half before is done (those before that are: these scores came after them)
-                            if (n > 0 || h > 0) wide_wait(b_o + 16 * x + 8 * (h ^ 1), (h == 0 ? n - 1 : n) & 1, dead, P.wait_polls);
-                            tc_after_sync();
-                            if (k > k0 || h > 0) {
-#pragma unroll 1
-                                for (int c = 0; c < D / 8; ++c) {
-                                    uint32_t o[8];
-                                    __syncwarp();
-                                    tmem_load8(t_o + 8 * c, o);
-#pragma unroll
-                                    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                                    tmem_store8(t_o + 8 * c, o);
-                                }
-                            }
-                            __syncwarp();
-                            weights();
+                            tmem_store8(t_s + 64 * h + 8 * c, w);
                         }
                         sum += s2.x + s2.y;
-                        __syncwarp();
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) tmem_store16(t_s + 64 * h + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
-                        tc_wait_st();
                     };
 #pragma unroll 1
                     for (int h = 0; h < 2; ++h) {
@@ -473,12 +497,12 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                         const uint32_t there0 = s_valid[stage][2 * h], there1 = s_valid[stage][2 * h + 1];
                         if (h == 0) wide_wait(b_vfull + 8 * stage, phase, dead, P.wait_polls);   // (the marks of the values)
                         const uint32_t odd = s_bad[stage][2 * h] | s_bad[stage][2 * h + 1] | s_far[stage][2 * h] | s_far[stage][2 * h + 1];
-                        if ((there0 & there1) == 0xffffffffu && odd == 0u && pos0 + 64 <= all) {
-                            half(std::true_type(), h, 0u, 0u);
-                        } else {
+                        const bool plain = (there0 & there1) == 0xffffffffu && odd == 0u && pos0 + 64 <= all;
+                        if (!plain || (k == k0 && h == 0) || !swift(h)) {       // (at first there is no reference)
                             auto first = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
-                            half(std::false_type(), h, there0 & first(sees - pos0), there1 & first(sees - pos0 - 32));
+                            careful(h, there0 & first(sees - pos0), there1 & first(sees - pos0 - 32));
                         }
+                        tc_wait_st();
                         tc_before_sync();
                         warp_arrive(b_p + 16 * x + 8 * h, lane);
                     }
@@ -497,31 +521,58 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
             if (*dead) l = __int_as_float(0x7fffffff);
             const float inv = l == 0.f ? 0.f : 1.f / l;         // (nothing seen: zeros)
             const int at_row = 128 * x + r;
-            const long long out = live ? ChunkRows::out_at(P, it, row) : 0;
             float *part = P.part + att_slot(it.k0) * part_floats(kChunkRows, D);
-            for (int c = 0; c < D / 16; ++c) {
-                uint32_t o[16];
+            // The rows of a warp go through its part of the queries' memory (which nobody reads any more), so that they leave
+            // side by side: 32 numbers of every row at a time as float32, or all of them in their type.
+            unsigned char *own = s_q + x * TILE + (warp & 3) * 32 * 128;
+            constexpr int CR = D / 8;               // 16-byte chunks of a row in its type
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
                 __syncwarp();
-                tmem_load16(t_o + 16 * c, o);
-                if (live) {
+                tmem_load32(t_o + 32 * c, o);
 #pragma unroll
-                    for (int i = 0; i < 16; i += 8) {           // eight columns: one word's codes, in the operands' order
-                        float v[8];
+                for (int i = 0; i < 4; ++i) {       // eight columns: one word's codes, in the operands' order
+                    float v[8];
 #pragma unroll
-                        for (int p = 0; p < 8; ++p) v[(p >> 1) + 4 * (p & 1)] = any ? __uint_as_float(o[i + p]) : 0.f;
-                        if (it.whole) {
+                    for (int p = 0; p < 8; ++p) v[(p >> 1) + 4 * (p & 1)] = any ? __uint_as_float(o[8 * i + p]) : 0.f;
+                    if (it.whole) {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) v[e] *= inv;
-                            if (P.o_vec) {
-                                *reinterpret_cast<uint4 *>(static_cast<char *>(P.out) + 2 * (out + 16 * c + i)) = pack_elems<DT>(v);
-                            } else {
+                        for (int e = 0; e < 8; ++e) v[e] *= inv;
+                        const int cc = 4 * c + i;
+                        *reinterpret_cast<uint4 *>(own + lane * 128 + (cc >> 3) * (kAttUnit * 128) + (((cc & 7) ^ (lane & 7)) << 4)) = pack_elems<DT>(v);
+                    } else {
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) store_elem<DT>(P.out, out + 16 * c + i + e, v[e]);
-                            }
+                        for (int e = 0; e < 2; ++e)
+                            *reinterpret_cast<float4 *>(own + lane * 128 + (((2 * i + e) ^ (lane & 7)) << 4)) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+                    }
+                }
+                if (!it.whole) {
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int rr = 4 * i + (lane >> 3), grow = 128 * x + (warp & 3) * 32 + rr;
+                        if (it.row0 + grow < it.rows)
+                            *reinterpret_cast<float4 *>(part + grow * D + 32 * c + 4 * (lane & 7)) = *reinterpret_cast<const float4 *>(own + rr * 128 + (((lane & 7) ^ (rr & 7)) << 4));
+                    }
+                }
+            }
+            if (it.whole) {
+                const long long row_at = live ? ChunkRows::out_at(P, it, row) : -1;
+                __syncwarp();
+#pragma unroll 4
+                for (int i = 0; i < CR; ++i) {
+                    const int rr = i * (32 / CR) + lane / CR, c = lane % CR;
+                    const long long first = __shfl_sync(0xffffffffu, row_at, rr), at = first + 8 * c;
+                    if (first >= 0) {
+                        const uint4 v = *reinterpret_cast<const uint4 *>(own + rr * 128 + (c >> 3) * (kAttUnit * 128) + (((c & 7) ^ (rr & 7)) << 4));
+                        if (P.o_vec) {
+                            *reinterpret_cast<uint4 *>(static_cast<char *>(P.out) + 2 * at) = v;
                         } else {
-                            float4 *to = reinterpret_cast<float4 *>(part + at_row * D + 16 * c + i);
-                            to[0] = make_float4(v[0], v[1], v[2], v[3]);
-                            to[1] = make_float4(v[4], v[5], v[6], v[7]);
+                            unsigned short *to = static_cast<unsigned short *>(P.out) + at;
+                            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) to[e] = static_cast<unsigned short>(w[e >> 1] >> (16 * (e & 1)));
                         }
                     }
                 }

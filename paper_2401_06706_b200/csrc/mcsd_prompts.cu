@@ -96,8 +96,8 @@ int launch_with_join(int threads, int smem, const ChunkParams &p, cudaStream_t s
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
     if (p.n_ctas < 2) return MCSD_OK;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.n_ctas - 1), ROWS / 8);
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = dim3(static_cast<unsigned>(p.n_ctas - 1), ROWS > 64 ? 4 : 1);
+    cfg.blockDim = dim3(kChunkJoinThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
