@@ -156,8 +156,8 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {            // of an
 
 // What a CTA has of an item: units [k0, k1) of one block of rows of one (sequence, key/value head). Rows row0 .. rows - 1 of the head's
 // are the block's (or fewer: a block has at most as many as the kernel's), the first `tail` positions are seen by all of them;
-// whole: all of the item's units.
-struct AttItem { int b, head, len, tail, row0, rows, k0, k1; bool whole; };
+// whole: all of the item's units; last (of chunks): the CTA that has the last of them.
+struct AttItem { int b, head, len, tail, row0, rows, k0, k1; bool whole; int last; };
 // Where a part of an item goes: a CTA has one that others began and one that others end at most.
 __device__ __forceinline__ long long att_slot(int k0) { return 2 * blockIdx.x + (k0 > 0 ? 0 : 1); }
 
@@ -201,6 +201,9 @@ struct TreeRows {
             return true;
         }
     };
+    // (the joining kernel finds what was divided by itself)
+    static __device__ __forceinline__ void begun(const AttendParams &) {}
+    static __device__ __forceinline__ void divided(const AttendParams &, const AttItem &) {}
     static __device__ __forceinline__ long long q_at(const AttendParams &P, const AttItem &it, int row)
     {
         const int node = row / P.group, h = it.head * P.group + (row - node * P.group);
@@ -292,6 +295,7 @@ narrow_kernel(const __grid_constant__ typename Rows::Params P)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;
     const int ps = 1 << P.c.page_shift;
+    if (tid == 0) Rows::begun(P);
     typename Rows::Walk walk;
     if (!walk.begin(P, lane)) return;
     AttItem it;
@@ -350,6 +354,7 @@ narrow_kernel(const __grid_constant__ typename Rows::Params P)
         for (int i = 0; i < STAGES - 1; ++i) issue(i, i);
 
         if (tid < ROWS) Rows::see(P, it, row0 + tid, s_seen[tid]);
+        if (tid == 0) Rows::divided(P, it);
         // queries: this lane's D / 4 numbers of row g of every tile, scaled to the top of half's range
         uint32_t qb[NB][KS][2];
         float ra[NB][2], rb[NB][2];                 // of rows 2 t and 2 t + 1: log2 units per unit of an accumulator, and per unit of mid - 8 scale

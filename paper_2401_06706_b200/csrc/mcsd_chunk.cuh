@@ -12,6 +12,7 @@ struct ChunkParams {
     void *out;
     float *lse;                                     // of the attention: written (may be null); of the weights: read
     float *part;                                    // partial results, two slots per CTA
+    struct ChunkJoin *joins;                        // per CTA: the block that it began and others end, if there is one
     float *weights;
     const int32_t *table, *start, *cu;
     long long ld_table, n_tokens;
@@ -27,6 +28,9 @@ struct ChunkParams {
     float scale, decay;
     uint32_t wait_polls, test_extra;                // (as in AttendParams)
 };
+
+// A block that the cut divided: what the joining kernel needs to know, left by the CTA that has its first unit.
+struct ChunkJoin { int b, head, row0, rows, last, pad[3]; };
 
 // The new tokens of sequence b: the row of the first one, how many, the positions there are before them and with them.
 struct ChunkSeq { int row, count, start, len; };
@@ -144,18 +148,28 @@ __device__ __forceinline__ int chunk_units_below(const ChunkParams &P, ChunkPlac
     return k < static_cast<ChunkPlace>(units) ? static_cast<int>(k) : units;
 }
 
+// Left by one thread of a CTA when it begins (nothing to join), and when it has begun a block that others end.
+__device__ __forceinline__ void chunk_join_none(const ChunkParams &P) { P.joins[blockIdx.x].last = -1; }
+__device__ __forceinline__ void chunk_join_note(const ChunkParams &P, const AttItem &it)
+{
+    if (it.whole || it.k0 > 0) return;
+    ChunkJoin *j = P.joins + blockIdx.x;
+    j->b = it.b; j->head = it.head; j->row0 = it.row0; j->rows = it.rows; j->last = it.last;
+}
+
 // The rows of a chunk, as the narrow kernel and its like see them.
 struct ChunkRows {
     typedef ChunkParams Params;
     struct Walk {
         ChunkSpot t;
-        ChunkPlace left, per;                       // of the run; places of a run
+        ChunkPlace at, left, per;                   // place the walk has come to, places left of the run, places of a run
         bool fresh;
         __device__ __forceinline__ bool begin(const ChunkParams &P, int lane)
         {
             const ChunkCut cut = chunk_cut(P, lane);
             const ChunkPlace x = blockIdx.x * cut.per;
             if (x >= cut.span) return false;
+            at = x;
             left = cut.span - x < cut.per ? cut.span - x : cut.per;
             per = cut.per;
             t = chunk_find(P, x, lane);
@@ -170,6 +184,7 @@ struct ChunkRows {
                     const ChunkPlace had = t.places - t.at;
                     if (left <= had) return false;
                     left -= had;
+                    at += had;
                     if (!chunk_next(P, t)) {
                         int b = t.b + 1;
                         while (b < P.batch && chunk_places(P, b) == 0) ++b;
@@ -193,10 +208,13 @@ struct ChunkRows {
                 it.rows = min((t.block + 1) * P.tokens, t.s.count) * P.group;
                 it.tail = chunk_sees(t.s, t.block * P.tokens);
                 it.whole = it.k0 == 0 && it.k1 == units;
+                it.last = static_cast<int>((at - t.at + P.lead + static_cast<ChunkPlace>(units - 1) * kAttUnit) / per);
                 return true;
             }
         }
     };
+    static __device__ __forceinline__ void begun(const ChunkParams &P) { chunk_join_none(P); }
+    static __device__ __forceinline__ void divided(const ChunkParams &P, const AttItem &it) { chunk_join_note(P, it); }
     static __device__ __forceinline__ long long q_at(const ChunkParams &P, const AttItem &it, int row)
     {
         const int i = row / P.group, h = it.head * P.group + (row - i * P.group);
@@ -220,62 +238,34 @@ struct ChunkRows {
     }
 };
 
-// Joins the partial results of blocks that the cut divided: for every border between two runs a CTA, or a few for blocks of many
-// rows; the block that a border lies in belongs to its first one.
+// Joins the partial results of blocks that the cut divided: a CTA for eight (D = 128) or sixteen rows of each.
 constexpr int kChunkJoinThreads = 256;
 template <int DT, int D, int ROWS>
 __global__ void __launch_bounds__(kChunkJoinThreads)
 chunk_join_kernel(const __grid_constant__ ChunkParams P)
 {
     constexpr int TPR = D / 4;                      // threads of a row, four numbers each
-    __shared__ AttItem s_it;
-    __shared__ int s_first, s_last;
-    const int tid = threadIdx.x;
-    if (tid < 32) {
-        const ChunkCut cut = chunk_cut(P, tid);
-        const ChunkPlace border = (blockIdx.x + 1) * cut.per;
-        AttItem it = {};
-        int first = 0, last = -1;
-        if (border < cut.span) {
-            const ChunkSpot t = chunk_find(P, border, tid);
-            const ChunkPlace begin = border - t.at + P.lead;    // of the block's first unit
-            const int units = chunk_units(chunk_len(P, t));
-            first = static_cast<int>(begin / cut.per);
-            last = static_cast<int>((begin + static_cast<ChunkPlace>(units - 1) * kAttUnit) / cut.per);
-            if (first != static_cast<int>(blockIdx.x) || last == first) last = -1;
-            it.b = t.b;
-            it.head = t.head;
-            it.row0 = t.block * P.tokens * P.group;
-            it.rows = min((t.block + 1) * P.tokens, t.s.count) * P.group;
-        }
-        if (tid == 0) {
-            s_it = it;
-            s_first = first;
-            s_last = last;
-        }
-    }
-    __syncthreads();
+    const int first = blockIdx.x, r = blockIdx.y * (kChunkJoinThreads / TPR) + threadIdx.x / TPR, c = (threadIdx.x % TPR) * 4;
     asm volatile("griddepcontrol.wait;" ::: "memory");   // (every thread: this kernel must not end before the one it follows)
-    const AttItem it = s_it;
-    const int first = s_first, last = s_last, c = (tid % TPR) * 4;
-    const int rows = min(ROWS, it.rows - it.row0), step = gridDim.y * (kChunkJoinThreads / TPR);
+    const ChunkJoin j = P.joins[first];
+    if (j.last < 0 || r >= min(ROWS, j.rows - j.row0)) return;
+    AttItem it = {};
+    it.b = j.b; it.head = j.head; it.rows = j.rows;
     auto part_of = [&](int cta) { return P.part + static_cast<long long>(2 * cta + (cta == first ? 1 : 0)) * part_floats(ROWS, D); };
-    for (int r = blockIdx.y * (kChunkJoinThreads / TPR) + tid / TPR; first <= last && r < rows; r += step) {
-        float m = kNoTop;
-        for (int k = first; k <= last; ++k) m = fmaxf(m, __ldcg(part_of(k) + ROWS * D + r));
-        float l = 0.f;
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    // (relative to the largest reference so far: one pass over the parts)
+    float m = kNoTop, l = 0.f;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (int k = first; k <= last; ++k) {
-            const float *part = part_of(k);
-            const float lk = __ldcg(part + ROWS * (D + 1) + r);
-            const float f = att_factor(__ldcg(part + ROWS * D + r), lk, m);
-            const float4 v = __ldcg(reinterpret_cast<const float4 *>(part + r * D + c));
-            l = fmaf(f, lk, l);
-            a.x = fmaf(f, v.x, a.x); a.y = fmaf(f, v.y, a.y); a.z = fmaf(f, v.z, a.z); a.w = fmaf(f, v.w, a.w);
-        }
-        att_store<DT, ChunkRows>(P, it, it.row0 + r, c, a, m, l);
+    for (int k = first; k <= j.last; ++k) {
+        const float *part = part_of(k);
+        const float mk = __ldcg(part + ROWS * D + r), lk = __ldcg(part + ROWS * (D + 1) + r);
+        const float4 v = __ldcg(reinterpret_cast<const float4 *>(part + r * D + c));
+        const float top = fmaxf(m, mk), f = att_factor(m, l, top), g = att_factor(mk, lk, top);
+        m = top;
+        l = fmaf(f, l, g * lk);
+        a.x = fmaf(f, a.x, g * v.x); a.y = fmaf(f, a.y, g * v.y); a.z = fmaf(f, a.z, g * v.z); a.w = fmaf(f, a.w, g * v.w);
     }
+    att_store<DT, ChunkRows>(P, it, j.row0 + r, c, a, m, l);
 }
 
 }  // namespace mcsd

@@ -90,6 +90,7 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
         s_dead = 0;
     }
     if (warp == 16) tmem_alloc(smem_u32(&s_tmem), kColumns);
+    if (tid == 0) chunk_join_none(P);
     if (warp == 17) {
         ChunkRows::Walk walk;
         const bool any = walk.begin(P, lane);
@@ -323,6 +324,7 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
         int stage = 0;
         uint32_t phase = 0, n = 0;
         for_items([&](const AttItem &it) MCSD_INLINE {
+            if (tid == 0) chunk_join_note(P, it);
             const int row = it.row0 + 128 * x + r;
             const bool live = row < it.rows;
             const int units = tile_units(it, x);

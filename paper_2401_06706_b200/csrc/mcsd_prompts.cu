@@ -87,6 +87,9 @@ ChunkPlan chunk_plan(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache, bool 
     return plan;
 }
 
+// Bytes of the notes on divided blocks, ahead of the partial results in the workspace.
+size_t join_bytes(const ChunkPlan &plan) { return (sizeof(ChunkJoin) * static_cast<size_t>(plan.ctas[0] > plan.ctas[1] ? plan.ctas[0] : plan.ctas[1]) + 255) / 256 * 256; }
+
 // Launches the kernel that does the work and, as its programmatic dependent, the one that joins divided blocks.
 template <int DT, int D, int ROWS, auto Kernel>
 int launch_with_join(int threads, int smem, const ChunkParams &p, cudaStream_t st)
@@ -96,7 +99,8 @@ int launch_with_join(int threads, int smem, const ChunkParams &p, cudaStream_t s
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
     if (p.n_ctas < 2) return MCSD_OK;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.n_ctas - 1), ROWS > 64 ? 4 : 1);
+    constexpr int kRows = kChunkJoinThreads / (D / 4);
+    cfg.gridDim = dim3(static_cast<unsigned>(p.n_ctas - 1), (ROWS + kRows - 1) / kRows);
     cfg.blockDim = dim3(kChunkJoinThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -202,7 +206,7 @@ size_t mcsd_chunk_attention_workspace_bytes(const mcsd_chunk_desc *desc, const m
     const ChunkPlan plan = chunk_plan(desc, cache, true);
     const size_t narrow = static_cast<size_t>(plan.ctas[0]) * part_floats(plan.narrow, cache->head_dim);
     const size_t wide = static_cast<size_t>(plan.ctas[1]) * part_floats(kChunkRows, cache->head_dim);
-    return (2 * sizeof(float) * (narrow > wide ? narrow : wide) + 255) / 256 * 256;
+    return join_bytes(plan) + (2 * sizeof(float) * (narrow > wide ? narrow : wide) + 255) / 256 * 256;
 }
 
 int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table, const int32_t *start,
@@ -225,10 +229,11 @@ int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache
     ChunkParams p = chunk_params(desc, cache, page_table, start, cu_tokens, q);
     p.out = out;
     p.lse = lse;
-    p.part = static_cast<float *>(desc->workspace);
     p.o_vec = (reinterpret_cast<uintptr_t>(out) | 2ull * static_cast<unsigned long long>(desc->out_token_stride | desc->out_head_stride)) % 16 == 0;
     wait_limits(p);
     const ChunkPlan plan = chunk_plan(desc, cache, mixed(desc));
+    p.joins = static_cast<ChunkJoin *>(desc->workspace);
+    p.part = reinterpret_cast<float *>(static_cast<char *>(desc->workspace) + join_bytes(chunk_plan(desc, cache, true)));
     cudaStream_t st = static_cast<cudaStream_t>(desc->stream);
     const bool bf = desc->dtype == MCSD_DTYPE_BF16;
     if (cache->head_dim == 128) return bf ? launch_chunk<MCSD_DTYPE_BF16, 128>(p, plan, st) : launch_chunk<MCSD_DTYPE_F16, 128>(p, plan, st);
