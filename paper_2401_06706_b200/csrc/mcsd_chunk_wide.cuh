@@ -13,7 +13,8 @@ constexpr int kChunkThreads = 640;                  // 8 softmax warps, 8 decodi
 constexpr float kChunkHead = 4.f;                   // log2 of a row's largest weight when its reference is set
 constexpr float kChunkMost = 2048.f;                // sum of the weights of half a unit above which the reference moves (half holds 2^15, and 16 times this)
 template <int D> constexpr int kChunkAhead = D == 128 ? 1 : 3;         // units whose codes are on their way to shared memory
-template <int D> constexpr int kChunkSmem = 1024 + 6 * kWideTile<D> + 2 * kAttUnit * 8 + kChunkAhead<D> * kAttUnit * (D + 8);
+constexpr int kChunkParams = 4;                     // units whose parameters are kept
+template <int D> constexpr int kChunkSmem = 1024 + 6 * kWideTile<D> + kChunkParams * kAttUnit * 8 + kChunkAhead<D> * kAttUnit * (D + 16);
 
 // D (tensor memory) (+)= A (shared memory, 128 rows x 16) * B (shared memory), halves in, float32 out.
 __device__ __forceinline__ void tc_mma_ss(uint32_t d, uint32_t a_low, uint32_t b_low, uint32_t high, uint32_t idesc, bool add) {
@@ -56,7 +57,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
     __shared__ __align__(8) unsigned long long s_bar[23];
     __shared__ uint32_t s_tmem;
     __shared__ int s_dead;
-    __shared__ uint32_t s_valid[2][4], s_bad[2][4], s_far[2][4];        // keys of a stage that are there; values that are no numbers, or far from one
+    // of a unit: keys that are there; values that are no numbers, or far from one
+    __shared__ __align__(16) uint32_t s_valid[kChunkParams][4], s_bad[kChunkParams][4], s_far[kChunkParams][4];
     // Each warp goes over the CTA's blocks for itself; where it stands is kept here, since registers are short.
     __shared__ ChunkRows::Walk s_walk[kChunkThreads / 32];
     __shared__ AttItem s_item[kChunkThreads / 32];
@@ -65,8 +67,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
 
     unsigned char *base = s_raw + ((1024 - (smem_u32(s_raw) & 1023)) & 1023);
     unsigned char *s_q = base, *s_k = base + 2 * TILE, *s_v = base + 4 * TILE;  // Q of both tiles, two stages each of keys and values
-    float4 *s_param = reinterpret_cast<float4 *>(base + 6 * TILE);              // [stages][64 pairs of keys]
-    unsigned char *s_codes = reinterpret_cast<unsigned char *>(s_param + 2 * (kAttUnit / 2));   // [decoding warps][AHEAD]{codes, parameters}
+    float4 *s_param = reinterpret_cast<float4 *>(base + 6 * TILE);              // [kChunkParams][64 pairs of keys]
+    unsigned char *s_codes = reinterpret_cast<unsigned char *>(s_param + kChunkParams * (kAttUnit / 2));   // [decoding warps][AHEAD]{codes, parameters}
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bars = smem_u32(s_bar);
@@ -75,12 +77,12 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(b_kfull + 8 * i, 4);          // (arrivals of warps)
-            mbar_init(b_kempty + 8 * i, 10);        // the products of both tiles, and the softmax warps, which read the parameters
+            mbar_init(b_kempty + 8 * i, 2);         // (the products of both tiles)
             mbar_init(b_vfull + 8 * i, 4);
             mbar_init(b_vempty + 8 * i, 2);
             mbar_init(b_ready + 8 * i, 4 + P.test_extra);       // (0 but in a test of the expiry path: arrivals that never come)
             for (int h = 0; h < 2; ++h) {
-                mbar_init(b_s + 16 * i + 8 * h, 1);
+                mbar_init(b_s + 16 * i + 8 * h, 2);             // (the products, and the warp that has seen the keys' parameters)
                 mbar_init(b_p + 16 * i + 8 * h, 4);
                 mbar_init(b_o + 16 * i + 8 * h, 1);
             }
@@ -136,8 +138,9 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
         const int which = (warp >> 2) & 1, key0 = (warp & 3) * 32;       // which: 0 key rows, 1 value rows
         const int c = lane % CH;
         const uint32_t full = which ? b_vfull : b_kfull, empty = which ? b_vempty : b_kempty;
-        unsigned char *ring = s_codes + (warp & 7) * AHEAD * 32 * (RB + 4);
-        int stage = 0;
+        constexpr int SLOT = 32 * (RB + 8);         // codes, parameters of these rows, parameters of the values (key warps)
+        unsigned char *ring = s_codes + (warp & 7) * AHEAD * SLOT;
+        int stage = 0, keep = 0;                    // stage of the unit, and where its parameters are kept
         uint32_t phase = 1;                         // (the first round of stages is free)
         for_items([&](const AttItem &it) MCSD_INLINE {
             const int len = it.len, k1 = it.k1;
@@ -152,7 +155,7 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
             int page = -1;                          // of the unit asked for next
             auto issue = [&](int unit, int slot) MCSD_INLINE {
                 const int pos = unit * kAttUnit + key0 + lane;
-                unsigned char *to = ring + slot * 32 * (RB + 4);
+                unsigned char *to = ring + slot * SLOT;
                 if (unit < k1) {
                     const bool ok = static_cast<unsigned>(page) < static_cast<unsigned>(P.c.n_pages) && pos < len;
                     there = (there & ~(1u << slot)) | static_cast<uint32_t>(ok) << slot;
@@ -165,7 +168,11 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                             for (int i = 0; i < CH / 2; ++i) cp_async16(smem_u32(to + (hf * (CH / 2) + i) * 512 + lane * 16), src + 512 * i);
                         }
                     }
-                    if (ok) cp_async4(to + 32 * RB + lane * 4, pool + page * P.c.page_stride + ps * D + (which * ps + (pos & (ps - 1))) * 4);
+                    if (ok) {
+                        const unsigned char *src = pool + page * P.c.page_stride + ps * D + (pos & (ps - 1)) * 4;
+                        cp_async4(to + 32 * RB + lane * 4, src + which * ps * 4);
+                        if (which == 0) cp_async4(to + 32 * RB + 128 + lane * 4, src + ps * 4);
+                    }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
             };
@@ -181,18 +188,24 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
             int slot = 0;
             for (int k = it.k0; k < k1; ++k) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
-                unsigned char *from = ring + slot * 32 * (RB + 4);
+                const unsigned char *from = ring + slot * SLOT;
                 // what this lane copied itself: its codes, and the parameters of its key
                 uint4 code[CH];
 #pragma unroll
                 for (int i = 0; i < CH; ++i) code[i] = *reinterpret_cast<const uint4 *>(from + i * 512 + lane * 16);
                 const bool mine = (there >> slot) & 1u;
                 const uint32_t raw = *reinterpret_cast<const uint32_t *>(from + 32 * RB + lane * 4);
+                const uint32_t raw_value = *reinterpret_cast<const uint32_t *>(from + 32 * RB + 128 + lane * 4);      // (of a key warp)
                 issue(k + AHEAD, slot);
                 page = page_of(k + AHEAD + 1);      // (in flight until the next unit is asked for)
                 slot = slot == AHEAD - 1 ? 0 : slot + 1;
                 wide_wait(empty + 8 * stage, phase, dead, P.wait_polls);
                 const float2 p = mine ? __half22float2(*reinterpret_cast<const __half2 *>(&raw)) : make_float2(0.f, 0.f);
+                // values that are numbers, and those that half may not hold (a row's ends, by the roundings of its scale and mid)
+                const float2 pv = which == 0 && mine ? __half22float2(*reinterpret_cast<const __half2 *>(&raw_value)) : p;
+                const bool sound = fabsf(pv.x) <= 65504.f && fabsf(pv.y) <= 65504.f;
+                const uint32_t bad = __ballot_sync(0xffffffffu, mine && !sound);
+                const uint32_t far = __ballot_sync(0xffffffffu, mine && sound && fmaf(8.f, fabsf(pv.x), fabsf(pv.y)) > 65000.f);
                 unsigned char *tiles = (which ? s_v : s_k) + stage * TILE;
                 auto place = [&](int i, int j) MCSD_INLINE {            // where 16 bytes of operands go: chunk i of the lane, its word j
                     const int key = key0 + (i / (CH / 2)) * 16 + (i % (CH / 2)) * (32 / CH) + lane / CH;
@@ -214,18 +227,15 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                             *place(i, turn ? j ^ 2 : j) = make_uint4(w & 0x000f000fu, w & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
                         }
                     const int key = key0 + lane;
-                    float *par = reinterpret_cast<float *>(s_param + stage * (kAttUnit / 2) + (key >> 1)) + (key & 1);
+                    float *par = reinterpret_cast<float *>(s_param + keep * (kAttUnit / 2) + (key >> 1)) + (key & 1);
                     par[0] = p.x;
                     par[2] = fmaf(-8.f, p.x, p.y);
                     const uint32_t keys = __ballot_sync(0xffffffffu, mine);
-                    if (lane == 0) s_valid[stage][warp & 3] = keys;
+                    if (lane == 0) { s_valid[keep][warp & 3] = keys; s_bad[keep][warp & 3] = bad; s_far[keep][warp & 3] = far; }
                 } else {
-                    // values: numbers in half, rounded once. Rows that are no numbers are marked, and zeros here; those that may leave half's
-                    // range are stored as a sixteenth and marked, and their weights are sixteen times as large
-                    const bool sound = fabsf(p.x) <= 65504.f && fabsf(p.y) <= 65504.f;
-                    const uint32_t ok = __ballot_sync(0xffffffffu, mine && sound), bad = __ballot_sync(0xffffffffu, mine && !sound);
-                    const uint32_t far = __ballot_sync(0xffffffffu, mine && sound && fmaf(8.f, fabsf(p.x), fabsf(p.y)) > 65000.f);
-                    uint32_t own = (ok >> lane) & 1u ? raw : 0u;
+                    // values: numbers in half, rounded once. Rows that are no numbers are zeros here (and marked); those that half may not hold
+                    // are stored as a sixteenth, and their weights are sixteen times as large
+                    uint32_t own = mine && sound ? raw : 0u;
                     if ((far >> lane) & 1u) own = half2_bits(p.x * 0.0625f, p.y * 0.0625f);
 #pragma unroll
                     for (int i = 0; i < CH; ++i) {
@@ -239,11 +249,11 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                             *place(i, turn ? j ^ 2 : j) = *reinterpret_cast<const uint4 *>(x);
                         }
                     }
-                    if (lane == 0) { s_bad[stage][warp & 3] = bad; s_far[stage][warp & 3] = far; }
                 }
                 fence_proxy_async();
                 warp_arrive(full + 8 * stage, lane);
                 if (++stage == 2) { stage = 0; phase ^= 1; }
+                keep = (keep + 1) % kChunkParams;
             }
         });
         asm volatile("cp.async.wait_all;" ::: "memory");
@@ -267,6 +277,7 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                     tc_mma_ss(tmem + kS + 128 * x + 64 * h, q_at + off, at + off, kOperandHigh, tc_shape(64, false), s > 0);
                 }
                 tc_commit(b_s + 16 * x + 8 * h);
+                warp_arrive(b_s + 16 * x + 8 * h, lane);
                 if (h == 1) {
                     tc_commit(b_kempty + 8 * ahead);
                     if (++ahead == 2) { ahead = 0; ahead_phase ^= 1; }
@@ -321,8 +332,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
         const int r = tid & 127;                    // row of the tile = lane of tensor memory
         const uint32_t mine = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + mine + kS + 128 * x, t_o = tmem + mine + kO + D * x;
-        int stage = 0;
-        uint32_t phase = 0, n = 0;
+        int keep = 0;                               // where the unit's parameters are kept
+        uint32_t n = 0;
         for_items([&](const AttItem &it) MCSD_INLINE {
             if (tid == 0) chunk_join_note(P, it);
             const int row = it.row0 + 128 * x + r;
@@ -394,9 +405,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
             }
             float ref = kNoTop, sum = 0.f;
             for (int k = k0; k < k1; ++k) {
-                wide_wait(b_kfull + 8 * stage, phase, dead, P.wait_polls);
                 if (k < units) {
-                    const float4 *par = s_param + stage * (kAttUnit / 2);
+                    const float4 *par = s_param + keep * (kAttUnit / 2);
                     // One half of the unit's keys, where every row of the tile sees them and nothing is odd about the values: the
                     // weights with the reference as it is; false (and nothing stored) should their sum be too large for half.
                     auto swift = [&](int h) MCSD_INLINE {
@@ -467,7 +477,7 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {           // (what is stored lies over scores that are read)
                             const uint32_t see = (c < 2 ? see0 : see1) >> (16 * (c & 1));
-                            const uint32_t bad = see & s_bad[stage][2 * h + (c >> 1)] >> (16 * (c & 1)), far = s_far[stage][2 * h + (c >> 1)] >> (16 * (c & 1));
+                            const uint32_t bad = see & s_bad[keep][2 * h + (c >> 1)] >> (16 * (c & 1)), far = s_far[keep][2 * h + (c >> 1)] >> (16 * (c & 1));
                             uint32_t acc[16], w[8];
                             __syncwarp();
                             tmem_load16(t_s + 64 * h + 16 * c, acc);
@@ -496,9 +506,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                         wide_wait(b_s + 16 * x + 8 * h, n & 1, dead, P.wait_polls);
                         tc_after_sync();
                         const int pos0 = k * kAttUnit + 64 * h;
-                        const uint32_t there0 = s_valid[stage][2 * h], there1 = s_valid[stage][2 * h + 1];
-                        if (h == 0) wide_wait(b_vfull + 8 * stage, phase, dead, P.wait_polls);   // (the marks of the values)
-                        const uint32_t odd = s_bad[stage][2 * h] | s_bad[stage][2 * h + 1] | s_far[stage][2 * h] | s_far[stage][2 * h + 1];
+                        const uint32_t there0 = s_valid[keep][2 * h], there1 = s_valid[keep][2 * h + 1];
+                        const uint32_t odd = s_bad[keep][2 * h] | s_bad[keep][2 * h + 1] | s_far[keep][2 * h] | s_far[keep][2 * h + 1];
                         const bool plain = (there0 & there1) == 0xffffffffu && odd == 0u && pos0 + 64 <= all;
                         if (!plain || (k == k0 && h == 0) || !swift(h)) {       // (at first there is no reference)
                             auto first = [](int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; };
@@ -510,8 +519,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                     }
                     ++n;
                 }
-                warp_arrive(b_kempty + 8 * stage, lane);        // the parameters are read
-                if (++stage == 2) { stage = 0; phase ^= 1; }
+                // (what is kept of a unit is written over four units later, when this tile's products of the one after it are through)
+                keep = (keep + 1) % kChunkParams;
             }
             // ---- the end of the block
             if (any) {
