@@ -7,6 +7,7 @@ namespace mcsd {
 
 constexpr int kEvictThreads = 256;
 constexpr int kEvictKeys = 8192;                    // weights that are kept on chip between the passes over them
+constexpr int kEvictList = 4 * kEvictThreads;       // rows that are listed and not moved yet: a batch, the next one, and what a round adds
 
 struct EvictParams {
     CacheParams c;
@@ -27,9 +28,9 @@ __device__ __forceinline__ uint32_t weight_key(float w)
 
 // One CTA per (layer, sequence, head) at a time. The bar, the largest weight that enough rows reach, comes from four passes over the
 // weights, eight bits each (a count of every value of the bits in shared memory, then a search from the top); up to kEvictKeys
-// weights stay in shared memory between the passes. Then the rows are gone through in order, 256 at a time: those
-// that stay get their places by ballots and are moved, 16 bytes a thread, all of a round read before one is written. A place is never behind
-// its row, so that a round overwrites nothing that a later one reads, and the next round's places are found while rows are on their way.
+// weights stay in shared memory between the passes. Then the rows are gone through in order: those that
+// stay are listed by ballots and moved 256 at a time, 16 bytes a thread, all of a batch read before one is written. A place is never behind
+// its row, so that a batch overwrites nothing that a later one reads; the next batch is listed while rows are on their way.
 template <int D>
 __global__ void __launch_bounds__(kEvictThreads, 4)
 evict_kernel(const __grid_constant__ EvictParams P)
@@ -37,7 +38,8 @@ evict_kernel(const __grid_constant__ EvictParams P)
     constexpr int WARPS = kEvictThreads / 32, CH = D / 16;          // 16-byte pieces of a row: keys, then values
     extern __shared__ uint32_t s_key[];
     __shared__ int s_count[WARPS], s_tie[WARPS], s_bins[256], s_pick[2];
-    __shared__ int s_from[kEvictThreads], s_from_page[kEvictThreads], s_to[kEvictThreads], s_to_page[kEvictThreads];
+    __shared__ int s_from[kEvictList];              // rows that stay, a ring
+    __shared__ longlong2 s_move[kEvictThreads];     // of a batch: offsets of the key codes where a row is and where it goes, -1: it stays where it is
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ps = 1 << P.c.page_shift;
     const long long items = P.n_layers * P.batch * P.c.n_heads;
@@ -97,65 +99,84 @@ evict_kernel(const __grid_constant__ EvictParams P)
                 ties = s_pick[1];
             }
         }
-        // ---- the rows, 256 at a time
-        int kept = sink;
-        for (int pos0 = sink; pos0 < len; pos0 += kEvictThreads) {
-            const int pos = pos0 + tid;
-            const uint32_t key = pos < end ? key_of(pos - sink) : 0u;
-            const bool safe = pos >= end && pos < len, tie = pos < end && key == bar;
-            const unsigned tie_mask = __ballot_sync(0xffffffffu, tie);
-            if (lane == 0) s_tie[warp] = __popc(tie_mask);
-            __syncthreads();                        // (and the round before has read its places)
-            int before = __popc(tie_mask & ((1u << lane) - 1u)), all = 0;
+        // ---- the rows in order: those that stay are listed, and moved 256 at a time
+        int listed = 0, moved = 0, pos0 = sink;     // rows listed and moved so far; the next position to look at
+        // Goes on until `upto` rows are listed or there are no more.
+        auto list = [&](int upto) {
+            while (pos0 < len && listed < upto) {
+                const int pos = pos0 + tid;
+                pos0 += kEvictThreads;
+                const uint32_t key = pos < end ? key_of(pos - sink) : 0u;
+                const bool safe = pos >= end && pos < len, tie = pos < end && key == bar;
+                const unsigned tie_mask = __ballot_sync(0xffffffffu, tie), sure = __ballot_sync(0xffffffffu, safe || (pos < end && key > bar));
+                __syncthreads();                    // (the counts of the round before are read)
+                if (lane == 0) { s_tie[warp] = __popc(tie_mask); s_count[warp] = __popc(sure); }
+                __syncthreads();
+                // (a warp's ties are kept as far as those of the warps before it leave room)
+                int left = ties, rank = listed, all = 0, room = 0;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) { before += w < warp ? s_tie[w] : 0; all += s_tie[w]; }
-            const bool stays = safe || (pos < end && key > bar) || (tie && before < ties);
-            ties -= min(all, ties);
-            const unsigned mask = __ballot_sync(0xffffffffu, stays);
-            if (lane == 0) s_count[warp] = __popc(mask);
-            __syncthreads();
-            int rank = __popc(mask & ((1u << lane) - 1u)), count = 0;
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) { rank += w < warp ? s_count[w] : 0; count += s_count[w]; }
-            if (stays) {
-                const int to = kept + rank, from_page = page_of(pos), to_page = page_of(to);
-                const bool moves = to != pos && from_page >= 0 && to_page >= 0;
-                s_from[rank] = pos;
-                s_to[rank] = to;
-                s_from_page[rank] = moves ? from_page : -1;
-                s_to_page[rank] = to_page;
+                for (int w = 0; w < WARPS; ++w) {
+                    const int took = min(s_tie[w], left);
+                    if (w < warp) rank += s_count[w] + took;
+                    if (w == warp) room = took;
+                    all += s_count[w] + took;
+                    left -= took;
+                }
+                ties = left;
+                const bool stays = safe || (pos < end && key > bar) || (tie && __popc(tie_mask & ((1u << lane) - 1u)) < room);
+                const unsigned mask = __ballot_sync(0xffffffffu, stays);
+                if (stays) s_from[(rank + __popc(mask & ((1u << lane) - 1u))) % kEvictList] = pos;
+                listed += all;
             }
-            kept += count;
+            __syncthreads();
+        };
+        list(kEvictThreads);
+        while (moved < listed) {
+            const int count = min(listed - moved, kEvictThreads);
+            // where this thread's row comes from and goes to
+            int from = 0, to = 0, from_page = -1, to_page = -1;
+            if (tid < count) {
+                from = s_from[(moved + tid) % kEvictList];
+                to = sink + moved + tid;
+                if (from != to) {
+                    from_page = page_of(from);
+                    to_page = page_of(to);
+                    if (to_page < 0) from_page = -1;
+                }
+                s_move[tid] = from_page < 0 ? make_longlong2(-1, 0) :
+                    make_longlong2(from_page * P.c.page_stride + (from & (ps - 1)) * (D / 2), to_page * P.c.page_stride + (to & (ps - 1)) * (D / 2));
+            }
             __syncthreads();
             uint4 row[CH];
 #pragma unroll
             for (int u = 0; u < CH; ++u) {
                 const int x = tid + u * kEvictThreads, j = x / CH, c = x % CH;
-                if (j < count && s_from_page[j] >= 0)
-                    row[u] = *reinterpret_cast<const uint4 *>(pages + s_from_page[j] * P.c.page_stride + ((c / (CH / 2)) * ps + (s_from[j] & (ps - 1))) * (D / 2) + (c % (CH / 2)) * 16);
+                if (j < count && s_move[j].x >= 0)
+                    row[u] = *reinterpret_cast<const uint4 *>(pages + s_move[j].x + (c / (CH / 2)) * ps * (D / 2) + (c % (CH / 2)) * 16);
             }
             uint32_t key_param = 0u, value_param = 0u;
             float weight = 0.f;
-            const bool mine = tid < count && s_from_page[tid] >= 0;
-            if (mine) {
-                const uint32_t *param = reinterpret_cast<const uint32_t *>(pages + s_from_page[tid] * P.c.page_stride + ps * D) + (s_from[tid] & (ps - 1));
+            if (from_page >= 0) {
+                const uint32_t *param = reinterpret_cast<const uint32_t *>(pages + from_page * P.c.page_stride + ps * D) + (from & (ps - 1));
                 key_param = param[0];
                 value_param = param[ps];
-                weight = *weight_at(s_from_page[tid], s_from[tid]);
+                weight = *weight_at(from_page, from);
             }
-            __syncthreads();                        // every row of the round is read before one is written
+            list(moved + 2 * kEvictThreads);        // (the next batch, while these rows are on their way; its barriers stand between reading and writing)
 #pragma unroll
             for (int u = 0; u < CH; ++u) {
                 const int x = tid + u * kEvictThreads, j = x / CH, c = x % CH;
-                if (j < count && s_from_page[j] >= 0)
-                    *reinterpret_cast<uint4 *>(pages + s_to_page[j] * P.c.page_stride + ((c / (CH / 2)) * ps + (s_to[j] & (ps - 1))) * (D / 2) + (c % (CH / 2)) * 16) = row[u];
+                if (j < count && s_move[j].x >= 0)
+                    *reinterpret_cast<uint4 *>(pages + s_move[j].y + (c / (CH / 2)) * ps * (D / 2) + (c % (CH / 2)) * 16) = row[u];
             }
-            if (mine) {
-                uint32_t *param = reinterpret_cast<uint32_t *>(pages + s_to_page[tid] * P.c.page_stride + ps * D) + (s_to[tid] & (ps - 1));
+            if (from_page >= 0) {
+                uint32_t *param = reinterpret_cast<uint32_t *>(pages + to_page * P.c.page_stride + ps * D) + (to & (ps - 1));
                 param[0] = key_param;
                 param[ps] = value_param;
-                *weight_at(s_to_page[tid], s_to[tid]) = weight;
+                *weight_at(to_page, to) = weight;
             }
+            moved += count;
+            __syncthreads();                        // (the places of these rows are read)
         }
         __syncthreads();
     }

@@ -175,14 +175,14 @@ int launch_weigh(ChunkParams p, bool may_mix, cudaStream_t st)
     return rc == MCSD_OK ? launched(n) : rc;
 }
 
-// Rows that leave multiprocessors idle get CTAs of 1024 threads (their latency counts), others 256, six to a multiprocessor.
+// Rows that leave multiprocessors idle get CTAs of 1024 threads (their latency counts), others 256, eight to a multiprocessor.
 template <int DT>
 int launch_logprobs(const LogprobParams &p, bool vec, cudaStream_t st)
 {
     const long long sms = sm_count();
     if (sms <= 0) return MCSD_ERR_CUDA;
     const bool few = p.n_out <= 2 * sms;
-    const unsigned grid = static_cast<unsigned>(few || p.n_out < 6 * sms ? p.n_out : 6 * sms);
+    const unsigned grid = static_cast<unsigned>(p.n_out);
     if (few) {
         if (vec) logprob_kernel<DT, 1024, true><<<grid, 1024, 0, st>>>(p);
         else logprob_kernel<DT, 1024, false><<<grid, 1024, 0, st>>>(p);

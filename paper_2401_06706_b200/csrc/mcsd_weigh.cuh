@@ -1,8 +1,8 @@
 // The attention weight that cached rows gather of a chunk's tokens: a key's share of every row that sees it, summed per key head.
 #pragma once
 
-#include "mcsd_attend_wide.cuh"
 #include "mcsd_chunk.cuh"
+#include "mcsd_chunk_wide.cuh"
 
 namespace mcsd {
 
@@ -232,19 +232,29 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
                 }
         }
 
+        // this lane's own key of a chunk's 32, for the end: where its weight is (none: null), and what it was
+        const int mine = 16 * (t >> 1) + 8 * (t & 1) + kg;
+        float *w = nullptr;
+        float old = 0.f;
+        auto own = [&](int i, int slot) {
+            const int pos = (k0 + i) * kAttUnit + warp * kNarrowKeys + mine;
+            const int2 pages = s_pages[warp][slot];
+            const int page = mine < 16 ? pages.x : pages.y;
+            w = i < n_chunks && page >= 0 && pos < len ? P.weights + (static_cast<long long>(page) * P.c.n_heads + it.head) * ps + (pos & (ps - 1)) : nullptr;
+            old = w && pos < it.s.old && P.decay != 0.f ? *w : 0.f;
+        };
+        __syncwarp();
+        own(0, 0);
         int slot = 0, fill = STAGES - 1;
         for (int i = 0; i < n_chunks; ++i) {
             asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
             __syncwarp();                           // every lane's copies of chunk i are there, and chunk i - 1 is done with
             const unsigned char *stage = ring + slot * STAGE;
-            const int2 pages = s_pages[warp][slot];
             issue(i + STAGES - 1, fill);
             const int pos0 = (k0 + i) * kAttUnit + warp * kNarrowKeys;
-            // this lane's own key of the 32, for the end
-            const int mine = 16 * (t >> 1) + 8 * (t & 1) + kg, pos = pos0 + mine, page = mine < 16 ? pages.x : pages.y;
-            float *w = P.weights + (static_cast<long long>(page) * P.c.n_heads + it.head) * ps + (pos & (ps - 1));
-            const bool there = page >= 0 && pos < len;
-            const float old = there && pos < it.s.old && P.decay != 0.f ? P.decay * *w : 0.f;
+            float *const to = w;
+            const float from = P.decay * old;
+            own(i + 1, slot == STAGES - 1 ? 0 : slot + 1);          // (in flight until the next chunk's end)
             const bool plain = pos0 + kNarrowKeys - 1 <= pos_first;
             const __half2 *kp = reinterpret_cast<const __half2 *>(stage + kNarrowKeys * RB);
             float got[2][2];
@@ -302,7 +312,7 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
                     v += __shfl_xor_sync(0xffffffffu, v, 2);
                     if (t == 2 * m + x) sum = v;
                 }
-            if (there) *w = old + sum;
+            if (to) *to = from + sum;
             slot = slot == STAGES - 1 ? 0 : slot + 1;
             fill = fill == STAGES - 1 ? 0 : fill + 1;
         }
@@ -482,7 +492,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
             for_blocks([&](const WeighItem &, int, int n_tokens, int k0, int k1) MCSD_INLINE {
                 wide_wait(b_ready, blocks & 1, dead, P.wait_polls);
                 ++blocks;
-                const uint32_t shape = tc_shape((n_tokens * P.group + 31) & ~31, false);
+                const uint32_t shape = tc_shape((n_tokens * P.group + 63) & ~63, false);
                 for (int k = k0; k < k1; ++k) {
                     const int x = k & 1;
                     wide_wait(b_full + 8 * stage, phase, dead, P.wait_polls);
@@ -512,7 +522,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
         uint32_t phase = 0, n = 0;
         auto both = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
         for_blocks([&](const WeighItem &it, int i0, int n_tokens, int k0, int k1) MCSD_INLINE {
-            const int n_rows = n_tokens * P.group, columns = (n_rows + 31) & ~31;
+            const int n_rows = n_tokens * P.group, columns = (n_rows + 63) & ~63;
             float factor;                           // log2 units per unit of scale acc + (mid - 8 scale) rho
             {
                 // queries of the block: row `tid`, in the order that the ANDs of the keys give
@@ -574,11 +584,14 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
             }
             const int32_t *table = P.table + it.b * P.ld_table;
             const long long first = static_cast<long long>(it.s.pos) + i0;      // position of the block's first token
+            const int len = it.s.len;
+            auto page_of = [&](int k) MCSD_INLINE { return k < k1 && k * kAttUnit + r < len ? __ldg(table + ((k * kAttUnit + r) >> P.c.page_shift)) : -1; };
+            int page_next = page_of((k0 & 1) == x ? k0 : k0 + 1);
             for (int k = k0; k < k1; ++k) {
                 if ((k & 1) == x) {
                     // where this key's weight lies, and what it starts from
-                    const int pos = k * kAttUnit + r;
-                    const int page = pos < it.s.len ? __ldg(table + (pos >> P.c.page_shift)) : -1;
+                    const int pos = k * kAttUnit + r, page = page_next;
+                    page_next = page_of(k + 2);
                     const bool there = static_cast<unsigned>(page) < static_cast<unsigned>(P.c.n_pages);
                     float *w = P.weights + (static_cast<long long>(there ? page : 0) * P.c.n_heads + it.head) * ps + (pos & (ps - 1));
                     float old = 0.f;
@@ -596,12 +609,12 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                     auto add = [&](auto plain_tag, int from) MCSD_INLINE {              // from: first column that sees the key
                         constexpr bool plain = decltype(plain_tag)::value;
 #pragma unroll 1
-                        for (int c = 0; c < columns; c += 32) {
-                            uint32_t acc[32];
-                            tmem_load32(t_s + c, acc);
+                        for (int c = 0; c < columns; c += 64) {
+                            uint32_t acc[64];
+                            tmem_load64(t_s + c, acc);
                             const float4 *col = reinterpret_cast<const float4 *>(s_col) + (c >> 1);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) {
+                            for (int j = 0; j < 32; ++j) {
                                 const float4 v = col[j];
                                 const float2 t = fma2(m, make_float2(v.x, v.y), make_float2(-v.z, -v.w));
                                 const float2 e = fma2(a, make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), t);
