@@ -6,7 +6,8 @@
 namespace mcsd {
 
 constexpr int kEvictThreads = 256;
-constexpr int kEvictKeys = 8192;                    // weights that are kept on chip between the passes over them
+constexpr int kEvictBins = 2048;                    // values of the eleven bits that a pass counts
+constexpr int kEvictKeys = 7168;                    // weights that are kept on chip between the passes over them (with the bins, what a CTA has without asking)
 constexpr int kEvictList = 4 * kEvictThreads;       // rows that are listed and not moved yet: a batch, the next one, and what a round adds
 
 struct EvictParams {
@@ -26,8 +27,8 @@ __device__ __forceinline__ uint32_t weight_key(float w)
     return w != w ? 0u : (u >> 31) ? ~u : u | 0x80000000u;
 }
 
-// One CTA per (layer, sequence, head) at a time. The bar, the largest weight that enough rows reach, comes from four passes over the
-// weights, eight bits each (a count of every value of the bits in shared memory, then a search from the top); up to kEvictKeys
+// One CTA per (layer, sequence, head) at a time. The bar, the largest weight that enough rows reach, comes from three passes over the
+// weights, eleven bits each (a count of every value of the bits in shared memory, then a search from the top); up to kEvictKeys
 // weights stay in shared memory between the passes. Then the rows are gone through in order: those that
 // stay are listed by ballots and moved 256 at a time, 16 bytes a thread, all of a batch read before one is written. A place is never behind
 // its row, so that a batch overwrites nothing that a later one reads; the next batch is listed while rows are on their way.
@@ -37,13 +38,14 @@ evict_kernel(const __grid_constant__ EvictParams P)
 {
     constexpr int WARPS = kEvictThreads / 32, CH = D / 16;          // 16-byte pieces of a row: keys, then values
     extern __shared__ uint32_t s_key[];
-    __shared__ int s_count[WARPS], s_tie[WARPS], s_bins[256], s_pick[2];
+    __shared__ int s_count[WARPS], s_tie[WARPS], s_pick[2];
+    __shared__ __align__(16) int s_bins[kEvictBins];
     __shared__ int s_from[kEvictList];              // rows that stay, a ring
     __shared__ longlong2 s_move[kEvictThreads];     // of a batch: offsets of the key codes where a row is and where it goes, -1: it stays where it is
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ps = 1 << P.c.page_shift;
     const long long items = P.n_layers * P.batch * P.c.n_heads;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {      // (one, but for a million CTAs)
         const int head = static_cast<int>(item % P.c.n_heads), b = static_cast<int>(item / P.c.n_heads % P.batch);
         const long long layer = item / P.c.n_heads / P.batch;
         const int held = __ldg(P.len + b), keep = P.keep_len ? __ldg(P.keep_len + b) : P.keep;
@@ -66,24 +68,39 @@ evict_kernel(const __grid_constant__ EvictParams P)
         };
         // ---- the bar: `want` of the keys of [sink, end) are above it, or equal to it and among the first `ties` that are
         const int n = end - sink, held_keys = min(n, P.n_keys);
-        for (int i = tid; i < held_keys; i += kEvictThreads) s_key[i] = read_key(sink + i);
+        for (int i0 = tid; i0 < held_keys; i0 += 8 * kEvictThreads) {           // (eight pages, then eight weights on their way)
+            int page[8];
+            float w[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) page[u] = i0 + u * kEvictThreads < held_keys ? page_of(sink + i0 + u * kEvictThreads) : -1;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) w[u] = page[u] < 0 ? 0.f : *weight_at(page[u], sink + i0 + u * kEvictThreads);
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i0 + u * kEvictThreads < held_keys) s_key[i0 + u * kEvictThreads] = page[u] < 0 ? 0u : weight_key(w[u]);
+        }
         auto key_of = [&](int i) { return i < held_keys ? s_key[i] : read_key(sink + i); };
         uint32_t bar = 0u;
         int ties = want;
         if (want == 0) {
             bar = 0xffffffffu;                      // (the key of no number)
         } else {
-            for (int shift = 24; shift >= 0; shift -= 8) {
-                s_bins[tid] = 0;
+            for (int shift = 21; shift >= 0; shift = shift == 10 ? 0 : shift - 11) {        // bits 31..21, 20..10, 9..0
+                const int bits = shift == 0 ? 10 : 11;
+#pragma unroll
+                for (int u = 0; u < kEvictBins / 4 / kEvictThreads; ++u) reinterpret_cast<int4 *>(s_bins)[tid + u * kEvictThreads] = make_int4(0, 0, 0, 0);
                 __syncthreads();                    // (for the first pass: the keys are there, too)
                 for (int i = tid; i < n; i += kEvictThreads) {
                     const uint32_t key = key_of(i);
-                    if (shift == 24 || (key ^ bar) >> (shift + 8) == 0u) atomicAdd(&s_bins[key >> shift & 255u], 1);
+                    if (shift == 21 || (key ^ bar) >> (shift + bits) == 0u) atomicAdd(&s_bins[key >> shift & ((1u << bits) - 1u)], 1);
                 }
                 __syncthreads();
-                // keys in bins above this thread's
-                const int bin = 255 - tid, own = s_bins[bin];
-                int above = own;
+                // each thread has eight bins, the highest first; how many keys are above them
+                const int top = kEvictBins - 1 - 8 * tid;
+                int own[8], sum = 0;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) { own[u] = s_bins[top - u]; sum += own[u]; }
+                int above = sum;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
                     const int up = __shfl_up_sync(0xffffffffu, above, o);
@@ -92,8 +109,12 @@ evict_kernel(const __grid_constant__ EvictParams P)
                 if (lane == 31) s_count[warp] = above;
                 __syncthreads();
                 for (int w = 0; w < warp; ++w) above += s_count[w];
-                above -= own;
-                if (above < ties && above + own >= ties) { s_pick[0] = bin; s_pick[1] = ties - above; }
+                above -= sum;
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    if (above < ties && above + own[u] >= ties) { s_pick[0] = top - u; s_pick[1] = ties - above; }
+                    above += own[u];
+                }
                 __syncthreads();
                 bar |= static_cast<uint32_t>(s_pick[0]) << shift;
                 ties = s_pick[1];

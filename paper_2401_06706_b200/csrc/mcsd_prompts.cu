@@ -286,10 +286,8 @@ int mcsd_evict_rows(const mcsd_evict_desc *d, const mcsd_kv_cache *cache)
     p.table = d->page_table; p.len = d->len; p.keep_len = d->keep_len; p.weights = d->weights; p.len_out = d->len_out;
     p.batch = d->batch; p.max_pages = d->max_pages; p.keep = d->keep; p.sink = d->sink; p.recent = d->recent;
     const long long items = d->n_layers * d->batch * cache->n_heads, room = static_cast<long long>(d->max_pages) * cache->page_size;
-    const int sms = sm_count();
-    if (sms <= 0) return MCSD_ERR_CUDA;
     p.n_keys = static_cast<int>(room < kEvictKeys ? room : kEvictKeys);
-    const unsigned grid = static_cast<unsigned>(items < 4LL * sms ? items : 4LL * sms);
+    const unsigned grid = static_cast<unsigned>(items < 1 << 20 ? items : 1 << 20);
     cudaStream_t st = static_cast<cudaStream_t>(d->stream);
     if (cache->head_dim == 128) evict_kernel<128><<<grid, kEvictThreads, 4 * p.n_keys, st>>>(p);
     else evict_kernel<64><<<grid, kEvictThreads, 4 * p.n_keys, st>>>(p);

@@ -147,10 +147,9 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
             const int page = i < n_chunks && pos < len ? __ldg(table + (pos >> P.c.page_shift)) : -1;
             return static_cast<unsigned>(page) < static_cast<unsigned>(P.c.n_pages) ? page : -1;
         };
-        int page_next = page_of(0);
+        int page_next = -1;
         auto issue = [&](int i, int slot) {
             const int page = page_next;
-            page_next = page_of(i + 1);             // (its load is in flight while the next chunk is computed)
             if (i < n_chunks) {
                 const int row = ((k0 + i) * kAttUnit + warp * kNarrowKeys) & (ps - 1);
                 int p[2];
@@ -169,32 +168,63 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        __syncwarp();                               // (the item before has read its last chunks)
+        // Pages of the first chunks, queries and lse are asked for before any of them is used.
+        int pages[STAGES];
 #pragma unroll
-        for (int i = 0; i < STAGES - 1; ++i) issue(i, i);
-
-        // queries: this lane's D / 4 numbers of row g of every tile, scaled to the top of half's range; its rows' lse in log2 units
-        uint32_t qb[NB][KS][2];
-        float ra[NB][2], rb[NB][2], lse[NB][2];
+        for (int i = 0; i < STAGES; ++i) pages[i] = page_of(i);
+        uint4 raw[NB][D / 32];
+        float lse[NB][2];
         int token[NB][2];                           // last position that the row sees
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const int r = nb * 8 + g;
-            float x[D / 4];
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) x[i] = 0.f;
+            for (int i = 0; i < D / 32; ++i) raw[nb][i] = make_uint4(0u, 0u, 0u, 0u);
             if (r < n_rows) {
                 const int i = r / P.group, h = it.head * P.group + (r - i * P.group);
                 const long long at = (static_cast<long long>(it.s.row) + i) * P.q_token + h * P.q_head + t * (D / 4);
                 if (P.q_vec) {
                     const uint4 *src = reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + at * 2);
 #pragma unroll
-                    for (int i = 0; i < D / 32; ++i) Elem<DT>::unpack(__ldg(src + i), x + 8 * i);
+                    for (int i = 0; i < D / 32; ++i) raw[nb][i] = __ldg(src + i);
                 } else {
+                    const unsigned short *src = static_cast<const unsigned short *>(P.q) + at;
 #pragma unroll
-                    for (int i = 0; i < D / 4; ++i) x[i] = load_elem<DT>(P.q, at + i);
+                    for (int i = 0; i < D / 32; ++i)
+                        raw[nb][i] = make_uint4(src[8 * i] | src[8 * i + 1] << 16, src[8 * i + 2] | src[8 * i + 3] << 16,
+                                                src[8 * i + 4] | src[8 * i + 5] << 16, src[8 * i + 6] | src[8 * i + 7] << 16);
                 }
             }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int row = nb * 8 + 2 * t + c;
+                float l = INFINITY;                 // (of no row, or one that saw nothing: no weight)
+                token[nb][c] = -1;
+                if (row < n_rows) {
+                    const int i = row / P.group, h = it.head * P.group + (row - i * P.group);
+                    l = __ldg(P.lse + (static_cast<long long>(it.s.row) + i) * P.n_heads + h) * 1.4426950408889634f;
+                    if (l == -INFINITY) l = INFINITY;
+                    token[nb][c] = pos_first + i;
+                }
+                lse[nb][c] = l;
+            }
+        }
+        __syncwarp();                               // (the item before has read its last chunks)
+#pragma unroll
+        for (int i = 0; i < STAGES - 1; ++i) {
+            page_next = pages[i];
+            issue(i, i);
+        }
+        page_next = pages[STAGES - 1];
+
+        // queries: this lane's D / 4 numbers of row g of every tile, scaled to the top of half's range
+        uint32_t qb[NB][KS][2];
+        float ra[NB][2], rb[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            float x[D / 4];
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) Elem<DT>::unpack(raw[nb][i], x + 8 * i);
             float most = 0.f, sum = 0.f;
 #pragma unroll
             for (int i = 0; i < D / 4; ++i) { most = fmaxf(most, fabsf(x[i])); sum += x[i]; }
@@ -212,16 +242,6 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
             for (int c = 0; c < 2; ++c) {
                 ra[nb][c] = __shfl_sync(0xffffffffu, per_acc, (2 * t + c) * 4);
                 rb[nb][c] = __shfl_sync(0xffffffffu, per_mid, (2 * t + c) * 4);
-                const int row = nb * 8 + 2 * t + c;
-                float l = INFINITY;                 // (of no row, or one that saw nothing: no weight)
-                token[nb][c] = -1;
-                if (row < n_rows) {
-                    const int i = row / P.group, h = it.head * P.group + (row - i * P.group);
-                    l = __ldg(P.lse + (static_cast<long long>(it.s.row) + i) * P.n_heads + h) * 1.4426950408889634f;
-                    if (l == -INFINITY) l = INFINITY;
-                    token[nb][c] = pos_first + i;
-                }
-                lse[nb][c] = l;
             }
 #pragma unroll
             for (int j = 0; j < JW; ++j)
@@ -251,6 +271,7 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
             __syncwarp();                           // every lane's copies of chunk i are there, and chunk i - 1 is done with
             const unsigned char *stage = ring + slot * STAGE;
             issue(i + STAGES - 1, fill);
+            page_next = page_of(i + STAGES);        // (in flight while this chunk is computed)
             const int pos0 = (k0 + i) * kAttUnit + warp * kNarrowKeys;
             float *const to = w;
             const float from = P.decay * old;

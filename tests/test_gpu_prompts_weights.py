@@ -195,7 +195,7 @@ def test_evict_against_reference(D, ps, keep, sink, recent):
     _same(got, ref.evict(pages.numpy(), w.numpy(), table.numpy(), length.numpy(), [keep] * 7, sink, recent, D, ps))
 
 
-@pytest.mark.parametrize("length", [255, 256, 257, 1023, 1025, 2600])
+@pytest.mark.parametrize("length", [255, 256, 257, 1023, 1025, 2600, 7200, 9000])
 @pytest.mark.parametrize("share", [0.02, 0.5, 0.97])
 def test_evict_long_sequences(length, share):
     pages, w, table, n = _evict_problem(length, [length], 1, 2, 64, 16)
