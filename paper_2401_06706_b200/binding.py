@@ -989,6 +989,7 @@ class TokenLogprobs:
         d.vocab, d.dtype, d.n_given, d.n_top = self.vocab, MCSD_DTYPE[dtype], self.n_given, self.n_top
         d.logprobs, d.entropy = self.logprobs.data_ptr(), _ptr(self.entropy)
         d.top_ids, d.top_logprobs = (self.top_ids.data_ptr(), self.top_logprobs.data_ptr()) if self.n_top else (None, None)
+        self._views = (None, None)
         _settle(self.device)
 
     def _call(self, rows, logits, ld, tokens, temperature, lead):
@@ -1001,8 +1002,11 @@ class TokenLogprobs:
             d.stream = stream
             rc = self.lib.mcsd_token_logprobs(d)
         _check(rc)
-        return LogprobOutput(self.logprobs[:n].view(tokens.shape), None if self.entropy is None else self.entropy[:n].view(lead),
-                             self.top_ids[:n].view(lead + (self.n_top,)), self.top_logprobs[:n].view(lead + (self.n_top,)))
+        if self._views[0] != (lead, tokens.dim()):   # (views of the outputs, made anew when the shape changes)
+            self._views = (lead, tokens.dim()), LogprobOutput(
+                self.logprobs[:n].view(tokens.shape), None if self.entropy is None else self.entropy[:n].view(lead),
+                self.top_ids[:n].view(lead + (self.n_top,)), self.top_logprobs[:n].view(lead + (self.n_top,)))
+        return self._views[1]
 
     def mcsd_token_logprobs(self, logits: torch.Tensor, tokens: torch.Tensor, *, temperature: float = 1.0,
                             row_index: Optional[torch.Tensor] = None) -> LogprobOutput:
