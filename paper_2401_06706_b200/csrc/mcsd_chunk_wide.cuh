@@ -53,6 +53,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
 {
     constexpr int TILE = kWideTile<D>, RB = D / 2, AHEAD = kChunkAhead<D>;
     constexpr uint32_t kS = 0, kO = 256, kColumns = 512;                // S: 64 columns per tile and half of a unit's keys; P over the first 32 of them
+    // Weights of one half each, or (where the result has half's precision, which the values' rounding takes its share of) with what that leaves.
+    constexpr int PARTS = DT == MCSD_DTYPE_F16 ? 2 : 1;
     extern __shared__ unsigned char s_raw[];
     __shared__ __align__(8) unsigned long long s_bar[23];
     __shared__ uint32_t s_tmem;
@@ -306,8 +308,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                             wide_wait(b_p + 16 * x + 8 * h, n & 1, dead, P.wait_polls);
                             tc_after_sync();
 #pragma unroll
-                            for (int s = 0; s < 4; ++s)
-                                tc_mma(tmem + kO + D * x, tmem + kS + 128 * x + 64 * h + 8 * s, at + (4 * h + s) * (16 * 128 / 16), kOperandHigh, tc_shape(D, true),
+                            for (int s = 0; s < 4 * PARTS; ++s)
+                                tc_mma(tmem + kO + D * x, tmem + kS + 128 * x + 64 * h + 8 * s, at + (4 * h + s % 4) * (16 * 128 / 16), kOperandHigh, tc_shape(D, true),
                                        k > k0 || h > 0 || s > 0);
                             tc_commit(b_o + 16 * x + 8 * h);
                             if (h == 1) tc_commit(b_vempty + 8 * stage);
@@ -407,10 +409,14 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
             for (int k = k0; k < k1; ++k) {
                 if (k < units) {
                     const float4 *par = s_param + keep * (kAttUnit / 2);
+                    auto rest = [](float2 p, uint32_t w) MCSD_INLINE {     // of two weights beyond their halves
+                        const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+                        return half2_bits(p.x - h.x, p.y - h.y);
+                    };
                     // One half of the unit's keys, where every row of the tile sees them and nothing is odd about the values: the
                     // weights with the reference as it is; false (and nothing stored) should their sum be too large for half.
                     auto swift = [&](int h) MCSD_INLINE {
-                        uint32_t acc[64], w[32];
+                        uint32_t acc[64], w[32 * PARTS];
                         tmem_load64(t_s + 64 * h, acc);
                         float2 s2 = make_float2(0.f, 0.f);
                         const float rr = rho * ra;
@@ -423,11 +429,12 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                             const float2 p = make_float2(ex2f(e.x), ex2f(e.y));
                             s2 = add2(s2, p);
                             w[j] = half2_bits(p.x, p.y);
+                            if constexpr (PARTS == 2) w[32 + j] = rest(p, w[j]);
                         }
                         if (__any_sync(0xffffffffu, s2.x + s2.y > kChunkMost)) return false;
                         sum += s2.x + s2.y;
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) tmem_store16(t_s + 64 * h + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
+                        for (int c = 0; c < 2 * PARTS; ++c) tmem_store16(t_s + 64 * h + 16 * c, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * c));
                         return true;
                     };
                     // The same wherever the first does not do: the largest score, the reference moved where that leaves it by too much, then
@@ -474,30 +481,39 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                         }
                         const float rr = rho * ra;
                         float2 s2 = make_float2(0.f, 0.f);
+                        // (What is stored lies over scores that are read: of weights in two parts, over all of them.)
+                        constexpr int PER = PARTS == 2 ? 64 : 16;
 #pragma unroll 1
-                        for (int c = 0; c < 4; ++c) {           // (what is stored lies over scores that are read)
-                            const uint32_t see = (c < 2 ? see0 : see1) >> (16 * (c & 1));
-                            const uint32_t bad = see & s_bad[keep][2 * h + (c >> 1)] >> (16 * (c & 1)), far = s_far[keep][2 * h + (c >> 1)] >> (16 * (c & 1));
-                            uint32_t acc[16], w[8];
+                        for (int c = 0; c < 64 / PER; ++c) {
+                            const int first = PER * c, word = 2 * h + (first >> 5);
+                            uint32_t acc[PER], w[PER / 2 * PARTS];
                             __syncwarp();
-                            tmem_load16(t_s + 64 * h + 16 * c, acc);
+                            if constexpr (PARTS == 2) tmem_load64(t_s + 64 * h, acc);
+                            else tmem_load16(t_s + 64 * h + first, acc);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const float4 kp = at[8 * c + j];
+                            for (int j = 0; j < PER / 2; ++j) {
+                                const int shift = (first & 31) + 2 * j & 31, more = j >> 4;
+                                const uint32_t see = ((first >> 5) + more ? see1 : see0) >> shift;
+                                const uint32_t far = s_far[keep][word + more] >> shift, bad = see & s_bad[keep][word + more] >> shift;
+                                const float4 kp = at[first / 2 + j];
                                 const float2 a = __fmul2_rn(make_float2(kp.x, kp.y), make_float2(ra, ra));
                                 const float2 m = fma2(make_float2(kp.z, kp.w), make_float2(rr, rr), make_float2(-ref, -ref));
                                 const float2 e = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), a, m);
-                                float2 p = make_float2(ex2f(e.x), ex2f(e.y));
-                                if (!((see >> (2 * j)) & 1u)) p.x = 0.f;
-                                if (!((see >> (2 * j + 1)) & 1u)) p.y = 0.f;
+                                float2 p = make_float2(see & 1u ? ex2f(e.x) : 0.f, see & 2u ? ex2f(e.y) : 0.f);
                                 s2 = add2(s2, p);
-                                if ((far >> (2 * j)) & 1u) p.x *= 16.f;
-                                if ((far >> (2 * j + 1)) & 1u) p.y *= 16.f;
-                                if ((bad >> (2 * j)) & 1u) p.x = __int_as_float(0x7fffffff);
-                                if ((bad >> (2 * j + 1)) & 1u) p.y = __int_as_float(0x7fffffff);
+                                if (far & 1u) p.x *= 16.f;
+                                if (far & 2u) p.y *= 16.f;
+                                if (bad & 1u) p.x = __int_as_float(0x7fffffff);
+                                if (bad & 2u) p.y = __int_as_float(0x7fffffff);
                                 w[j] = half2_bits(p.x, p.y);
+                                if constexpr (PARTS == 2) w[PER / 2 + j] = rest(p, w[j]);
                             }
-                            tmem_store8(t_s + 64 * h + 8 * c, w);
+                            if constexpr (PARTS == 2) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) tmem_store16(t_s + 64 * h + 16 * i, *reinterpret_cast<const uint32_t(*)[16]>(w + 16 * i));
+                            } else {
+                                tmem_store8(t_s + 64 * h + first / 2, w);
+                            }
                         }
                         sum += s2.x + s2.y;
                     };
