@@ -52,11 +52,15 @@ void wait_limits(ChunkParams &p)
     p.test_extra = mcsd_get_option(MCSD_OPT_TEST_EXTRA_TX) > 0 ? 1u : 0u;
 }
 
-// Whether many sequences can have far fewer tokens than the longest chunk: those get the kernel for few rows beside the one for many. (Where
-// most have as many, the second launch would be for nothing, 2 to 3 us.)
+// Whether many sequences can have far fewer tokens than the longest chunk: those get the kernel for few rows beside the one for many. A
+// batch of 24 with three chunks of 253 tokens and 21 of one takes 95 us with both and 131 with the wide one alone. Where all have as many
+// tokens, the second launch is for nothing: 57 instead of 50 us (4 chunks of 16 tokens), 29 instead of 26 (weights, 8 windows of 32).
 bool mixed(const mcsd_chunk_desc *d) { return d->n_tokens < static_cast<int64_t>(d->batch) * d->max_new / 2; }
 
-// How a call is laid out; depends on the sizes only.
+// How a call is laid out; depends on the sizes only. Few rows go to the narrow kernel (blocks of up to 24, which decode the keys once for each
+// block), others to the wide one (blocks of 256, most of them empty then). 8 key heads of 128 numbers, 4000 keys, 64 sequences and 4, narrow
+// against wide in us: 32 rows 183 | 299 and 32 | 47, 64 rows 263 | 319 and 40 | 50, 96 rows 361 | 316 and 48 | 50. So up to three blocks of 24.
+constexpr int kChunkNarrowRows = 72;
 struct ChunkPlan {
     int narrow;     // rows of the narrow kernel's blocks, 0: it is not needed
     bool wide;
@@ -70,11 +74,11 @@ ChunkPlan chunk_plan(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache, bool 
     if (sms <= 0) sms = 148;
     const int group = d->n_heads / cache->n_heads;
     const long long rows = static_cast<long long>(d->max_new) * group;
-    // rows of a sequence that the narrow kernel is for: one token's, or what a block or two of 24 hold
+    // beside the wide kernel the narrow one has the sequences of one token
     const int narrow = group <= 8 ? 8 : group <= 16 ? 16 : group <= 24 ? 24 : 0;
-    if (rows <= 48 && narrow) {
+    if (rows <= kChunkNarrowRows && narrow) {
         plan.narrow = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 24 ? 24 : rows <= 32 && group <= 16 ? 16 : 24;
-        plan.most = 48;
+        plan.most = kChunkNarrowRows;
     } else {
         plan.wide = true;
         if (may_mix && narrow) {
@@ -111,6 +115,10 @@ int launch_with_join(int threads, int smem, const ChunkParams &p, cudaStream_t s
     return cudaLaunchKernelEx(&cfg, chunk_join_kernel<DT, D, ROWS>, p) == cudaSuccess ? MCSD_OK : MCSD_ERR_CUDA;
 }
 
+// Places of the cut that a block costs beside its keys: its queries, its results and the first unit's way through the kernel. Six prompts of 80 to
+// 2041 tokens 435 us at 256, 416 at 512, 431 at 1024; 64 sequences of 6 tokens (narrow kernel) 116, 111 and 116.
+constexpr int kChunkLead = 512;
+
 template <int DT, int D>
 int launch_chunk(ChunkParams p, const ChunkPlan &plan, cudaStream_t st)
 {
@@ -119,7 +127,7 @@ int launch_chunk(ChunkParams p, const ChunkPlan &plan, cudaStream_t st)
         p.tokens = kChunkRows / p.group;
         p.least = plan.narrow ? plan.most + 1 : 0;
         p.most = 0x7fffffff;
-        p.lead = 256;
+        p.lead = kChunkLead;
         p.n_ctas = plan.ctas[1];
         rc = launch_with_join<DT, D, kChunkRows, chunk_wide_kernel<DT, D>>(kChunkThreads, kChunkSmem<D>, p, st);
     }
@@ -127,7 +135,7 @@ int launch_chunk(ChunkParams p, const ChunkPlan &plan, cudaStream_t st)
         p.tokens = plan.narrow / p.group;
         p.least = 0;
         p.most = plan.wide ? plan.most : 0x7fffffff;
-        p.lead = plan.narrow == 8 ? 256 : 512;
+        p.lead = kChunkLead;
         p.n_ctas = plan.ctas[0];
         if (plan.narrow == 8) rc = launch_with_join<DT, D, 8, narrow_kernel<DT, D, 1, ChunkRows>>(kNarrowWarps * 32, kNarrowSmem<D, 1>, p, st);
         else if (plan.narrow == 16) rc = launch_with_join<DT, D, 16, narrow_kernel<DT, D, 2, ChunkRows>>(kNarrowWarps * 32, kNarrowSmem<D, 2>, p, st);
@@ -146,8 +154,9 @@ int launch_weigh_narrow(ChunkParams p, int sms, cudaStream_t st)
     return cudaGetLastError() == cudaSuccess ? MCSD_OK : MCSD_ERR_CUDA;
 }
 
-// Sequences of few rows (their tokens that count x query heads of a key head) go to the narrow kernel, others to the wide one; a call with rows for
-// the wide one launches both only where there can be many sequences of the other kind.
+// Sequences of few rows (their tokens that count x query heads of a key head: what one block of the narrow kernel holds) go to the narrow kernel,
+// others to the wide one; a call with rows for the wide one launches both only where there can be many sequences of the other kind. 32 sequences of
+// 4000 keys, 8 key heads, narrow against wide: 25 | 46 us with 4 rows, 28 | 48 with 16, 34 | 48 with 24.
 template <int DT, int D>
 int launch_weigh(ChunkParams p, bool may_mix, cudaStream_t st)
 {
@@ -175,13 +184,14 @@ int launch_weigh(ChunkParams p, bool may_mix, cudaStream_t st)
     return rc == MCSD_OK ? launched(n) : rc;
 }
 
-// Rows that leave multiprocessors idle get CTAs of 1024 threads (their latency counts), others 256, eight to a multiprocessor.
+// Rows that leave multiprocessors idle get CTAs of 1024 threads (their latency counts), others 256, eight to a multiprocessor: rows of 32000 bf16
+// logits and 20 tokens 13 | 17 us at 100 rows, 21 | 19 at 200, 67 | 31 at 1000.
 template <int DT>
 int launch_logprobs(const LogprobParams &p, bool vec, cudaStream_t st)
 {
     const long long sms = sm_count();
     if (sms <= 0) return MCSD_ERR_CUDA;
-    const bool few = p.n_out <= 2 * sms;
+    const bool few = p.n_out <= sms;
     const unsigned grid = static_cast<unsigned>(p.n_out);
     if (few) {
         if (vec) logprob_kernel<DT, 1024, true><<<grid, 1024, 0, st>>>(p);
