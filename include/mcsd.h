@@ -681,7 +681,11 @@ size_t mcsd_chunk_attention_workspace_bytes(const mcsd_chunk_desc *desc, const m
  * head h reads key/value head h / (n_heads / cache->n_heads), at most MCSD_MAX_GROUP to one.  A row that sees no
  * position is 0 with lse = -inf.  q, out device [n_tokens][n_heads][D] with the given strides (out may be q, with the same strides; they
  * must not overlap otherwise); lse device [n_tokens][n_heads] float32 or NULL; page_table [batch][ld_table], start
- * [batch], cu_tokens [batch + 1] device int32.  Calls that may overlap on the device need workspaces of their own. */
+ * [batch], cu_tokens [batch + 1] device int32.  Calls that may overlap on the device need workspaces of their own.
+ * Precision: scores and lse are those of float32; cached values and the weights that multiply them are rounded to half (2^-11
+ * of each; a weight below 2^-18 of the row's largest so far by 2^-29 of that one), sums are float32.  bf16 queries above 2^112 count as infinite (NaN).  A key or
+ * value that is NaN makes the rows NaN that see it.  Results depend on the sizes, the lengths and the GPU, not on timing.  A
+ * row whose kernel gave up a wait (see MCSD_OPT_WAIT_POLLS) is NaN. */
 int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
                          const int32_t *start, const int32_t *cu_tokens, const void *q, void *out, float *lse);
 
@@ -690,7 +694,8 @@ int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache
  * over the last `last_tokens` new tokens of the sequence (0: all of them) that see p and the query heads of the key head, with s as
  * above and lse as mcsd_chunk_attention gave it (rows with lse = -inf count nothing).  weights: device float32 [n_pages][cache->n_heads]
  * [page_size], a number for each row of the cache.  Rows of sequences without new tokens keep theirs.  Sums are float32 in a
- * fixed order.  Of the descriptor the strides of out and the workspace are not read. */
+ * fixed order.  No two sequences with new tokens may share a page.  Of the descriptor the strides of out and the workspace are not read; a wait given
+ * up makes weights NaN, as above. */
 int mcsd_accumulate_weights(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache, const int32_t *page_table,
                             const int32_t *start, const int32_t *cu_tokens, const void *q, const float *lse,
                             float *weights, float decay, int32_t last_tokens);

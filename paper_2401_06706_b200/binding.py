@@ -920,7 +920,7 @@ class ChunkAttention:
                                 last_tokens: int = 0) -> torch.Tensor:
         """Adds what the last last_tokens new tokens of every sequence (0: all) give to each cached row to weights
         [n_pages, heads, page_size] float32, in place (rows from before are multiplied by decay first); lse [tokens, n_heads] as
-        mcsd_chunk_attention returned it, the other arguments as there. Returns weights."""
+        mcsd_chunk_attention returned it, the other arguments as there. No two sequences with new tokens may share a page. Returns weights."""
         d = self._bind(q, cache, page_table, start, cu_tokens, scale)
         _device_tensor(lse, torch.float32, (q.shape[0], self.n_heads), self.device, "lse")
         _device_tensor(weights, torch.float32, (cache.n_pages, cache.n_heads, cache.page_size), self.device, "weights")

@@ -47,6 +47,28 @@ __device__ __forceinline__ __half2 value_pair(uint32_t w, __half2 scale, __half2
     return __hfma2(n, scale, mid);
 }
 
+// One CTA per SM. A block is up to 256 rows (tokens x query heads of one key head), 128 in each of the tiles A and B; a unit is 128 keys, in
+// two halves of 64. A unit is decoded once for both tiles. Roles:
+//   key warps (4)     codes come by cp.async AHEAD units before their use; one AND makes two of them subnormal halves (exact, c 2^-24), which
+//                     go to shared memory as an operand. A key's scale and mid go there as float32 and are kept for kChunkParams units;
+//   value warps (4)   scale (c - 8) + mid, rounded to half once: the product's other operand can have nothing left to apply;
+//   issuing warps (2) one per tile: S = Q K^T of each half of a unit into its own 64 columns of tensor memory, O += P V with P over S;
+//   softmax warps (8) one thread per row: s = ra (scale acc + (mid - 8 scale) rho), where rho is the row's sum of queries, so that K is exact
+//                     and the scores (and lse) have float32's precision; weights 2^(s - ref), their sum in float32, and P to tensor memory.
+// The maximum of a row is not formed for every unit. A row's reference is set in its first half unit (2^kChunkHead below its largest weight)
+// and holds until a half unit's sum passes kChunkMost; then the half is done again with a maximum (careful), O scaled by the factor
+// in tensor memory. Weights are rounded to half, relative to the largest one of the row so far: 2^-11 of each, or 2^-25 of 2^-kChunkHead where they are
+// subnormal. For fp16 results, which show that, P has two parts (PARTS), the second what the first leaves: with the values' rounding 1.4 times
+// the error of rounding the result, 1.55 without; bf16 results show neither. Values that half does not hold (beyond 65504, by scale and mid) are stored
+// as a sixteenth and their weights are sixteen times as large; rows that are NaN or infinite are zeros in the operand and make
+// the weights NaN where they are seen.
+// While weights of one half are formed, the scores of the other are computed: all scores of a unit at once, P over them, took 1.72 instead of 1.45 ms
+// (2048 tokens, 32 heads on 8 of 128 numbers, over 30011 rows), P apart from S with S given back early 1.48, parameters as pairs of halves 1.71.
+// Keeping parameters for four units, so that a decoded tile is free once its products are done, took it from 1.45 to 1.36 ms.
+// What bounds it: shared memory. A unit of 256 rows takes about 5800 cycles, of which its bandwidth has 2048 for broadcast loads of parameters by the softmax
+// warps, 2048 for the operands of the products (Q, K and V; P comes from tensor memory) and 512 for the decoded tiles; beside that the
+// chain softmax -> P V -> S of a half. With the parameters left out it would be 1.0 ms, without the exponentials or the decoding 1.19 each.
+// Measured: 1.36 to 1.40 ms there, 770 to 745 TFLOP/s, 0.49 to 0.48 of the library's rate for large bf16 products; 64 numbers a head in fp16 1.52 ms (342).
 template <int DT, int D>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 chunk_wide_kernel(const __grid_constant__ ChunkParams P)

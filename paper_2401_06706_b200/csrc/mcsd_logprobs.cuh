@@ -64,6 +64,9 @@ __device__ __forceinline__ LogprobSums join_sums(const LogprobSums &a, const Log
 // overflows (many equal logits) is searched n times instead.
 // Sums of a thread (V / THREADS terms) and their joining are float32: an error of 2^-22 of the result or so; a distance from the maximum
 // is formed before it is scaled, so that the lowest finite logits (a mask) do not overflow against one another.
+// Bound by the reading of the logits and by the tail of a row (joining, candidates), in which a CTA reads nothing; eight CTAs an SM overlap that: 1021 rows of
+// 50272 fp32 logits, 8 tokens: 54 us where a part comes from L2, 77 from HBM (2.7 of 6.55 TB/s); 2047 rows of 32000 bf16, 20 tokens: 53 and 68. A CTA per row instead
+// of a loop over rows 75 -> 54; a maximum and the candidates in a pass of their own 97 (fp32).
 template <int DT, int THREADS, bool VEC>
 __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : 8)
 logprob_kernel(const __grid_constant__ LogprobParams P)

@@ -144,11 +144,15 @@ int launch_chunk(ChunkParams p, const ChunkPlan &plan, cudaStream_t st)
     return rc == MCSD_OK ? launched(plan.wide && plan.narrow ? 4 : 2) : rc;
 }
 
+// Places that a (sequence, key head) costs beside its units. Hardly felt: decoding batch 25.4, 25.2 and 27.3 us at 32, 128 and 384, windows of 32 tokens
+// (wide kernel) 27.1, 25.7 and 25.3 at 64, 256 and 1024.
+constexpr int kWeighLeadNarrow = 128, kWeighLeadWide = 256;
+
 template <int DT, int D, int NB>
 int launch_weigh_narrow(ChunkParams p, int sms, cudaStream_t st)
 {
     if (!allow_smem<weigh_narrow_kernel<DT, D, NB>>(kWeighSmem<D>)) return MCSD_ERR_CUDA;
-    p.lead = 128;
+    p.lead = kWeighLeadNarrow;
     p.n_ctas = sms * kWeighCtas<NB>;
     weigh_narrow_kernel<DT, D, NB><<<p.n_ctas, kNarrowWarps * 32, kWeighSmem<D>, st>>>(p);
     return cudaGetLastError() == cudaSuccess ? MCSD_OK : MCSD_ERR_CUDA;
@@ -169,7 +173,7 @@ int launch_weigh(ChunkParams p, bool may_mix, cudaStream_t st)
         if (!allow_smem<weigh_wide_kernel<DT, D>>(kWeighWideSmem<D>)) return MCSD_ERR_CUDA;
         p.least = narrow ? narrow + 1 : 0;
         p.most = 0x7fffffff;
-        p.lead = 256;
+        p.lead = kWeighLeadWide;
         p.n_ctas = sms;
         weigh_wide_kernel<DT, D><<<p.n_ctas, kWeighThreads, kWeighWideSmem<D>, st>>>(p);
         if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;

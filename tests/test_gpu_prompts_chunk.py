@@ -32,6 +32,13 @@ def test_lengths_around_every_border(D, heads):
     check_attention(p, attend(p))
 
 
+@pytest.mark.parametrize("heads,count", [(1, 24), (1, 25), (1, 48), (1, 49), (1, 72), (1, 73), (4, 6), (4, 12), (4, 18), (4, 19), (7, 10), (7, 11), (13, 5), (24, 3), (25, 2)])
+def test_rows_around_the_blocks_borders(heads, count):
+    """One block of few rows, two and three, and the first chunk that is too long for them; queries of one key head."""
+    p = problem(5, [700, 0, 1300], [count, count, 1], heads, 1, 128, 16, torch.bfloat16)
+    check_attention(p, attend(p, max_new=count))
+
+
 @pytest.mark.parametrize("heads", [4, 32])
 def test_one_long_sequence(heads):
     """Few rows over a long prefix: the work of a block is divided and joined."""
