@@ -107,6 +107,21 @@ struct WeighWalk {
     }
 };
 
+// Key codes as halves, the eight of a word. One AND makes two of them subnormal numbers, c 2^-24 or 16 c 2^-24 (the queries of these are a sixteenth); but
+// the matrix instructions align products by the operands' exponents, and a subnormal number has that of 2^-14: of queries with eleven
+// bits (fp16) that loses some, an error of 4.5e-6 instead of 1e-6 of the weights. Those get codes at the top of the mantissa, c 2^-18, at a shift more each.
+template <int DT> constexpr bool kWeighHigh = DT == MCSD_DTYPE_F16;
+template <int DT> constexpr int kWeighExp = kWeighHigh<DT> ? 18 : 24;
+template <int DT> constexpr float kWeighUnit = kWeighHigh<DT> ? 3.814697265625e-6f : 5.9604644775390625e-8f;       // 2^-18, 2^-24
+template <int DT> constexpr float kWeighOdd = kWeighHigh<DT> ? 1.f : 0.0625f;          // what the queries of the odd codes are multiplied by
+template <int DT>
+__device__ __forceinline__ uint4 weigh_codes(uint32_t w)
+{
+    if constexpr (kWeighHigh<DT>) return make_uint4(w << 6 & 0x03c003c0u, w << 2 & 0x03c003c0u, w >> 2 & 0x03c003c0u, w >> 6 & 0x03c003c0u);
+    const uint32_t y = w >> 8;
+    return make_uint4(w & 0x000f000fu, w & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
+}
+
 // ---- few rows: warp-level matrix instructions, as in the narrow attention kernel
 template <int D> constexpr int kWeighStage = kNarrowKeys * (D / 2 + 4);
 constexpr int kWeighStages = 4;
@@ -240,7 +255,7 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
             e = max(min(e, 112), -110);
             const float up = __int_as_float((127 + 15 - e) << 23);
             const float log2e = P.scale * 1.4426950408889634f;
-            const float per_acc = ldexpf(log2e, e - 15 + 24), per_mid = log2e * sum;
+            const float per_acc = ldexpf(log2e, e - 15 + kWeighExp<DT>), per_mid = log2e * sum;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 ra[nb][c] = __shfl_sync(0xffffffffu, per_acc, (2 * t + c) * 4);
@@ -251,7 +266,7 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     qb[nb][2 * j + s][0] = half2_bits(x[8 * j + 2 * s] * up, x[8 * j + 2 * s + 4] * up);
-                    qb[nb][2 * j + s][1] = half2_bits(x[8 * j + 2 * s + 1] * up * 0.0625f, x[8 * j + 2 * s + 5] * up * 0.0625f);
+                    qb[nb][2 * j + s][1] = half2_bits(x[8 * j + 2 * s + 1] * up * kWeighOdd<DT>, x[8 * j + 2 * s + 5] * up * kWeighOdd<DT>);
                 }
         }
 
@@ -301,13 +316,11 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
                 }
 #pragma unroll
                 for (int n = 0; n < JW; ++n) {
-                    const uint32_t y0 = v[0][n] >> 8, y1 = v[1][n] >> 8;
-                    const uint32_t a[4] = {v[0][n] & 0x000f000fu, v[1][n] & 0x000f000fu, v[0][n] & 0x00f000f0u, v[1][n] & 0x00f000f0u};
-                    const uint32_t c[4] = {y0 & 0x000f000fu, y1 & 0x000f000fu, y0 & 0x00f000f0u, y1 & 0x00f000f0u};
+                    const uint4 a = weigh_codes<DT>(v[0][n]), c = weigh_codes<DT>(v[1][n]);        // of key kg and of the one eight on
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
-                        mma_f16(s[nb], a[0], a[1], a[2], a[3], qb[nb][2 * n][0], qb[nb][2 * n][1]);
-                        mma_f16(s[nb], c[0], c[1], c[2], c[3], qb[nb][2 * n + 1][0], qb[nb][2 * n + 1][1]);
+                        mma_f16(s[nb], a.x, c.x, a.y, c.y, qb[nb][2 * n][0], qb[nb][2 * n][1]);
+                        mma_f16(s[nb], a.z, c.z, a.w, c.w, qb[nb][2 * n + 1][0], qb[nb][2 * n + 1][1]);
                     }
                 }
 #pragma unroll
@@ -491,10 +504,9 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                     const uint32_t w[4] = {turn ? v.z : v.x, turn ? v.w : v.y, turn ? v.x : v.z, turn ? v.y : v.w};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const uint32_t y = w[j] >> 8;
                         const int chunk = 4 * c + (turn ? j ^ 2 : j);
                         *reinterpret_cast<uint4 *>(tile + (chunk >> 3) * (kAttUnit * 128) + (((chunk & 7) ^ (key & 7)) << 4)) =
-                            make_uint4(w[j] & 0x000f000fu, w[j] & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
+                            weigh_codes<DT>(w[j]);
                     }
                 }
                 if (lane < 16) {
@@ -590,8 +602,8 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                 int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 126 : 0;
                 e = max(min(e, 112), -110);
                 const float up = __int_as_float((127 + 15 - e) << 23);
-                factor = ldexpf(P.scale * 1.4426950408889634f, e - 15 + 24);
-                s_col[(tid >> 1) * 4 + (tid & 1)] = sum * up * 5.9604644775390625e-8f;      // 2^-24
+                factor = ldexpf(P.scale * 1.4426950408889634f, e - 15 + kWeighExp<DT>);
+                s_col[(tid >> 1) * 4 + (tid & 1)] = sum * up * kWeighUnit<DT>;
                 s_col[(tid >> 1) * 4 + 2 + (tid & 1)] = lse;
                 unsigned char *to = s_q + tid * 128;
 #pragma unroll
@@ -601,7 +613,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                     uint32_t out[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const float f = i & 1 ? up * 0.0625f : up;
+                        const float f = i & 1 ? up * kWeighOdd<DT> : up;
                         out[i] = half2_bits(v[i] * f, v[i + 4] * f);
                     }
                     *reinterpret_cast<uint4 *>(to + (c >> 3) * (kWeighRows * 128) + (((c & 7) ^ (tid & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
