@@ -148,6 +148,18 @@ __device__ __forceinline__ int chunk_units_below(const ChunkParams &P, ChunkPlac
     return k < static_cast<ChunkPlace>(units) ? static_cast<int>(k) : units;
 }
 
+// Key codes as halves, the eight of a word. Bits of a code in the mantissa of a subnormal number are a number without further ado; which bits
+// matters: the matrix instructions align products, it seems, by the operands' exponents, and a subnormal number has that of 2^-14. One AND for
+// two codes gives c 2^-24 and 16 c 2^-24, and an error of 4.5e-6 of gathered weights with fp16 queries (eleven bits each, windows of 32 tokens). At
+// the top of the mantissa, c 2^-18, it is 3.6e-7, half as large as before with bf16 ones, and the shifts cost nothing that shows (weights of 32
+// sequences of one token 25 us either way).
+constexpr int kKeyExp = 18;
+constexpr float kKeyUnit = 3.814697265625e-6f;      // 2^-18
+__device__ __forceinline__ uint4 key_codes(uint32_t w)
+{
+    return make_uint4(w << 6 & 0x03c003c0u, w << 2 & 0x03c003c0u, w >> 2 & 0x03c003c0u, w >> 6 & 0x03c003c0u);
+}
+
 // Left by one thread of a CTA when it begins (nothing to join), and when it has begun a block that others end.
 __device__ __forceinline__ void chunk_join_none(const ChunkParams &P) { P.joins[blockIdx.x].last = -1; }
 __device__ __forceinline__ void chunk_join_note(const ChunkParams &P, const AttItem &it)

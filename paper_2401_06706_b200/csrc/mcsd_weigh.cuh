@@ -107,21 +107,6 @@ struct WeighWalk {
     }
 };
 
-// Key codes as halves, the eight of a word. One AND makes two of them subnormal numbers, c 2^-24 or 16 c 2^-24 (the queries of these are a sixteenth); but
-// the matrix instructions align products by the operands' exponents, and a subnormal number has that of 2^-14: of queries with eleven
-// bits (fp16) that loses some, an error of 4.5e-6 instead of 1e-6 of the weights. Those get codes at the top of the mantissa, c 2^-18, at a shift more each.
-template <int DT> constexpr bool kWeighHigh = DT == MCSD_DTYPE_F16;
-template <int DT> constexpr int kWeighExp = kWeighHigh<DT> ? 18 : 24;
-template <int DT> constexpr float kWeighUnit = kWeighHigh<DT> ? 3.814697265625e-6f : 5.9604644775390625e-8f;       // 2^-18, 2^-24
-template <int DT> constexpr float kWeighOdd = kWeighHigh<DT> ? 1.f : 0.0625f;          // what the queries of the odd codes are multiplied by
-template <int DT>
-__device__ __forceinline__ uint4 weigh_codes(uint32_t w)
-{
-    if constexpr (kWeighHigh<DT>) return make_uint4(w << 6 & 0x03c003c0u, w << 2 & 0x03c003c0u, w >> 2 & 0x03c003c0u, w >> 6 & 0x03c003c0u);
-    const uint32_t y = w >> 8;
-    return make_uint4(w & 0x000f000fu, w & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
-}
-
 // ---- few rows: warp-level matrix instructions, as in the narrow attention kernel
 template <int D> constexpr int kWeighStage = kNarrowKeys * (D / 2 + 4);
 constexpr int kWeighStages = 4;
@@ -129,7 +114,7 @@ template <int D> constexpr int kWeighSmem = kNarrowWarps * kWeighStages * kWeigh
 template <int NB> constexpr int kWeighCtas = NB == 1 ? 6 : NB == 2 ? 4 : 3;         // per SM
 
 // The first half of the narrow attention kernel (see there): a warp takes every fourth chunk of 32 keys, codes become operands by
-// one AND, S^T = K Q^T. A lane then has the scores of four keys with its rows: their weights 2^(s - lse) are added up over its rows
+// a shift and an AND for two, S^T = K Q^T. A lane then has the scores of four keys with its rows: their weights 2^(s - lse) are added up over its rows
 // and, by two shuffles, over the four lanes that share the keys; a key's old weight is on its way meanwhile. No row has a maximum or a sum of its
 // own here, so nothing is joined.
 // Bytes that must move: key codes, scale and mid, weights read and written. 32 sequences of one token over 4001 rows at most, 8 key heads of 128, 4 query heads each: 25 us
@@ -255,7 +240,7 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
             e = max(min(e, 112), -110);
             const float up = __int_as_float((127 + 15 - e) << 23);
             const float log2e = P.scale * 1.4426950408889634f;
-            const float per_acc = ldexpf(log2e, e - 15 + kWeighExp<DT>), per_mid = log2e * sum;
+            const float per_acc = ldexpf(log2e, e - 15 + kKeyExp), per_mid = log2e * sum;
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 ra[nb][c] = __shfl_sync(0xffffffffu, per_acc, (2 * t + c) * 4);
@@ -266,7 +251,7 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     qb[nb][2 * j + s][0] = half2_bits(x[8 * j + 2 * s] * up, x[8 * j + 2 * s + 4] * up);
-                    qb[nb][2 * j + s][1] = half2_bits(x[8 * j + 2 * s + 1] * up * kWeighOdd<DT>, x[8 * j + 2 * s + 5] * up * kWeighOdd<DT>);
+                    qb[nb][2 * j + s][1] = half2_bits(x[8 * j + 2 * s + 1] * up, x[8 * j + 2 * s + 5] * up);
                 }
         }
 
@@ -316,7 +301,7 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
                 }
 #pragma unroll
                 for (int n = 0; n < JW; ++n) {
-                    const uint4 a = weigh_codes<DT>(v[0][n]), c = weigh_codes<DT>(v[1][n]);        // of key kg and of the one eight on
+                    const uint4 a = key_codes(v[0][n]), c = key_codes(v[1][n]);        // of key kg and of the one eight on
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb) {
                         mma_f16(s[nb], a.x, c.x, a.y, c.y, qb[nb][2 * n][0], qb[nb][2 * n][1]);
@@ -367,7 +352,7 @@ template <int D> constexpr int kWeighWideSmem = 1024 + (2 + kWeighKeys) * kWideT
 // One CTA per SM. A product has 128 keys as its rows (lanes of tensor memory) and a block of up to 256 rows of queries as its columns, so that a
 // thread that adds up has one key: its scale and mid are two registers, its weights are added up without another thread, and what
 // differs by column (the sum of a query, its lse) is one broadcast load for two columns. Roles:
-//   decoding warps  copy codes two units ahead and turn them into subnormal halves by one AND, sixteen keys of each unit a warp;
+//   decoding warps  copy codes two units ahead and turn them into subnormal halves (key_codes), sixteen keys of each unit a warp;
 //   issuing warp    S^T = K Q^T into one of two halves of tensor memory, even and odd units in turn;
 //   adding groups   even and odd units: 2^(scale_j acc + mid_j rho_n - lse_n), added up over n. Together they bring a block of queries to shared
 //                   memory, scaled by one power of two, so that a factor is the same for all columns.
@@ -506,7 +491,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                     for (int j = 0; j < 4; ++j) {
                         const int chunk = 4 * c + (turn ? j ^ 2 : j);
                         *reinterpret_cast<uint4 *>(tile + (chunk >> 3) * (kAttUnit * 128) + (((chunk & 7) ^ (key & 7)) << 4)) =
-                            weigh_codes<DT>(w[j]);
+                            key_codes(w[j]);
                     }
                 }
                 if (lane < 16) {
@@ -602,8 +587,8 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                 int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 126 : 0;
                 e = max(min(e, 112), -110);
                 const float up = __int_as_float((127 + 15 - e) << 23);
-                factor = ldexpf(P.scale * 1.4426950408889634f, e - 15 + kWeighExp<DT>);
-                s_col[(tid >> 1) * 4 + (tid & 1)] = sum * up * kWeighUnit<DT>;
+                factor = ldexpf(P.scale * 1.4426950408889634f, e - 15 + kKeyExp);
+                s_col[(tid >> 1) * 4 + (tid & 1)] = sum * up * kKeyUnit;
                 s_col[(tid >> 1) * 4 + 2 + (tid & 1)] = lse;
                 unsigned char *to = s_q + tid * 128;
 #pragma unroll
@@ -612,10 +597,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                     Elem<DT>::unpack(raw[c], v);
                     uint32_t out[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float f = i & 1 ? up * kWeighOdd<DT> : up;
-                        out[i] = half2_bits(v[i] * f, v[i + 4] * f);
-                    }
+                    for (int i = 0; i < 4; ++i) out[i] = half2_bits(v[i] * up, v[i + 4] * up);
                     *reinterpret_cast<uint4 *>(to + (c >> 3) * (kWeighRows * 128) + (((c & 7) ^ (tid & 7)) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
                 }
                 fence_proxy_async();
