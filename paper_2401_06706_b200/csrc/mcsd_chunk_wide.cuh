@@ -54,7 +54,8 @@ __device__ __forceinline__ __half2 value_pair(uint32_t w, __half2 scale, __half2
 //   value warps (4)   scale (c - 8) + mid, rounded to half once: the product's other operand can have nothing left to apply;
 //   issuing warps (2) one per tile: S = Q K^T of each half of a unit into its own 64 columns of tensor memory, O += P V with P over S;
 //   softmax warps (8) one thread per row: s = ra (scale acc + (mid - 8 scale) rho), where rho is the row's sum of queries, so that K is exact
-//                     (lse off by 9e-6 at most with fp16 queries, 7e-6 with bf16 ones; key_codes make it 3e-6 and 2e-6, and a call 3.5 % longer); weights 2^(s - ref), their sum in float32, and P to tensor memory.
+//                     (lse off by 9e-6 at most with fp16 queries, 7e-6 with bf16 ones; key_codes make it 3e-6 and 2e-6, and a call 3.5 % longer);
+//                     weights 2^(s - ref), their sum in float32, and P to tensor memory.
 // The maximum of a row is not formed for every unit. A row's reference is set in its first half unit (2^kChunkHead below its largest weight)
 // and holds until a half unit's sum passes kChunkMost; then the half is done again with a maximum (careful), O scaled by the factor
 // in tensor memory. Weights are rounded to half, relative to the largest one of the row so far: 2^-11 of each, or 2^-25 of 2^-kChunkHead where they are
