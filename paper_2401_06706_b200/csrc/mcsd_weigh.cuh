@@ -346,8 +346,9 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
 constexpr int kWeighRows = 256;                     // rows of queries (columns of a product) in a block
 constexpr int kWeighKeys = 3;                       // decoded units
 constexpr int kWeighAhead = 2;                      // units whose codes are on their way to shared memory
+constexpr int kWeighSpread = 12;                    // log2 of what the rows of a block with one scale may lie apart
 constexpr int kWeighThreads = 640;                  // 8 warps that add up, 8 that decode, one that issues (and 3 beside it)
-template <int D> constexpr int kWeighWideSmem = 1024 + (2 + kWeighKeys) * kWideTile<D> + kWeighKeys * kAttUnit * 8 + kWeighRows * 8 + kWeighAhead * kAttUnit * (D / 2 + 4);
+template <int D> constexpr int kWeighWideSmem = 1024 + (2 + kWeighKeys) * kWideTile<D> + kWeighKeys * kAttUnit * 8 + kWeighRows * 12 + kWeighAhead * kAttUnit * (D / 2 + 4);
 
 // One CTA per SM. A product has 128 keys as its rows (lanes of tensor memory) and a block of up to 256 rows of queries as its columns, so that a
 // thread that adds up has one key: its scale and mid are two registers, its weights are added up without another thread, and what
@@ -355,11 +356,14 @@ template <int D> constexpr int kWeighWideSmem = 1024 + (2 + kWeighKeys) * kWideT
 //   decoding warps  copy codes two units ahead and turn them into subnormal halves (key_codes), sixteen keys of each unit a warp;
 //   issuing warp    S^T = K Q^T into one of two halves of tensor memory, even and odd units in turn;
 //   adding groups   even and odd units: 2^(scale_j acc + mid_j rho_n - lse_n), added up over n. Together they bring a block of queries to shared
-//                   memory, scaled by one power of two, so that a factor is the same for all columns.
+//                   memory. Where the largest numbers of its rows lie within 2^kWeighSpread of each other, they are scaled by one power of two, and
+//                   a factor is the same for all columns: a row that is 2^12 below the loudest has its largest number at 2^3, half's steps are 2^-24, so that it is
+//                   off by 2^-28 of itself. Otherwise (a loud row, one that is infinite) each row has its own, and a column a factor of its own: one more
+//                   multiplication a score, so that no row takes bits from its neighbours.
 // Sequences with more rows than a block take the units once for every block; a key's sum then goes on from what its thread wrote before.
 // Of the products only half a softmax is left: one multiply-add, one exponential and one addition per score, in pairs where there is such an instruction.
-// 2 x 1500 tokens over 2500 rows, 16 heads of 64: 86 us (floor 11 by the products); 8 windows of 32 tokens over 3500 rows, 4 heads to a key head: 26 (3.7 by the
-// bytes); 2048 tokens over 8000, 32 heads on 8 of 128: 432. Bound by a group's way through a unit (read the scores, weights, wait: 6300 cycles per 128 x 256), the
+// 2 x 1500 tokens over 2500 rows, 16 heads of 64: 87 us (floor 11 by the products), 109 with rows far apart in every block; 8 windows of 32 tokens over 3500
+// rows, 4 heads to a key head: 27 and 30 (3.7 by the bytes); 2048 tokens over 8000, 32 heads on 8 of 128: 432. Bound by a group's way through a unit (read the scores, weights, wait: 6300 cycles per 128 x 256), the
 // products are done in a third of it.
 template <int DT, int D>
 __global__ void __launch_bounds__(kWeighThreads, 1)
@@ -371,7 +375,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
     __shared__ __align__(8) unsigned long long s_bar[2 * kWeighKeys + 6];
     __shared__ uint32_t s_tmem;
     __shared__ int s_dead, s_any;
-    __shared__ float s_most[8];
+    __shared__ int s_high[8], s_low[8];             // of a warp's rows: exponents of the largest number of the loudest row, and of the softest
     __shared__ WeighWalk s_walk[kWeighThreads / 32];
     __shared__ WeighItem s_item[kWeighThreads / 32];
 
@@ -379,7 +383,8 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
     unsigned char *s_q = base, *s_k = base + 2 * TILE;                          // [2 x 128 rows], [stages][128 keys]
     float2 *s_param = reinterpret_cast<float2 *>(base + (2 + kWeighKeys) * TILE);       // [stages][keys]{scale, mid - 8 scale}
     float *s_col = reinterpret_cast<float *>(s_param + kWeighKeys * kAttUnit);          // [128 pairs of columns]{rho, rho, lse, lse}
-    unsigned char *s_codes = reinterpret_cast<unsigned char *>(s_col + 2 * kWeighRows); // [decoding warps][kWeighAhead]{codes, parameters}
+    float *s_factor = s_col + 2 * kWeighRows;                                   // [columns] of a block whose rows lie far apart
+    unsigned char *s_codes = reinterpret_cast<unsigned char *>(s_factor + kWeighRows);  // [decoding warps][kWeighAhead]{codes, parameters}
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bars = smem_u32(s_bar);
@@ -548,7 +553,8 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
         auto both = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
         for_blocks([&](const WeighItem &it, int i0, int n_tokens, int k0, int k1) MCSD_INLINE {
             const int n_rows = n_tokens * P.group, columns = (n_rows + 63) & ~63;
-            float factor;                           // log2 units per unit of scale acc + (mid - 8 scale) rho
+            float factor;                           // log2 units per unit of scale acc + (mid - 8 scale) rho: of all columns, or of this thread's
+            bool apart;                             // whether each column has its own
             {
                 // queries of the block: row `tid`, in the order that the ANDs of the keys give
                 uint4 raw[D / 8];
@@ -579,15 +585,17 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) { most = fmaxf(most, fabsf(v[i])); sum += v[i]; }
                 }
-                most = warp_max(most);
-                if (lane == 0) s_most[warp] = most;
+                int e = most > 0.f ? max(min(static_cast<int>(__float_as_uint(most) >> 23) - 126, 112), -110) : 0;
+                int high = __reduce_max_sync(0xffffffffu, most > 0.f ? e : -110), low = __reduce_min_sync(0xffffffffu, most > 0.f ? e : 112);
+                if (lane == 0) { s_high[warp] = high; s_low[warp] = low; }
                 both();                             // (and all scores of the block before are there: its queries are done with)
 #pragma unroll
-                for (int w = 0; w < 8; ++w) most = fmaxf(most, s_most[w]);
-                int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 126 : 0;
-                e = max(min(e, 112), -110);
+                for (int w = 0; w < 8; ++w) { high = max(high, s_high[w]); low = min(low, s_low[w]); }
+                apart = high - low > kWeighSpread;
+                if (!apart) e = high;               // (a block of zeros: any)
                 const float up = __int_as_float((127 + 15 - e) << 23);
                 factor = ldexpf(P.scale * 1.4426950408889634f, e - 15 + kKeyExp);
+                s_factor[tid] = factor;
                 s_col[(tid >> 1) * 4 + (tid & 1)] = sum * up * kKeyUnit;
                 s_col[(tid >> 1) * 4 + 2 + (tid & 1)] = lse;
                 unsigned char *to = s_q + tid * 128;
@@ -628,8 +636,9 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                     ++n;
                     tc_after_sync();
                     float2 s0 = make_float2(0.f, 0.f), s1 = make_float2(0.f, 0.f);
-                    auto add = [&](auto plain_tag, int from) MCSD_INLINE {              // from: first column that sees the key
-                        constexpr bool plain = decltype(plain_tag)::value;
+                    // plain: all columns see the key; even: they have one factor; from: first column that sees the key
+                    auto add = [&](auto plain_tag, auto even_tag, int from) MCSD_INLINE {
+                        constexpr bool plain = decltype(plain_tag)::value, even = decltype(even_tag)::value;
 #pragma unroll 1
                         for (int c = 0; c < columns; c += 64) {
                             uint32_t acc[64];
@@ -638,8 +647,15 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
 #pragma unroll
                             for (int j = 0; j < 32; ++j) {
                                 const float4 v = col[j];
-                                const float2 t = fma2(m, make_float2(v.x, v.y), make_float2(-v.z, -v.w));
-                                const float2 e = fma2(a, make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), t);
+                                const float2 got = make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), rho = make_float2(v.x, v.y),
+                                             less = make_float2(-v.z, -v.w);
+                                float2 e;
+                                if constexpr (even) {
+                                    e = fma2(a, got, fma2(m, rho, less));
+                                } else {
+                                    const float2 f = *reinterpret_cast<const float2 *>(s_factor + c + 2 * j);
+                                    e = fma2(fma2(make_float2(par.x, par.x), got, __fmul2_rn(make_float2(par.y, par.y), rho)), f, less);
+                                }
                                 float2 p = make_float2(ex2f(e.x), ex2f(e.y));
                                 if (!plain) {
                                     if (c + 2 * j < from || c + 2 * j >= n_rows) p.x = 0.f;
@@ -649,11 +665,13 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                             }
                         }
                     };
-                    if ((k + 1) * static_cast<long long>(kAttUnit) - 1 <= first) {
-                        add(std::true_type(), 0);
+                    if (!apart && (k + 1) * static_cast<long long>(kAttUnit) - 1 <= first) {
+                        add(std::true_type(), std::true_type(), 0);
                     } else {
                         const long long token = pos - first;
-                        add(std::false_type(), token <= 0 ? 0 : static_cast<int>(min(token * P.group, 1ll << 20)));
+                        const int from = token <= 0 ? 0 : static_cast<int>(min(token * P.group, 1ll << 20));
+                        if (apart) add(std::false_type(), std::false_type(), from);
+                        else add(std::false_type(), std::true_type(), from);
                     }
                     tc_before_sync();
                     warp_arrive(b_read + 8 * x, lane);
