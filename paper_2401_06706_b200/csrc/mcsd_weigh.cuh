@@ -201,13 +201,12 @@ weigh_narrow_kernel(const __grid_constant__ ChunkParams P)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int row = nb * 8 + 2 * t + c;
-                float l = INFINITY;                 // (of no row, or one that saw nothing: no weight)
+                float l = INFINITY;
                 token[nb][c] = -1;
                 if (row < n_rows) {
                     const int i = row / P.group, h = it.head * P.group + (row - i * P.group);
                     l = __ldg(P.lse + (static_cast<long long>(it.s.row) + i) * P.n_heads + h) * 1.4426950408889634f;
-                    if (l == -INFINITY) l = INFINITY;
-                    token[nb][c] = pos_first + i;
+                    if (l != -INFINITY) token[nb][c] = pos_first + i;       // (else it counts nothing, whatever its scores are)
                 }
                 lse[nb][c] = l;
             }
@@ -357,13 +356,13 @@ template <int D> constexpr int kWeighWideSmem = 1024 + (2 + kWeighKeys) * kWideT
 //   issuing warp    S^T = K Q^T into one of two halves of tensor memory, even and odd units in turn;
 //   adding groups   even and odd units: 2^(scale_j acc + mid_j rho_n - lse_n), added up over n. Together they bring a block of queries to shared
 //                   memory. Where the largest numbers of its rows lie within 2^kWeighSpread of each other, they are scaled by one power of two, and
-//                   a factor is the same for all columns: a row that is 2^12 below the loudest has its largest number at 2^3, half's steps are 2^-24, so that it is
-//                   off by 2^-28 of itself. Otherwise (a loud row, one that is infinite) each row has its own, and a column a factor of its own: one more
-//                   multiplication a score, so that no row takes bits from its neighbours.
+//                   a factor is the same for all columns: the largest number of a row that is 2^12 below the loudest is at 2^2 at least, and what half's
+//                   range takes of its numbers is 2^-25 at most, 2^-27 of that one. Otherwise (a loud row, one that is infinite, one without an lse)
+//                   each row has its own, and a column a factor of its own: one more multiplication a score, so that no row takes bits from its neighbours.
 // Sequences with more rows than a block take the units once for every block; a key's sum then goes on from what its thread wrote before.
 // Of the products only half a softmax is left: one multiply-add, one exponential and one addition per score, in pairs where there is such an instruction.
-// 2 x 1500 tokens over 2500 rows, 16 heads of 64: 87 us (floor 11 by the products), 109 with rows far apart in every block; 8 windows of 32 tokens over 3500
-// rows, 4 heads to a key head: 27 and 30 (3.7 by the bytes); 2048 tokens over 8000, 32 heads on 8 of 128: 432. Bound by a group's way through a unit (read the scores, weights, wait: 6300 cycles per 128 x 256), the
+// 2 x 1500 tokens over 2500 rows, 16 heads of 64: 88 us (floor 11 by the products), 124 with rows far apart in every block; 8 windows of 32 tokens over 3500
+// rows, 4 heads to a key head: 27 and 32 (3.7 by the bytes); 2048 tokens over 8000, 32 heads on 8 of 128: 432. Bound by a group's way through a unit (read the scores, weights, wait: 6300 cycles per 128 x 256), the
 // products are done in a third of it.
 template <int DT, int D>
 __global__ void __launch_bounds__(kWeighThreads, 1)
@@ -560,13 +559,15 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                 uint4 raw[D / 8];
 #pragma unroll
                 for (int c = 0; c < D / 8; ++c) raw[c] = make_uint4(0u, 0u, 0u, 0u);
-                float lse = INFINITY;               // (of no row, or one that saw nothing: no weight)
+                float lse = INFINITY;               // (of no row: no weight)
+                bool none = false;                  // a row without an lse: it counts nothing, whatever its queries and the keys are
                 if (tid < n_rows) {
                     const int i = tid / P.group, h = it.head * P.group + (tid - i * P.group);
                     const long long token = static_cast<long long>(it.s.row) + i0 + i, at = token * P.q_token + h * P.q_head;
                     lse = __ldg(P.lse + token * P.n_heads + h) * 1.4426950408889634f;
-                    if (lse == -INFINITY) lse = INFINITY;
-                    if (P.q_vec) {
+                    none = lse == -INFINITY;
+                    if (none) {                     // (its queries stay zeros)
+                    } else if (P.q_vec) {
 #pragma unroll
                         for (int c = 0; c < D / 8; ++c) raw[c] = __ldg(reinterpret_cast<const uint4 *>(static_cast<const char *>(P.q) + 2 * at) + c);
                     } else {
@@ -586,7 +587,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                     for (int i = 0; i < 8; ++i) { most = fmaxf(most, fabsf(v[i])); sum += v[i]; }
                 }
                 int e = most > 0.f ? max(min(static_cast<int>(__float_as_uint(most) >> 23) - 126, 112), -110) : 0;
-                int high = __reduce_max_sync(0xffffffffu, most > 0.f ? e : -110), low = __reduce_min_sync(0xffffffffu, most > 0.f ? e : 112);
+                int high = __reduce_max_sync(0xffffffffu, most > 0.f ? e : -110), low = __reduce_min_sync(0xffffffffu, none ? -1000 : most > 0.f ? e : 112);
                 if (lane == 0) { s_high[warp] = high; s_low[warp] = low; }
                 both();                             // (and all scores of the block before are there: its queries are done with)
 #pragma unroll
@@ -595,7 +596,7 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                 if (!apart) e = high;               // (a block of zeros: any)
                 const float up = __int_as_float((127 + 15 - e) << 23);
                 factor = ldexpf(P.scale * 1.4426950408889634f, e - 15 + kKeyExp);
-                s_factor[tid] = factor;
+                s_factor[tid] = none ? __int_as_float(0x7fffffff) : factor;      // (NaN: the column's weights are dropped)
                 s_col[(tid >> 1) * 4 + (tid & 1)] = sum * up * kKeyUnit;
                 s_col[(tid >> 1) * 4 + 2 + (tid & 1)] = lse;
                 unsigned char *to = s_q + tid * 128;
@@ -649,17 +650,21 @@ weigh_wide_kernel(const __grid_constant__ ChunkParams P)
                                 const float4 v = col[j];
                                 const float2 got = make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), rho = make_float2(v.x, v.y),
                                              less = make_float2(-v.z, -v.w);
-                                float2 e;
+                                float2 e, f;
                                 if constexpr (even) {
                                     e = fma2(a, got, fma2(m, rho, less));
                                 } else {
-                                    const float2 f = *reinterpret_cast<const float2 *>(s_factor + c + 2 * j);
+                                    f = *reinterpret_cast<const float2 *>(s_factor + c + 2 * j);
                                     e = fma2(fma2(make_float2(par.x, par.x), got, __fmul2_rn(make_float2(par.y, par.y), rho)), f, less);
                                 }
                                 float2 p = make_float2(ex2f(e.x), ex2f(e.y));
                                 if (!plain) {
                                     if (c + 2 * j < from || c + 2 * j >= n_rows) p.x = 0.f;
                                     if (c + 2 * j + 1 < from || c + 2 * j + 1 >= n_rows) p.y = 0.f;
+                                }
+                                if constexpr (!even) {
+                                    if (f.x != f.x) p.x = 0.f;
+                                    if (f.y != f.y) p.y = 0.f;
                                 }
                                 if (j & 1) s1 = add2(s1, p); else s0 = add2(s0, p);
                             }

@@ -77,3 +77,32 @@ def test_a_row_that_is_no_number_spoils_what_it_sees_only(rows, D, dtype, value)
     seen = slots_of(p, 0, range(int(p.start[0]) + token + 1)).cpu().numpy()
     want[seen // 16, 0, seen % 16] = np.nan
     within(got, want, tol, "weights")
+
+
+@pytest.mark.parametrize("rows", sorted(COUNTS))
+@pytest.mark.parametrize("value", [1.0, 2.0 ** 60, float("inf"), float("nan")])
+def test_rows_without_an_lse_count_nothing_whatever_their_queries(rows, value):
+    p, token = _problem(rows, 128, torch.bfloat16)
+    lse, w = plain_lse(p), _weights(p)
+    p.q[token, 1, 5], lse[token, 1] = value, float("-inf")
+    got = _run(p, lse, w)
+    p.q[token, 1] = 0.0
+    want, tol = _statement(p, lse, w)
+    within(got, want, tol, "weights")
+
+
+@pytest.mark.parametrize("rows", sorted(COUNTS))
+def test_rows_without_an_lse_count_nothing_whatever_the_keys(rows):
+    """The last token alone sees the last key, which is NaN, and counts nothing: that key starts at 0."""
+    p, _ = _problem(rows, 64, torch.bfloat16)
+    lse, w = plain_lse(p), _weights(p)
+    n = COUNTS[rows][0]
+    last = slots_of(p, 0, [int(p.start[0]) + n - 1])
+    bad = torch.full((1, 2, 64), float("nan"), device="cuda")
+    binding.mcsd_append_kv(p.cache, bad, bad, last)
+    lse[n - 1] = float("-inf")
+    got = _run(p, lse, w)
+    want, tol = _statement(p, lse, w)
+    at = int(last)
+    assert (want[at // 16, :, at % 16] == 0).all()
+    within(got, want, tol, "weights")
