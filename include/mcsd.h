@@ -662,7 +662,8 @@ typedef struct mcsd_chunk_desc {
     int32_t dtype;           /* of q and out: MCSD_DTYPE_BF16 or MCSD_DTYPE_F16                        */
     int32_t max_pages;       /* columns of page_table that exist; max_pages * page_size < 2^31         */
     int32_t max_new;         /* new tokens that a sequence has at most (rows of further ones are left
-                                as they were); <= 2^24                                                 */
+                                as they were); <= 2^24, and min(max_new, n_tokens) times the query
+                                heads of a key head < 2^31 - 256                                       */
     int32_t reserved;        /* must be 0                                                             */
     int64_t n_tokens;        /* rows of q, out and lse; <= 2^31 - 1                                    */
     int64_t ld_table;        /* entries between rows of page_table, >= max_pages                       */

@@ -21,6 +21,9 @@ int check_chunk(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache)
     if (d->n_heads % cache->n_heads != 0) return MCSD_ERR_SHAPE;
     if (d->n_heads / cache->n_heads > MCSD_MAX_GROUP || d->max_new > 1 << 24 || d->n_tokens > 0x7fffffffLL) return MCSD_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(d->max_pages) * cache->page_size > 0x7fffffffLL - 512) return MCSD_ERR_UNSUPPORTED;
+    // (rows of a sequence, and those that a last block has room for beyond them, are counted in 32 bits)
+    const int64_t most = d->max_new < d->n_tokens ? d->max_new : d->n_tokens;
+    if (most * (d->n_heads / cache->n_heads) > 0x7fffffffLL - kChunkRows) return MCSD_ERR_UNSUPPORTED;
     // (the cuts count places of all blocks, and of all units with their rows, in 64 bits)
     const double room = static_cast<double>(d->max_pages) * cache->page_size + d->max_new + 1024.0;
     if ((static_cast<double>(d->n_tokens) + d->batch) * cache->n_heads * room > 4e18) return MCSD_ERR_UNSUPPORTED;
