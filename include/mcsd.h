@@ -723,7 +723,7 @@ typedef struct mcsd_evict_desc {
     const int32_t *len;          /* [B] rows held, clipped to max_pages * page_size                    */
     const int32_t *keep_len;     /* [B] or NULL: keep                                                 */
     float *weights;              /* [n_layers][n_pages][n_heads][page_size]                            */
-    int32_t *len_out;            /* [B] rows held afterwards, or NULL; must not be len                 */
+    int32_t *len_out;            /* [B] rows held afterwards, or NULL; overlaps neither len nor keep_len */
     void *stream;
 } mcsd_evict_desc;
 int mcsd_evict_rows(const mcsd_evict_desc *desc, const mcsd_kv_cache *cache);

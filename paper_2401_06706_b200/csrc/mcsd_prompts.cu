@@ -1,6 +1,7 @@
 // Host side of the operators of prompts and long conversations: argument validation, launch configuration and the
 // extern "C" entry points from mcsd_chunk_attention on (mcsd.h).
 #include <cmath>
+#include <initializer_list>
 
 #include "mcsd_chunk.cuh"
 #include "mcsd_chunk_wide.cuh"
@@ -294,8 +295,13 @@ int mcsd_evict_rows(const mcsd_evict_desc *d, const mcsd_kv_cache *cache)
     set_last_launches(0);
     if (d->batch == 0) return MCSD_OK;
     if (!d->len || (!d->page_table && d->max_pages > 0) || (!d->weights && cache->n_pages > 0)) return MCSD_ERR_NULL;
-    if (d->len_out == d->len) return MCSD_ERR_SHAPE;
     if (!on_multiples(4, d->page_table, d->len, d->keep_len, d->weights, d->len_out)) return MCSD_ERR_STRIDE;
+    // (what some CTAs read, others must not write)
+    const uintptr_t out = reinterpret_cast<uintptr_t>(d->len_out), bytes = 4 * static_cast<uintptr_t>(d->batch);
+    for (const int32_t *read : {d->len, d->keep_len}) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(read);
+        if (out && at && out < at + bytes && at < out + bytes) return MCSD_ERR_SHAPE;
+    }
     if (d->n_layers > (1LL << 40) / (static_cast<int64_t>(d->batch) * cache->n_heads)) return MCSD_ERR_UNSUPPORTED;
     EvictParams p = {};
     p.c = cache_params(cache);

@@ -19,3 +19,20 @@ def test_rows_of_a_chunk_are_counted_in_32_bits(lib, n_tokens, fits):
     assert _attend(lib, d) == (-8 if fits else -10)
     assert _weigh(lib, d, q=None) == (-1 if fits else -10)
     assert (lib.mcsd_chunk_attention_workspace_bytes(d, _cache()) > 0) == fits
+
+
+@pytest.mark.parametrize("change,code", [
+    ({"keep_len": FAKE + 64, "len_out": FAKE + 64}, -2),                                     # the kernel reads it as one that nothing writes
+    ({"keep_len": FAKE + 64, "len_out": FAKE + 68}, -2), ({"keep_len": FAKE + 68, "len_out": FAKE + 64}, -2),
+    ({"len_out": FAKE + 4}, -2), ({"len_out": FAKE - 4}, -2),
+    ({"keep_len": FAKE + 64, "len_out": FAKE + 66}, -7)])
+def test_new_lengths_overlap_neither_the_lengths_nor_what_to_keep(lib, change, code):
+    """(Two sequences: eight bytes each.)"""
+    assert lib.mcsd_evict_rows(_evict(len=FAKE, **change), _cache()) == code
+
+
+def test_arrays_side_by_side_are_no_overlap(lib):
+    """(Taken as far as the descriptor's last check: more layers than a grid counts.)"""
+    for change in ({"keep_len": FAKE + 64, "len_out": FAKE + 72}, {"keep_len": FAKE + 64, "len_out": FAKE + 56}, {"len_out": FAKE + 8}, {"len_out": FAKE - 8},
+                   {"keep_len": FAKE, "len_out": None}):
+        assert lib.mcsd_evict_rows(_evict(n_layers=1 << 40, **change), _cache()) == -10
