@@ -757,7 +757,7 @@ typedef struct mcsd_logprob_desc {
     float *entropy;              /* [n_out]; NULL to skip                                             */
     int32_t *top_ids;            /* [n_out][n_top]; NULL to skip                                      */
     float *top_logprobs;         /* [n_out][n_top]; NULL to skip                                      */
-    float temperature;           /* > 0, finite                                                       */
+    float temperature;           /* > 0, finite, and log2(e) / temperature finite in float32 (4.24e-39) */
     int32_t reserved;            /* must be 0                                                         */
     void *stream;
 } mcsd_logprob_desc;

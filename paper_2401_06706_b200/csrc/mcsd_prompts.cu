@@ -324,7 +324,7 @@ int mcsd_token_logprobs(const mcsd_logprob_desc *d)
     if (d->n_top > d->vocab) return MCSD_ERR_SHAPE;
     if (d->vocab > MCSD_MAX_VOCAB || d->n_top > MCSD_MAX_TOP || d->n_out > 0x7fffffffLL) return MCSD_ERR_UNSUPPORTED;
     if (!good_dtype(d->dtype)) return MCSD_ERR_DTYPE;
-    if (!(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.f / d->temperature)) return MCSD_ERR_TEMPERATURE;
+    if (!(d->temperature > 0.f) || !std::isfinite(d->temperature) || !std::isfinite(1.4426950408889634f / d->temperature)) return MCSD_ERR_TEMPERATURE;
     if (d->path_nodes && (d->row_index || d->path_len < 1 || d->nodes_per_tree < 1 || d->n_out % d->path_len != 0)) return MCSD_ERR_SHAPE;
     if (d->ld < d->vocab) return MCSD_ERR_STRIDE;
     set_last_launches(0);

@@ -36,3 +36,9 @@ def test_arrays_side_by_side_are_no_overlap(lib):
     for change in ({"keep_len": FAKE + 64, "len_out": FAKE + 72}, {"keep_len": FAKE + 64, "len_out": FAKE + 56}, {"len_out": FAKE + 8}, {"len_out": FAKE - 8},
                    {"keep_len": FAKE, "len_out": None}):
         assert lib.mcsd_evict_rows(_evict(n_layers=1 << 40, **change), _cache()) == -10
+
+
+@pytest.mark.parametrize("temperature,code", [(1.2e-38, -1), (4.3e-39, -1), (4.2e-39, -5), (3.0e-39, -5), (2.9e-39, -5)])
+def test_temperatures_whose_factor_is_out_of_range(lib, temperature, code):
+    """log2(e) / temperature has to be a float32: up to 2^128 / 1.4427 = 1 / 4.2397e-39. (Null logits end the calls that pass.)"""
+    assert lib.mcsd_token_logprobs(_logprobs(temperature=temperature, logits=None)) == code
