@@ -167,28 +167,26 @@ struct TreeRows {
     struct Walk {
         AttCut cut;
         AttCursor cur;
-        uint32_t u, u_end, places, items;
+        uint32_t u, u_end;
+        AttPiece piece;
         __device__ __forceinline__ bool begin(const AttendParams &P, int lane)
         {
-            items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
+            const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
             cut = att_cut(P, items, lane);
             if (cut.span == 0 || blockIdx.x > (cut.span - 1) / cut.per) return false;      // (runs before the last one are whole)
             u = blockIdx.x * cut.per;
             u_end = cut.span - u < cut.per ? cut.span : u + cut.per;
             cur = att_find(P, cut, u, items, lane);
-            places = 0u;
             return true;
         }
+        // What the run has at its place (false: nothing any more), and, behind the work on it, the way to the next place. (Both in one step ahead of
+        // the work took more registers: 26.0 -> 27.0 us of 8 sequences x 7 nodes, 32 heads on 8, 36.4 -> 37.8 of 13 nodes, 32 heads.)
         template <int ROWS>
-        __device__ __forceinline__ bool next(const AttendParams &P, int lane, AttItem &it)
+        __device__ __forceinline__ bool here(const AttendParams &P, int, AttItem &it)
         {
-            u += places;
-            cur.at += places;
             if (u >= u_end) return false;
-            if (places > 0u && cur.at >= cur.places * items) cur = att_find(P, cut, u, items, lane);
-            const AttPiece piece = att_piece(cut, cur, u_end - u);
+            piece = att_piece(cut, cur, u_end - u);
             if (piece.k1 <= 0) return false;
-            places = piece.places;
             it.b = cur.b;
             it.len = cur.len;
             it.head = piece.item / P.n_blocks;
@@ -199,6 +197,13 @@ struct TreeRows {
             it.k1 = piece.k1;
             it.whole = piece.k0 == 0 && piece.k1 == piece.units;
             return true;
+        }
+        __device__ __forceinline__ void on(const AttendParams &P, int lane)
+        {
+            const uint32_t items = static_cast<uint32_t>(P.c.n_heads * P.n_blocks);
+            u += piece.places;
+            cur.at += piece.places;
+            if (u < u_end && cur.at >= cur.places * items) cur = att_find(P, cut, u, items, lane);
         }
     };
     // (the joining kernel finds what was divided by itself)
@@ -273,7 +278,7 @@ __device__ __forceinline__ float att_factor(float m, float l, float top) { retur
 // pipe bounds it (53 % busy: an AND for every two codes and row block, a byte permutation and a shift for every
 // eight of the values), then the warps' own latencies; with queries as the long side (sixteen rows a block, a
 // maximum by shuffles in every chunk) the first took 165 us. Blocks of 24 rows take 255 registers, eight warps per SM; with
-// D = 128 every form spills a few words (16 to 92 bytes a thread).
+// D = 128 every form spills a few words (stored: 16 to 92 bytes a thread over a tree's rows, 12 to 276 over a chunk's).
 //
 // Row c of a tile of eight keys is key kappa(c): with this order (and, where a row has four 16-byte chunks, those of
 // rows 4 to 7 exchanged by two) every shared-memory load of codes touches each bank once.
@@ -304,7 +309,7 @@ narrow_kernel(const __grid_constant__ typename Rows::Params P)
     auto swizzle = [](int row, int chunk) { return D == 128 ? chunk ^ ((row >> 1) & 2) : chunk; };
     const int kg = kappa(g), ka = kappa(2 * t), kb = kappa(2 * t + 1);
 
-    while (walk.template next<ROWS>(P, lane, it)) {
+    for (; walk.template here<ROWS>(P, lane, it); walk.on(P, lane)) {
         const int k0 = it.k0, k1 = it.k1, b = it.b, len = it.len, head = it.head, row0 = it.row0, prefix = it.tail;
 
         __syncthreads();                            // the shared memory of the item before is free

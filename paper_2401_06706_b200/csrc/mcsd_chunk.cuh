@@ -226,6 +226,9 @@ struct ChunkRows {
                 return true;
             }
         }
+        template <int ROWS>
+        __device__ __forceinline__ bool here(const ChunkParams &P, int lane, AttItem &it) { return next<ROWS>(P, lane, it); }
+        __device__ __forceinline__ void on(const ChunkParams &, int) {}
     };
     static __device__ __forceinline__ void begun(const ChunkParams &P) { chunk_join_none(P); }
     static __device__ __forceinline__ void divided(const ChunkParams &P, const AttItem &it) { chunk_join_note(P, it); }
