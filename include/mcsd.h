@@ -683,7 +683,8 @@ size_t mcsd_chunk_attention_workspace_bytes(const mcsd_chunk_desc *desc, const m
  * position is 0 with lse = -inf.  q, out device [n_tokens][n_heads][D] with the given strides (out may be q, with the same strides; they
  * must not overlap otherwise); lse device [n_tokens][n_heads] float32 or NULL; page_table [batch][ld_table], start
  * [batch], cu_tokens [batch + 1] device int32.  Calls that may overlap on the device need workspaces of their own.
- * Precision: scores and lse are float32 (lse of 600 rows was off by 1e-5 at most); cached values and the weights that multiply them are rounded to half (2^-11
+ * Precision: scores and lse are float32, held to D 2^-24 of |scale| sum |q| (|mid| + 15 scale_j), the sizes of a score's parts, and 2^-19 (normal queries over 600
+ * rows: lse off by 1e-5 at most, measured); cached values and the weights that multiply them are rounded to half (2^-11
  * of each; a weight below 2^-18 of the row's largest so far by 2^-29 of that one), sums are float32.  bf16 queries above 2^112 count as infinite (NaN).  A key or
  * value that is NaN makes the rows NaN that see it.  Results depend on the sizes, the lengths and the GPU, not on timing.  A
  * row whose kernel gave up a wait (see MCSD_OPT_WAIT_POLLS) is NaN. */

@@ -61,7 +61,9 @@ __device__ __forceinline__ LogprobSums join_sums(const LogprobSums &a, const Log
 // one correction), which a tree of shuffles joins. For the largest tokens that maximum is all that the pass costs: the n-th
 // largest of the 64 group maxima is reached by n elements at least, so that only threads whose own maximum reaches it look at their
 // elements again (from L2) and hand those that do to a list, of which the n first are taken by counting. A row whose list
-// overflows (many equal logits) is searched n times instead.
+// overflows is searched n times instead, element by element: one with many equal logits, and one in which fewer than n groups have a finite
+// logit, so that the bar is -inf or the value of a mask (few allowed tokens; short 16-bit rows on 1024 threads, whose groups are neighbours). That is slow: 98 instead of 14 us for 8 rows of 32000 bf16
+// logits with 20 allowed and 20 asked for, 480 instead of 39 for 1021 of them, 46 for 8 rows of 2000 (12 in fp32).
 // Sums of a thread (V / THREADS terms) and their joining are float32: an error of 2^-22 of the result or so; a distance from the maximum
 // is formed before it is scaled, so that the lowest finite logits (a mask) do not overflow against one another.
 // Bound by the reading of the logits and by the tail of a row (joining, candidates), in which a CTA reads nothing; eight CTAs an SM overlap that: 1021 rows of

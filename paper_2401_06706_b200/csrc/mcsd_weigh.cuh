@@ -362,7 +362,7 @@ template <int D> constexpr int kWeighWideSmem = 1024 + (2 + kWeighKeys) * kWideT
 // Sequences with more rows than a block take the units once for every block; a key's sum then goes on from what its thread wrote before.
 // Of the products only half a softmax is left: one multiply-add, one exponential and one addition per score, in pairs where there is such an instruction.
 // 2 x 1500 tokens over 2500 rows, 16 heads of 64: 88 us (floor 11 by the products), 124 with rows far apart in every block; 8 windows of 32 tokens over 3500
-// rows, 4 heads to a key head: 27 and 32 (3.7 by the bytes); 2048 tokens over 8000, 32 heads on 8 of 128: 432. Bound by a group's way through a unit (read the scores, weights, wait: 6300 cycles per 128 x 256), the
+// rows, 4 heads to a key head: 27 and 32 (3.7 by the products); 2048 tokens over 8000, 32 heads on 8 of 128: 432. Bound by a group's way through a unit (read the scores, weights, wait: 6300 cycles per 128 x 256), the
 // products are done in a third of it.
 template <int DT, int D>
 __global__ void __launch_bounds__(kWeighThreads, 1)
