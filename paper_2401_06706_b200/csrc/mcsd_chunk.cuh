@@ -26,6 +26,8 @@ struct ChunkParams {
     int32_t last;                                   // tokens whose weights count, 0: all
     int32_t q_vec, o_vec;                           // rows of q may be read, those of out written in 16-byte vectors
     float scale, decay;
+    float scale_part;                               // |scale| log2(e) = scale_part 2^scale_power, the part below 1
+    int32_t scale_power;
     uint32_t wait_polls, test_extra;                // (as in AttendParams)
 };
 

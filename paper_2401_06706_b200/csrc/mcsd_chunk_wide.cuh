@@ -253,8 +253,8 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                         }
                     const int key = key0 + lane;
                     float *par = reinterpret_cast<float *>(s_param + keep * (kAttUnit / 2) + (key >> 1)) + (key & 1);
-                    par[0] = p.x;
-                    par[2] = fmaf(-8.f, p.x, p.y);
+                    par[0] = p.x * P.scale_part;
+                    par[2] = fmaf(-8.f, p.x, p.y) * P.scale_part;
                     const uint32_t keys = __ballot_sync(0xffffffffu, mine);
                     if (lane == 0) { s_valid[keep][warp & 3] = keys; s_bad[keep][warp & 3] = bad; s_far[keep][warp & 3] = far; }
                 } else {
@@ -368,7 +368,7 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
             const int token = min(row, it.rows - 1) / P.group - it.row0 / P.group;
             const int sees = static_cast<int>(min(static_cast<long long>(it.tail) + token, static_cast<long long>(it.len)));
             const int all = static_cast<int>(min(static_cast<long long>(it.tail) + min(it.row0 + 128 * x, it.rows - 1) / P.group - it.row0 / P.group, static_cast<long long>(it.len)));
-            float rho = 0.f, ra = 0.f;              // score in log2 units: ra (scale acc + (mid - 8 scale) rho)
+            float rho = 0.f, ra = 0.f;              // score in log2 units: ra (scale acc + (mid - 8 scale) rho), ra a power of two
             const int k0 = it.k0, k1 = it.k1;
             const bool any = k0 < units;            // (of the tile)
             if (any) {
@@ -406,7 +406,7 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                 int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 126 : 0;
                 e = max(min(e, 112), -110);
                 const float up = __int_as_float((127 + 15 - e) << 23) * (P.scale < 0.f ? -1.f : 1.f);
-                ra = ldexpf(fabsf(P.scale) * 1.4426950408889634f, e - 15 + 24);
+                ra = ldexpf(1.f, P.scale_power + e - 15 + 24);
                 float2 sum = make_float2(0.f, 0.f);
                 const float2 f0 = make_float2(up, up), f1 = make_float2(up * 0.0625f, up * 0.0625f);
 #pragma unroll 2
@@ -482,8 +482,9 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                             }
                         }
                         const float high = most * ra - kChunkHead;
-                        if (__any_sync(0xffffffffu, high > ref + kNarrowSlack)) {
-                            const float now = high > ref + kNarrowSlack ? high : ref;
+                        const bool move = high - ref > kNarrowSlack;            // (a difference that is exact, however large the two are)
+                        if (__any_sync(0xffffffffu, move)) {
+                            const float now = move ? high : ref;
                             const float f = ex2f(ref - now);
                             ref = now;
                             sum *= f;
@@ -502,7 +503,6 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                                 }
                             }
                         }
-                        const float rr = rho * ra;
                         float2 s2 = make_float2(0.f, 0.f);
                         // (What is stored lies over scores that are read: of weights in two parts, over all of them.)
                         constexpr int PER = PARTS == 2 ? 64 : 16;
@@ -519,9 +519,11 @@ chunk_wide_kernel(const __grid_constant__ ChunkParams P)
                                 const uint32_t see = ((first >> 5) + more ? see1 : see0) >> shift;
                                 const uint32_t far = s_far[keep][word + more] >> shift, bad = see & s_bad[keep][word + more] >> shift;
                                 const float4 kp = at[first / 2 + j];
-                                const float2 a = __fmul2_rn(make_float2(kp.x, kp.y), make_float2(ra, ra));
-                                const float2 m = fma2(make_float2(kp.z, kp.w), make_float2(rr, rr), make_float2(-ref, -ref));
-                                const float2 e = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), a, m);
+                                // (the same numbers as above, and their products with ra are exact: none is above its reference by more than the
+                                // slack, however large a step of the scores is)
+                                const float2 z = fma2(make_float2(__uint_as_float(acc[2 * j]), __uint_as_float(acc[2 * j + 1])), make_float2(kp.x, kp.y),
+                                                      __fmul2_rn(make_float2(kp.z, kp.w), make_float2(rho, rho)));
+                                const float2 e = fma2(z, make_float2(ra, ra), make_float2(-ref, -ref));
                                 float2 p = make_float2(see & 1u ? ex2f(e.x) : 0.f, see & 2u ? ex2f(e.y) : 0.f);
                                 s2 = add2(s2, p);
                                 if (far & 1u) p.x *= 16.f;

@@ -6,7 +6,7 @@ import torch
 
 import prompts_reference as ref
 from paper_2401_06706_b200 import binding
-from prompts_util import DTYPES, attention, host, plain_lse, problem, slots_of, within
+from prompts_util import DTYPES, attend, attention, check_attention, host, plain_lse, problem, slots_of, within
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,15 @@ def test_rows_without_an_lse_count_nothing_whatever_the_keys(rows):
     at = int(last)
     assert (want[at // 16, :, at % 16] == 0).all()
     within(got, want, tol, "weights")
+
+
+@pytest.mark.parametrize("rows", sorted(COUNTS))
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_attention_of_the_rows_beside_one_that_is_no_number(rows, D, value):
+    p, token = _problem(rows, D, torch.bfloat16)
+    p.q[token, 1, 7] = value
+    r = attend(p)
+    check_attention(p, r)
+    odd = torch.isnan(r.out).any(-1)
+    assert bool(odd[token, 1]) and int(odd.sum()) == 1
