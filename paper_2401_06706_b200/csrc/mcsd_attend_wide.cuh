@@ -283,8 +283,8 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 const float2 p = mine ? __half22float2(*reinterpret_cast<const __half2 *>(from + 32 * RB + lane * 4)) : make_float2(0.f, 0.f);
                 const int key = key0 + lane;
                 float *par = reinterpret_cast<float *>(s_param + stage * kAttUnit + (key >> 1) * 2 + which) + (key & 1);
-                par[0] = p.x;
-                par[2] = which ? p.y : fmaf(-8.f, p.x, p.y);
+                par[0] = which ? p.x : p.x * P.scale_part;
+                par[2] = which ? p.y : fmaf(-8.f, p.x, p.y) * P.scale_part;
                 if (which == 0) {
                     const uint32_t keys = __ballot_sync(0xffffffffu, mine);
                     if (lane == 0) s_valid[stage][warp & 3] = keys;
@@ -357,7 +357,7 @@ wide_kernel(const __grid_constant__ AttendParams P)
             const bool busy = row0 + (r & ~31) < P.n_rows;        // this warp has rows
             const int prefix = P.prefix_len[b];
             const int node = row < P.n_rows ? row / P.group : 0, h = head * P.group + (row - node * P.group);
-            float rho, ra;                          // score in log2 units: ra (scale acc + (mid - 8 scale) rho)
+            float rho, ra;                          // score in log2 units: ra (scale acc + (mid - 8 scale) rho), ra a power of two
             if (x == 0) {
                 // Q to tensor memory, scaled by a power of two to the top of half's range (and to a positive softmax scale)
                 uint4 raw[D / 8];
@@ -389,7 +389,9 @@ wide_kernel(const __grid_constant__ AttendParams P)
                 int e = most > 0.f ? static_cast<int>(__float_as_uint(most) >> 23) - 126 : 0;
                 e = max(min(e, 112), -110);
                 const float up = __int_as_float((127 + 15 - e) << 23) * (P.scale < 0.f ? -1.f : 1.f);
-                ra = ldexpf(fabsf(P.scale) * 1.4426950408889634f, e - 15 + 24);
+                // (a power of two: products with it are exact, so that a weight and its row's reference go by the same number, however
+                // large a step of the scores is; the rest of the scale is in the keys' parameters)
+                ra = ldexpf(1.f, P.scale_power + e - 15 + 24);
                 rho = sum * up * 5.9604644775390625e-8f;          // 2^-24
 #pragma unroll
                 for (int c0 = 0; c0 < D / 32; ++c0) {

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <atomic>
+#include <cmath>
 
 #include "mcsd_cache.cuh"
 #include "mcsd_host.h"
@@ -61,6 +62,15 @@ int launched(int n)
     if (cudaGetLastError() != cudaSuccess) return MCSD_ERR_CUDA;
     set_last_launches(n);
     return MCSD_OK;
+}
+
+// |scale| in log2 units as a part below 1 and a power of two.
+float scale_part(float scale, int32_t *power)
+{
+    int e = 0;
+    const float part = std::frexp(std::fabs(scale) * 1.4426950408889634f, &e);
+    *power = e;
+    return part;
 }
 
 int check_cache(const mcsd_kv_cache *c)

@@ -346,6 +346,7 @@ int mcsd_tree_attention(const mcsd_attention_desc *desc, const mcsd_kv_cache *ca
     p.o_seq = desc->out_seq_stride; p.o_node = desc->out_node_stride; p.o_head = desc->out_head_stride;
     p.batch = desc->batch; p.n_nodes = desc->n_nodes; p.n_heads = desc->n_heads; p.max_pages = desc->max_pages;
     p.scale = desc->scale;
+    p.scale_part = scale_part(desc->scale, &p.scale_power);
     const int polls = mcsd_get_option(MCSD_OPT_WAIT_POLLS);
     p.wait_polls = polls > 0 ? static_cast<uint32_t>(polls) : kWaitPolls;
     p.test_extra = mcsd_get_option(MCSD_OPT_TEST_EXTRA_TX) > 0 ? 1u : 0u;

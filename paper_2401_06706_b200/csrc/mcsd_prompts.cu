@@ -45,9 +45,7 @@ ChunkParams chunk_params(const mcsd_chunk_desc *d, const mcsd_kv_cache *cache, c
     p.batch = d->batch; p.n_heads = d->n_heads; p.max_pages = d->max_pages; p.max_new = d->max_new;
     p.group = d->n_heads / cache->n_heads;
     p.scale = d->scale;
-    int power = 0;
-    p.scale_part = std::frexp(std::fabs(d->scale) * 1.4426950408889634f, &power);
-    p.scale_power = power;
+    p.scale_part = scale_part(d->scale, &p.scale_power);
     p.q_vec = (reinterpret_cast<uintptr_t>(q) | 2ull * static_cast<unsigned long long>(d->q_token_stride | d->q_head_stride)) % 16 == 0;
     return p;
 }

@@ -3,6 +3,7 @@ scores as the kernel has them, and finite, whichever kernel has the rows."""
 import pytest
 import torch
 
+import test_gpu_ops_attention as trees
 from paper_2401_06706_b200 import binding
 from prompts_util import attend, check_attention, problem
 
@@ -26,3 +27,13 @@ def test_chunks(power, D, counts, heads, kv):
     r = attend(p)
     check_attention(p, r)                            # (the tolerance of the loud rows is as large as their scores' steps)
     _in_reach(r.out, p.cache)
+
+@pytest.mark.parametrize("power", POWERS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kconfig,heads,kv", [("", 4, 2), ("4x2x2x1", 2, 2), ("4x2x2x1", 4, 2), ("4x4x2x2x1", 4, 2), ("8x8x6", 2, 1)])
+def test_trees(power, D, kconfig, heads, kv):
+    parent, q, cache, table, prefix = trees._problem(45, 2, kconfig, heads, kv, D, 16, [700, 301], torch.bfloat16)
+    q[:, ::3, 1] *= 2.0 ** power
+    r = trees._run(q, cache, table, prefix, parent)
+    trees._check(q, cache, table, prefix, parent, r.out, r.lse)
+    _in_reach(r.out, cache)
