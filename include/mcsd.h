@@ -694,7 +694,8 @@ int mcsd_chunk_attention(const mcsd_chunk_desc *desc, const mcsd_kv_cache *cache
 /* What every cached row of the sequences with new tokens gathers of their attention, per key/value head:
  *   weights[p] := (p < start[b] and decay != 0 ? decay * weights[p] : 0) + sum exp(s_p - lse)
  * over the last `last_tokens` new tokens of the sequence (0: all of them) that see p and the query heads of the key head, with s as
- * above and lse as mcsd_chunk_attention gave it (rows with lse = -inf count nothing).  weights: device float32 [n_pages][cache->n_heads]
+ * above and lse as mcsd_chunk_attention gave it (rows with lse = -inf count nothing).  A share below 2^-126 counts as 0; it carries exp of its score's error,
+ * which with scores beyond 2^20 or so is no number to go by.  weights: device float32 [n_pages][cache->n_heads]
  * [page_size], a number for each row of the cache.  Rows of sequences without new tokens keep theirs.  Sums are float32 in a
  * fixed order.  No two sequences with new tokens may share a page.  Of the descriptor the strides of out and the workspace are not read; a wait given
  * up makes weights NaN, as above. */
